@@ -510,6 +510,131 @@ int tent_release(tent_ctx *ctx, tent_batch_t batch);
 int tent_probe_copy(const void *read_window, void *write_window, uint64_t bytes, uint32_t page_bytes,
                     uint32_t repeats, void *stream, float *ms_out);
 
+/*
+ * Operators on paged key/value caches.
+ *
+ * What the engine moves between pools is filled, shrunk and answered from by four operators on the pages themselves:
+ * tent_kv_append writes the keys and values of new tokens, tent_kv_pack turns 16-bit pages into 4-bit pages (for a
+ * migration of 3.8 times fewer bytes), tent_kv_read returns tokens as dense rows, tent_kv_attend computes softmax
+ * attention over the pages.  They need no context, allocate nothing, keep nothing between calls, only enqueue kernels on
+ * `stream` (so they can be recorded into a graph) and launch on the device that is current.  Structures are host memory
+ * and are copied before the call returns; everything that they point to is device memory.
+ *
+ * A page holds `page_tokens` tokens of `kv_heads` heads of `head_dim` values.  K and V lie in pools of their own, at the
+ * same page numbers.  A 16-bit page is [token][head][dim].  A 4-bit page is the codes, [token][head][dim / 2], followed
+ * by the scales, [token][head][dim / 32]: 32 values of a head share a power of two 2^(scale - 127); a code is a sign
+ * (8) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0..7), the even dimension in a byte's low half.  The power is the least at
+ * which no value of the block exceeds 7 times it (values above 6 times it become 6 times it), at least 2^-127 and at most
+ * 2^125 (TENT_BF16), or 2^-23 and 2^13 (TENT_FP16), so that every stored value is one of the 16-bit type; values go to the
+ * nearest code, ties to the even one.  A block that holds an infinity or a NaN is scale 255, codes 0, and reads as NaN.
+ *
+ * Rows.  A call works on the last tokens of `n_seqs` sequences, `n_rows` rows in all: the rows of sequence s are
+ * row_start[s] .. row_start[s + 1] - 1, and its kv_len[s] tokens include them, so row r stands for the token at position
+ * kv_len[s] - row_start[s + 1] + r.  Token t of sequence s is in page page_table[s * table_stride + t / page_tokens].
+ * Lengths and page numbers are read on the device, where a wrong one cannot be refused any more: it is left out, and noted
+ * in `*errors` if that is given (bits are only ever set).  TENT_KV_BAD_SEQUENCE: rows outside 0 .. n_rows, or more than
+ * max_rows of them, or kv_len outside 0 .. max_kv; nothing is written of the sequence.  TENT_KV_BAD_PAGE: a page number
+ * outside the pool; nothing is written there, tent_kv_read returns zeros for its tokens and tent_kv_attend does not see
+ * them.  TENT_KV_BAD_POSITION: a row at a negative position (kv_len below the number of rows) or outside the rotation's
+ * table; tent_kv_append and tent_kv_read write nothing of it.  Output rows that are left out, or belong to no sequence,
+ * keep what they held.  Two tokens at one place of a pool, or pages written twice by one call, have no defined order.
+ *
+ * Alignment: pools, rows, tables of rotations, norm weights and the workspace start at multiples of 16 bytes, strides are
+ * whole multiples of 16 bytes.  TENT_ERR_INVALID for null pointers, other alignments, unknown types and flags,
+ * TENT_ERR_RANGE for sizes that are not supported or do not go together.
+ */
+enum { TENT_BF16 = 0, TENT_FP16 = 1 };                      /* tent_kv_cache.type                                    */
+enum { TENT_KV_BAD_SEQUENCE = 1, TENT_KV_BAD_PAGE = 2, TENT_KV_BAD_POSITION = 4 };
+enum { TENT_KV_MAX_HEADS = 1024, TENT_KV_MAX_PAGE_TOKENS = 1024 };
+enum { TENT_KV_ROPE_PAIRS = 1u << 0 };                      /* tent_kv_append_args.flags: rotate dims (2i, 2i+1)     */
+enum { TENT_KV_ATTEND_ALL = 1u << 0 };                      /* tent_kv_attend_args.flags: no row is causal           */
+
+typedef struct {
+    void    *k, *v;            /* device: pools of n_pages pages                                   */
+    uint64_t n_pages;          /* 1 .. 2^31 - 1                                                    */
+    uint64_t page_stride;      /* bytes from a page to the next, at least a page, a multiple of 16 */
+    uint32_t page_tokens;      /* a power of two, 1 .. TENT_KV_MAX_PAGE_TOKENS                     */
+    uint32_t kv_heads;         /* 1 .. TENT_KV_MAX_HEADS                                           */
+    uint32_t head_dim;         /* 64, 128 or 256                                                   */
+    uint32_t type;             /* TENT_BF16 or TENT_FP16: of 16-bit pages, and of the rows of every call */
+    uint32_t bits;             /* 16 or 4                                                          */
+    uint32_t reserved;         /* 0                                                                */
+} tent_kv_cache;
+
+typedef struct {
+    const int32_t *page_table; /* device [n_seqs][table_stride]                                    */
+    const int32_t *kv_len;     /* device [n_seqs]                                                  */
+    const int32_t *row_start;  /* device [n_seqs + 1], ascending                                   */
+    int32_t *errors;           /* device, or NULL                                                  */
+    uint32_t n_seqs;           /* 0: nothing to do; at most 65535                                  */
+    uint32_t table_stride;     /* entries from a sequence's page numbers to the next's             */
+    uint32_t n_rows;           /* 0: nothing to do                                                 */
+    uint32_t max_rows;         /* most rows of a sequence, at most n_rows                          */
+    uint32_t max_kv;           /* most tokens of a sequence, at most table_stride * page_tokens and 2^30 */
+    uint32_t reserved;         /* 0                                                                */
+} tent_kv_batch;
+
+typedef struct {
+    const void *q, *k, *v;     /* device [n_rows][heads][head_dim]; q may be NULL (with q_heads 0) */
+    void *q_out;               /* device [n_rows][q_heads][head_dim]; may be q with q's stride     */
+    uint64_t q_stride, k_stride, v_stride, q_out_stride;    /* values from a row to the next       */
+    const void *q_weight, *k_weight;   /* device [head_dim]: RMS norm of every head, or NULL: none */
+    const float *rope;         /* device [rope_rows][rope_dim]: cosines of rope_dim / 2 angles, then their sines; or NULL */
+    const int32_t *positions;  /* device [n_rows]: row of `rope` for every row; or NULL: its position in the sequence */
+    uint32_t q_heads;          /* 0 .. TENT_KV_MAX_HEADS                                           */
+    uint32_t rope_rows, rope_dim;      /* rope_dim: a multiple of 16, at most head_dim             */
+    uint32_t flags;            /* TENT_KV_ROPE_PAIRS                                               */
+    float eps;                 /* of the norms: x / sqrt(mean(x^2) + eps) * weight                 */
+    uint32_t reserved;         /* 0                                                                */
+} tent_kv_append_args;
+
+typedef struct {
+    const void *q;             /* device [n_rows][q_heads][head_dim]                               */
+    void *out;                 /* device [n_rows][q_heads][head_dim]                               */
+    float *lse;                /* device [n_rows][q_heads], or NULL                                */
+    uint64_t q_stride, out_stride;     /* values from a row to the next                            */
+    void *workspace;           /* device: tent_kv_attend_workspace bytes; NULL where that is 0     */
+    uint64_t workspace_bytes;
+    uint32_t q_heads;          /* a multiple of kv_heads, at most TENT_KV_MAX_HEADS                */
+    uint32_t window;           /* a row sees the last `window` tokens up to its own; 0: all        */
+    uint32_t flags;            /* TENT_KV_ATTEND_ALL                                               */
+    float scale;               /* of the scores, above 0                                           */
+} tent_kv_attend_args;
+
+/* Bytes of a 4-bit page, rounded up to whole 16 (what page_stride has to be at least).  0 for sizes that are refused. */
+uint64_t tent_kv_packed_page(uint32_t page_tokens, uint32_t kv_heads, uint32_t head_dim);
+
+/* Normalise (RMS over a head, with a weight) and rotate the queries and keys of every row, write the queries to q_out and
+ * the keys and values to their pages.  Without `rope` nothing is rotated; dimensions from rope_dim on never are.
+ * Dimension i < rope_dim / 2 turns with i + rope_dim / 2 (TENT_KV_ROPE_PAIRS: 2i with 2i + 1) by angle i:
+ * (a, b) -> (a cos - b sin, b cos + a sin).  Keys are computed in 64 bits and rounded to 32 and from there to 16 bits, for
+ * both kinds of page, so a 4-bit cache holds what tent_kv_pack makes of a 16-bit one; queries are computed in 32 bits. */
+int tent_kv_append(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_append_args *args, void *stream);
+
+/* Pack `n_pages` whole pages: page src_pages[i] of the 16-bit cache `src` becomes page dst_pages[i] of the 4-bit cache
+ * `dst` (same page_tokens, kv_heads, head_dim and type).  Tokens of a page that hold nothing yet are packed as they are.
+ * A number outside its pool leaves that page out and is noted in *errors (may be NULL). */
+int tent_kv_pack(const tent_kv_cache *src, const tent_kv_cache *dst, const int32_t *src_pages, const int32_t *dst_pages,
+                 uint32_t n_pages, int32_t *errors, void *stream);
+
+/* The keys and values that the pages hold for every row of the batch, as rows of 16 bits: k_out and v_out are device
+ * [n_rows][kv_heads][head_dim] with `out_stride` values from a row to the next. */
+int tent_kv_read(const tent_kv_cache *cache, const tent_kv_batch *batch, void *k_out, void *v_out, uint64_t out_stride,
+                 void *stream);
+
+/* Device memory that tent_kv_attend needs for such a batch: parts of the result where the tokens of a sequence are split
+ * over several workgroups.  The least that the call takes; contents need no preparation and mean nothing afterwards. */
+int tent_kv_attend_workspace(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_attend_args *args,
+                             uint64_t *bytes);
+
+/* Attention of every row over its sequence: out = sum_t softmax_t(scale q . k_t) v_t over the tokens t that the row sees,
+ * its own and those before it (TENT_KV_ATTEND_ALL: all kv_len), within the window; query head h reads head
+ * h / (q_heads / kv_heads).  lse is the natural logarithm of the softmax's sum with its maximum (the logsumexp of the
+ * scores).  A row that sees no token, or only scores of minus infinity, gives zeros and lse minus infinity.  Tokens that a
+ * row does not see have no influence on it, whatever their values.  Scores and sums are 32 bits, weights are rounded to the
+ * 16-bit type (to nearest) before they multiply the values. */
+int tent_kv_attend(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_attend_args *args, void *stream);
+
 /* Static description of a status code. */
 const char *tent_strerror(int status);
 

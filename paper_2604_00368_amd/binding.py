@@ -28,7 +28,8 @@ EXPORTS = ["tent_create", "tent_destroy", "tent_register_segment", "tent_declare
            "tent_sim_advance", "tent_sim_latency", "tent_update_bandwidth", "tent_get_latencies", "tent_execute", "tent_poll", "tent_reset", "tent_slice_count",
            "tent_get_plan", "tent_get_timings", "tent_release", "tent_strerror",
            "tent_sim_fail", "tent_get_retries", "tent_monitor_init", "tent_monitor_update",
-           "tent_plan_dispatch", "tent_get_modes", "tent_execute_bounded", "tent_probe_copy", "tent_declare_static"]
+           "tent_plan_dispatch", "tent_get_modes", "tent_execute_bounded", "tent_probe_copy", "tent_declare_static",
+           "tent_kv_packed_page", "tent_kv_append", "tent_kv_pack", "tent_kv_read", "tent_kv_attend_workspace", "tent_kv_attend"]
 
 
 class tent_config(C.Structure):
@@ -54,6 +55,39 @@ SLICE_DTYPE = np.dtype(
     {"names": ["desc", "len", "off", "stage_off", "rail", "state"],
      "formats": ["<u4", "<u4", "<u8", "<u8", "<u4", "<u4"],
      "offsets": [0, 4, 8, 16, 24, 28], "itemsize": 32})
+
+
+# Operators on paged key/value caches (kv.py passes tensors to them)
+TENT_BF16, TENT_FP16 = 0, 1
+TENT_KV_BAD_SEQUENCE, TENT_KV_BAD_PAGE, TENT_KV_BAD_POSITION = 1, 2, 4
+TENT_KV_MAX_HEADS, TENT_KV_MAX_PAGE_TOKENS = 1024, 1024
+TENT_KV_ROPE_PAIRS, TENT_KV_ATTEND_ALL = 1, 1
+
+
+class tent_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_uint64), ("page_stride", C.c_uint64),
+                ("page_tokens", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("type", C.c_uint32),
+                ("bits", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tent_kv_batch(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("row_start", C.c_void_p), ("errors", C.c_void_p),
+                ("n_seqs", C.c_uint32), ("table_stride", C.c_uint32), ("n_rows", C.c_uint32), ("max_rows", C.c_uint32),
+                ("max_kv", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tent_kv_append_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p),
+                ("q_stride", C.c_uint64), ("k_stride", C.c_uint64), ("v_stride", C.c_uint64), ("q_out_stride", C.c_uint64),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("rope", C.c_void_p), ("positions", C.c_void_p),
+                ("q_heads", C.c_uint32), ("rope_rows", C.c_uint32), ("rope_dim", C.c_uint32), ("flags", C.c_uint32),
+                ("eps", C.c_float), ("reserved", C.c_uint32)]
+
+
+class tent_kv_attend_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("q_stride", C.c_uint64), ("out_stride", C.c_uint64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("q_heads", C.c_uint32), ("window", C.c_uint32),
+                ("flags", C.c_uint32), ("scale", C.c_float)]
 
 
 class TentError(RuntimeError):
@@ -108,6 +142,14 @@ def lib():
         L.tent_monitor_init.argtypes = [C.c_void_p, C.c_void_p, C.c_uint32]
         L.tent_monitor_update.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p,
                                           C.c_void_p, C.c_void_p]
+        L.tent_kv_packed_page.restype = C.c_uint64
+        L.tent_kv_packed_page.argtypes = [C.c_uint32, C.c_uint32, C.c_uint32]
+        cache, batch = C.POINTER(tent_kv_cache), C.POINTER(tent_kv_batch)
+        L.tent_kv_append.argtypes = [cache, batch, C.POINTER(tent_kv_append_args), C.c_void_p]
+        L.tent_kv_pack.argtypes = [cache, cache, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p]
+        L.tent_kv_read.argtypes = [cache, batch, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
+        L.tent_kv_attend_workspace.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.POINTER(C.c_uint64)]
+        L.tent_kv_attend.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.c_void_p]
         _lib = L
     return _lib
 
@@ -317,3 +359,31 @@ def tent_probe_copy(read_window: int, write_window: int, nbytes: int, page_bytes
 
 def tent_release(ctx, batch: int):
     _check(lib().tent_release(ctx, batch), "tent_release")
+
+
+def tent_kv_packed_page(page_tokens: int, kv_heads: int, head_dim: int) -> int:
+    """Bytes of a 4-bit page; 0 for sizes that are refused."""
+    return lib().tent_kv_packed_page(page_tokens, kv_heads, head_dim)
+
+
+def tent_kv_append(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_append_args, stream=None):
+    _check(lib().tent_kv_append(cache, batch, args, _stream(stream)), "tent_kv_append")
+
+
+def tent_kv_pack(src: tent_kv_cache, dst: tent_kv_cache, src_pages_ptr: int, dst_pages_ptr: int, n_pages: int, errors_ptr: int = 0,
+                 stream=None):
+    _check(lib().tent_kv_pack(src, dst, src_pages_ptr, dst_pages_ptr, n_pages, errors_ptr, _stream(stream)), "tent_kv_pack")
+
+
+def tent_kv_read(cache: tent_kv_cache, batch: tent_kv_batch, k_out_ptr: int, v_out_ptr: int, out_stride: int, stream=None):
+    _check(lib().tent_kv_read(cache, batch, k_out_ptr, v_out_ptr, out_stride, _stream(stream)), "tent_kv_read")
+
+
+def tent_kv_attend_workspace(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_attend_args) -> int:
+    n = C.c_uint64()
+    _check(lib().tent_kv_attend_workspace(cache, batch, args, n), "tent_kv_attend_workspace")
+    return n.value
+
+
+def tent_kv_attend(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_attend_args, stream=None):
+    _check(lib().tent_kv_attend(cache, batch, args, _stream(stream)), "tent_kv_attend")

@@ -1,0 +1,878 @@
+// Softmax attention over the pages of a key/value cache: tent_kv_attend.
+//
+//   s_rt = scale q_r . k_t,  m_r = max_t s_rt,  l_r = sum_t exp(s_rt - m_r),  o_r = sum_t exp(s_rt - m_r) v_t / l_r
+//
+// in one pass over the tokens with the running maximum and sum.  The query heads that share a head of the cache and the rows
+// of a sequence are one list of "lines" (line = row * group + head in the group), so the cache is read once for all of them.
+// Both kernels compute the transposed products S^T = K Q^T and O^T = V^T P^T: a lane then holds scores, weights and sums of
+// one line only, and the weights come out of the first product in the lanes where the second one wants them.  V is read
+// from LDS with the transposing read; K's rows may enter the first product in any order, which is chosen so that a lane gets
+// the tokens that its part of the second product sums over.
+//
+//   narrow_kernel  up to 64 lines: 16 lines to a matrix tile, each wave takes tokens of its own, the cache streams from HBM
+//                  through registers; bound by HBM
+//   wide_kernel    more lines: 128 to a workgroup, 32 to a wave, tiles of 64 tokens in LDS for all four waves; bound by the
+//                  matrix units and the softmax's vector work beside them
+//
+// Where lines are few and contexts long the tokens are split over workgroups; their parts (largest score, sum, output, all in
+// 32 bits) go through the workspace and are joined by join_kernel.
+#include "kv_elem.h"
+
+namespace tent {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// The maximum that weights are taken against may lag behind the true one by a factor of 2^8: sums and products are in 32 bits
+// and lose nothing by it, and most tiles then need no rescaling.
+constexpr float kLag = 8.f;
+constexpr int32_t kStep = 32;          // splits and the tokens that a workgroup begins with are multiples of it
+
+struct AttendArgs {
+    KvCache c;
+    tent_kv_batch b;
+    const uint8_t* q;
+    uint8_t* out;
+    float* lse;
+    uint64_t q_stride, out_stride;     // bytes
+    float* part_o;                     // [n_rows * q_heads][n_splits][D], or null: one split
+    float* part_ml;                    // [n_rows * q_heads][n_splits][2]
+    uint32_t q_heads, group, window, all;
+    float to_log2;                     // scale * log2(e)
+    uint32_t n_splits, split_tokens;   // tokens of a split: a multiple of 128
+    uint32_t line_tiles;               // workgroups over the lines of a sequence and head
+};
+
+// ---- what both kernels share ---------------------------------------------------------------------
+// A sequence's splits begin at the first token that its first row sees, rounded down to a whole step.
+__device__ __forceinline__ int32_t splits_from(const AttendArgs& g, const KvSeq& q)
+{
+    return kv_span(0, q.rows, q.len, g.window, g.all).lo & ~(kStep - 1);
+}
+__device__ __forceinline__ uint32_t splits_of(const AttendArgs& g, const KvSeq& q)
+{
+    const uint32_t span = (uint32_t)(q.len - splits_from(g, q));
+    const uint32_t n = (span + g.split_tokens - 1) / g.split_tokens;
+    return n < 1 ? 1 : n;
+}
+
+// The tokens that a workgroup goes through: those that its lines see, within its split.
+struct Range { int32_t lo, hi; };
+__device__ __forceinline__ Range token_range(const AttendArgs& g, const KvSeq& q, int32_t first_line, int32_t last_line, uint32_t split)
+{
+    const KvSpan a = kv_span(first_line / (int32_t)g.group, q.rows, q.len, g.window, g.all);
+    const KvSpan z = kv_span(last_line / (int32_t)g.group, q.rows, q.len, g.window, g.all);
+    const int64_t lo = (int64_t)splits_from(g, q) + (int64_t)split * g.split_tokens, hi = lo + g.split_tokens;
+    const int32_t first = a.lo & ~(kStep - 1);
+    return Range{first > lo ? first : (int32_t)lo, z.hi < hi ? z.hi : (int32_t)hi};
+}
+
+// Place of a token's row of this head in a pool: bytes to its values, or to its codes and its scales.
+template <int kBits>
+struct RowAt;
+template <>
+struct RowAt<16> { uint64_t row; };
+template <>
+struct RowAt<4> { uint64_t row, scale; };
+
+template <int D, int kBits>
+__device__ __forceinline__ RowAt<kBits> row_at(const KvCache& c, uint32_t page, uint32_t token, uint32_t head)
+{
+    const uint64_t at = page * c.page_stride;
+    const uint32_t r = (token & ((1u << c.page_shift) - 1u)) * c.heads + head;
+    if constexpr (kBits == 16) return RowAt<16>{at + (uint64_t)r * (D * 2)};
+    else return RowAt<4>{at + (uint64_t)r * (D / 2), at + ((uint64_t)(c.heads * (D / 2)) << c.page_shift) + (uint64_t)r * (D / 32)};
+}
+
+// Largest value, and sum, over the lanes that hold one line: lane ^ 32 and, where 16 lines make a tile, lane ^ 16.
+__device__ __forceinline__ float max_over32(float x)
+{
+    const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1]));
+}
+__device__ __forceinline__ float max_over16(float x)
+{
+    const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1]));
+}
+__device__ __forceinline__ float sum_over32(float x) { return x + __shfl_xor(x, 32, 64); }
+__device__ __forceinline__ float sum_over16(float x) { return x + __shfl_xor(x, 16, 64); }
+
+// The root of 2^(a - b), where a is what weights were taken against before and b what they are taken against now; nothing yet is
+// 0.  Sums are multiplied by it twice: the power itself may be below the least normal number where the product is not.
+__device__ __forceinline__ float rescale(float a, float b) { return a == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(0.5f * (a - b)); }
+
+// Sixteen-byte chunks of a token's row change places in LDS by the token, so that the rows' writes, the reads of K's rows by
+// 16 or 32 lanes and the transposing reads of V (four tokens by 16 or 32 dimensions) each spread over all banks.
+template <int D>
+__device__ __forceinline__ uint32_t v_swap(uint32_t t)
+{
+    return D == 64 ? ((t >> 1) & 1u) << 2 | ((t >> 2) & 3u) : (t & 3u) << 2 | ((t >> 2) & 3u);
+}
+template <int D>
+__device__ __forceinline__ uint32_t k_swap(uint32_t t)
+{
+    return D == 64 ? (t >> 1) & 7u : t & 15u;
+}
+
+// The lanes of 16 give the addresses of four values each, rows of 16 in the order of the lanes; lane i gets value i of each row.
+__device__ __forceinline__ u32x2 read_transposed(const uint8_t* p)
+{
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+}
+
+// LDS written by some lanes of a wave is read by others: the wave's LDS operations keep their order, the compiler has to as well.
+__device__ __forceinline__ void same_wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+// In a tile where some lines do not see some tokens, a value that is infinite or NaN would reach lines that do not see it,
+// by way of a weight of zero.  There zeros take the places of such values in LDS, and what lines see of them is added behind
+// the loop, in a second walk over those tiles (add_unfinite) that hardly any call takes.
+template <class E>
+__device__ __forceinline__ u32x4 finite_only(u32x4 v, bool& other)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((v[i] & 0x7FFFu) >= E::kInf) { v[i] &= 0xFFFF0000u; other = true; }
+        if (((v[i] >> 16) & 0x7FFFu) >= E::kInf) { v[i] &= 0xFFFFu; other = true; }
+    }
+    return v;
+}
+
+// Adds the values that are not finite among four of a row of V that a line sees: dims `dim` .. `dim` + 3.
+template <class E, int D, int kBits>
+__device__ __forceinline__ void add_unfinite(float* o, const uint8_t* pool, const RowAt<kBits>& at, uint32_t dim)
+{
+    if constexpr (kBits == 16) {
+        const u32x2 v = dev_load<u32x2>(pool + at.row + dim * 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = (v[i >> 1] >> (16 * (i & 1))) & 0xFFFFu;
+            if ((x & 0x7FFFu) >= E::kInf) o[i] += E::to_float(x);
+        }
+    } else {
+        if (dev_load<uint8_t>(pool + at.scale + dim / 32) != 255u) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = NAN;
+    }
+}
+
+__device__ __forceinline__ float lse_of(float top, float sum, float shift)
+{
+    return sum > 0.f ? kLn2 * (top - shift + __builtin_amdgcn_logf(sum)) : sum == 0.f ? -INFINITY : sum;
+}
+
+// ---- few lines -----------------------------------------------------------------------------------
+constexpr int kWaves = 4;
+constexpr int kTile = 32;              // tokens of a wave's step
+
+// One tile of a wave in registers.  K: lane (m = lane % 16, quad = lane / 16) has, for half 0 and 1, the token
+// 8 (m / 4) + 4 half + m % 4 and its dimensions (D / 4) quad ..: after the product, quad holds tokens 8 quad .. 8 quad + 7.
+// V: a token's row in lanes side by side, 16 bytes each.
+template <int D, int kBits>
+struct Tile {
+    static constexpr int kPerRow = kBits == 16 ? D / 8 : D / 32;         // lanes to a row of V
+    static constexpr int kPasses = kTile * kPerRow / 64;
+    static constexpr int kWords = kBits == 16 ? D / 8 : D / 32;          // registers of a lane's part of a row of K
+    uint32_t k[2][kWords];
+    uint32_t k_scale[2];
+    u32x4 v[kPasses];
+    uint32_t v_scale[kPasses];
+};
+
+template <class E, int D, int kBits, int kLineTiles>
+__global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
+{
+    constexpr int kK = D / 32;                                           // steps of the first product
+    constexpr int kDims = D / 16;                                        // tiles of 16 dimensions of the second
+    using T = Tile<D, kBits>;
+    constexpr uint32_t kVBytes = kWaves * kTile * D * 2, kOBytes = kWaves * 16 * (D + 4) * 4;
+    __shared__ __align__(16) uint8_t lds[kVBytes > kOBytes ? kVBytes : kOBytes];
+    __shared__ RowAt<kBits> rows_at[kWaves][kTile];
+    __shared__ float line_top[kWaves][16 * kLineTiles], line_sum[kWaves][16 * kLineTiles];
+
+    const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t m = lane & 15u, quad = lane >> 4;
+    // All heads of a (sequence, split) go to one XCD one after the other: the heads of a token share lines of its page.
+    const uint32_t eight = blockIdx.x / (8 * g.c.heads), in_eight = blockIdx.x - eight * 8 * g.c.heads;
+    const uint32_t unit = eight * 8 + in_eight % 8, head = in_eight / 8;
+    if (unit >= g.b.n_seqs * g.n_splits) return;
+    const uint32_t seq = unit / g.n_splits, split = unit - seq * g.n_splits;
+    const KvSeq q = kv_sequence(g.b, seq);
+    if (q.bad && threadIdx.x == 0 && split == 0 && head == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
+    if (q.rows == 0 || split >= splits_of(g, q)) return;
+    const int32_t lines = q.rows * (int32_t)g.group;                     // at most 16 kLineTiles, by the host's choice
+    const Range range = token_range(g, q, 0, lines - 1, split);
+
+    // This lane's line of every tile of 16: its queries as the second operand of S^T, and the tokens that it sees.
+    u32x4 qf[kLineTiles][kK];
+    KvSpan see[kLineTiles];
+#pragma unroll
+    for (int rt = 0; rt < kLineTiles; ++rt) {
+        const int32_t line = rt * 16 + (int32_t)m;
+        const int32_t row = line < lines ? line / (int32_t)g.group : 0, h = line < lines ? line - row * (int32_t)g.group : 0;
+        see[rt] = kv_span(row, q.rows, q.len, g.window, g.all);
+        const uint8_t* p = g.q + (uint64_t)(q.row0 + row) * g.q_stride + ((uint64_t)(head * g.group + h) * D + quad * (D / 4)) * 2;
+#pragma unroll
+        for (int k = 0; k < kK; ++k) qf[rt][k] = dev_load<u32x4>(p + k * 16);
+    }
+    // tokens that every line sees
+    const int32_t all_lo = kv_span(q.rows - 1, q.rows, q.len, g.window, g.all).lo, all_hi = kv_span(0, q.rows, q.len, g.window, g.all).hi;
+
+    f32x4 o[kLineTiles][kDims];
+    float top[kLineTiles], sum[kLineTiles];
+#pragma unroll
+    for (int rt = 0; rt < kLineTiles; ++rt) {
+        top[rt] = -INFINITY;
+        sum[rt] = 0.f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[rt][d] = f32x4{0, 0, 0, 0};
+    }
+
+    auto seen_by_all = [&](int32_t t0) -> bool { return t0 >= all_lo && t0 + kTile <= all_hi; };
+
+    // Waves take tiles in turn.  Page numbers are loaded two of a wave's tiles ahead, rows one ahead.
+    const int32_t tiles = (range.hi - range.lo + kTile - 1) / kTile;
+    auto load_page = [&](int32_t tile) -> uint32_t {
+        const int32_t t = range.lo + tile * kTile + (int32_t)(lane & 31u);
+        return t < range.hi ? (uint32_t)g.b.page_table[(uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift)] : 0u;
+    };
+    // Puts the places of a tile's rows into LDS and says which of its tokens are there; the others get the place of a row that is.
+    auto place_rows = [&](int32_t tile, uint32_t page) -> uint32_t {
+        const int32_t t = range.lo + tile * kTile + (int32_t)(lane & 31u);
+        const bool inside = t < range.hi, there = inside && page < g.c.n_pages;
+        if (lane < 32) {
+            rows_at[wave][lane] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
+            if (inside && !there) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
+        }
+        same_wave_order();
+        return (uint32_t)__ballot(there);
+    };
+    T tile_now;
+    auto load_k = [&]() {
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            const RowAt<kBits> at = rows_at[wave][8 * (m >> 2) + 4 * a + (m & 3)];
+            const uint8_t* p = g.c.k + at.row + quad * (T::kWords * 4);
+            if constexpr (T::kWords == 2) {
+                const u32x2 w = dev_load<u32x2>(p);
+                tile_now.k[a][0] = w[0];
+                tile_now.k[a][1] = w[1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < T::kWords / 4; ++i) {
+                    const u32x4 w = dev_load<u32x4>(p + i * 16);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) tile_now.k[a][i * 4 + j] = w[j];
+                }
+            }
+            if constexpr (kBits == 4) {
+                const uint8_t* sp = g.c.k + at.scale + quad * (D / 4) / 32;
+                tile_now.k_scale[a] = D == 256 ? dev_load<uint16_t>(sp) : dev_load<uint8_t>(sp);
+            }
+        }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+        for (int i = 0; i < T::kPasses; ++i) {
+            const RowAt<kBits> at = rows_at[wave][i * (64 / T::kPerRow) + lane / T::kPerRow];
+            tile_now.v[i] = dev_load<u32x4>(g.c.v + at.row + (lane % T::kPerRow) * 16);
+            if constexpr (kBits == 4) tile_now.v_scale[i] = dev_load<uint8_t>(g.c.v + at.scale + lane % T::kPerRow);
+        }
+    };
+    uint8_t* const v_lds = lds + wave * (kTile * D * 2);
+    uint32_t there = 0, next_page = 0;
+    bool unfinite = false;                                               // this lane met a value that is infinite or NaN in a tile that is not whole
+    if ((int32_t)wave < tiles) {
+        there = place_rows((int32_t)wave, load_page((int32_t)wave));
+        load_k();
+        load_v();
+        next_page = load_page((int32_t)wave + kWaves);
+    }
+    for (int32_t tile = (int32_t)wave; tile < tiles; tile += kWaves) {
+        const int32_t t0 = range.lo + tile * kTile;
+        const bool more = tile + kWaves < tiles;
+        uint32_t there_next = 0;
+        same_wave_order();
+        if (more) {
+            there_next = place_rows(tile + kWaves, next_page);
+            next_page = load_page(tile + 2 * kWaves);
+        }
+        // S^T
+        f32x4 s[kLineTiles][2];
+#pragma unroll
+        for (int rt = 0; rt < kLineTiles; ++rt) s[rt][0] = s[rt][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+#pragma unroll
+            for (int k = 0; k < kK; ++k) {
+                u32x4 kf;
+                if constexpr (kBits == 16) kf = u32x4{tile_now.k[a][k * 4], tile_now.k[a][k * 4 + 1], tile_now.k[a][k * 4 + 2], tile_now.k[a][k * 4 + 3]};
+                else kf = decode8<E>(tile_now.k[a][k], scale_of(tile_now.k_scale[a] >> (8 * (k / 4)) & 0xFFu));
+#pragma unroll
+                for (int rt = 0; rt < kLineTiles; ++rt) s[rt][a] = E::mfma16(kf, qf[rt][k], s[rt][a]);
+            }
+        }
+        if (more) load_k();
+        // V's rows to LDS, tokens that are not there as zeros
+        const bool whole = there == 0xFFFFFFFFu && seen_by_all(t0);
+#pragma unroll
+        for (int i = 0; i < T::kPasses; ++i) {
+            const uint32_t t = i * (64 / T::kPerRow) + lane / T::kPerRow, part = lane % T::kPerRow, x = v_swap<D>(t);
+            bool gone = !whole && !((there >> t) & 1u);
+            if constexpr (kBits == 16) {
+                u32x4 v = tile_now.v[i];
+                if (!whole) v = gone ? u32x4{0, 0, 0, 0} : finite_only<E>(v, unfinite);
+                *(u32x4*)(v_lds + t * (D * 2) + ((part ^ x) << 4)) = v;
+            } else {
+                if (!whole && !gone && tile_now.v_scale[i] == 255u) gone = unfinite = true;
+                const float scale = scale_of(gone ? 0u : tile_now.v_scale[i]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) *(u32x4*)(v_lds + t * (D * 2) + (((part * 4 + c) ^ x) << 4)) = decode8<E>(gone ? 0u : tile_now.v[i][c], scale);
+            }
+        }
+        same_wave_order();
+        if (more) load_v();
+        // O^T's first operand: tokens 8 quad .. 8 quad + 7 of 16 dimensions
+        const uint32_t vt = 8 * quad + (m >> 2);
+        const uint8_t *row_a = v_lds + vt * (D * 2) + (m & 1u) * 8, *row_b = row_a + 4 * (D * 2);
+        const uint32_t xa = v_swap<D>(vt) ^ ((m >> 1) & 1u), xb = v_swap<D>(vt + 4) ^ ((m >> 1) & 1u);
+        auto v_operand = [&](int d) -> u32x4 {
+            const u32x2 a = read_transposed(row_a + (((uint32_t)(2 * d) ^ xa) << 4)), b = read_transposed(row_b + (((uint32_t)(2 * d) ^ xb) << 4));
+            return u32x4{a[0], a[1], b[0], b[1]};
+        };
+        // this lane has tokens t0 + 8 quad + 0 .. 7 of its lines
+        auto sees = [&](int rt, int j) -> bool {
+            const int32_t t = t0 + (int32_t)(8 * quad) + j;
+            return t >= see[rt].lo && t < see[rt].hi && ((there >> (8 * quad + j)) & 1u);
+        };
+        u32x4 p[kLineTiles];
+#pragma unroll
+        for (int rt = 0; rt < kLineTiles; ++rt) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = s[rt][j >> 2][j & 3];
+            if (!whole)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = sees(rt, j) ? x[j] : -INFINITY;
+            float big = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            big = max_over32(max_over16(big)) * g.to_log2;
+            if (__any(big > top[rt] + kLag)) {
+                const float now = fmaxf(top[rt], big), f = rescale(top[rt], now);
+                top[rt] = now;
+                sum[rt] = sum[rt] * f * f;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) o[rt][d] = o[rt][d] * f * f;
+            }
+            const float against = E::kWeightShift - (top[rt] == -INFINITY ? 0.f : top[rt]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                x[j] = __builtin_amdgcn_exp2f(fmaf(x[j], g.to_log2, against));
+                sum[rt] += x[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[rt][j] = E::pack2(x[2 * j], x[2 * j + 1]);
+        }
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            const u32x4 vf = v_operand(d);
+#pragma unroll
+            for (int rt = 0; rt < kLineTiles; ++rt) o[rt][d] = E::mfma16(vf, p[rt], o[rt][d]);
+        }
+        there = there_next;
+    }
+
+    if (__any(unfinite)) {
+        for (int32_t tile = (int32_t)wave; tile < tiles; tile += kWaves) {
+            const int32_t t0 = range.lo + tile * kTile;
+            there = place_rows(tile, load_page(tile));
+            if (there == 0xFFFFFFFFu && seen_by_all(t0)) continue;
+            for (int32_t t = 0; t < kTile; ++t) {
+                if (!((there >> t) & 1u)) continue;
+                const RowAt<kBits> at = rows_at[wave][t];
+#pragma unroll
+                for (int rt = 0; rt < kLineTiles; ++rt) {
+                    if (t0 + t < see[rt].lo || t0 + t >= see[rt].hi) continue;
+#pragma unroll
+                    for (int d = 0; d < kDims; ++d) {
+                        float x[4] = {o[rt][d][0], o[rt][d][1], o[rt][d][2], o[rt][d][3]};
+                        add_unfinite<E, D, kBits>(x, g.c.v, at, d * 16 + quad * 4);
+                        o[rt][d] = f32x4{x[0], x[1], x[2], x[3]};
+                    }
+                }
+            }
+        }
+    }
+
+    // The waves' parts are joined over LDS, 16 lines at a time.
+#pragma unroll
+    for (int rt = 0; rt < kLineTiles; ++rt) {
+        sum[rt] = sum_over32(sum_over16(sum[rt]));
+        if (quad == 0) {
+            line_top[wave][rt * 16 + m] = top[rt];
+            line_sum[wave][rt * 16 + m] = sum[rt];
+        }
+    }
+    float* const o_lds = (float*)lds;
+    constexpr uint32_t kRow = D + 4, kSeg = D / 16;
+#pragma unroll
+    for (int rt = 0; rt < kLineTiles; ++rt) {
+        __syncthreads();
+        float now = line_top[0][rt * 16 + m];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) now = fmaxf(now, line_top[w][rt * 16 + m]);
+        const float f = rescale(top[rt], now);
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) *(f32x4*)(o_lds + (wave * 16 + m) * kRow + d * 16 + quad * 4) = o[rt][d] * f * f;
+        __syncthreads();
+        const uint32_t in_tile = threadIdx.x >> 4, seg = threadIdx.x & 15u;
+        const int32_t line = rt * 16 + (int32_t)in_tile;
+        if (line >= lines) continue;
+        float best = line_top[0][line], total = 0.f;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) best = fmaxf(best, line_top[w][line]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float r = rescale(line_top[w][line], best);
+            total += line_sum[w][line] * r * r;
+        }
+        float y[kSeg];
+#pragma unroll
+        for (uint32_t i = 0; i < kSeg; ++i) {
+            y[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) y[i] += o_lds[(w * 16 + in_tile) * kRow + seg * kSeg + i];
+        }
+        const int32_t row = line / (int32_t)g.group, h = line - row * (int32_t)g.group;
+        const uint32_t q_head = head * g.group + (uint32_t)h;
+        const uint64_t out_row = (uint64_t)(q.row0 + row);
+        if (g.part_o) {
+            const uint64_t at = (out_row * g.q_heads + q_head) * g.n_splits + split;
+#pragma unroll
+            for (uint32_t i = 0; i < kSeg / 4; ++i) dev_store(g.part_o + at * D + seg * kSeg + i * 4, f32x4{y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]});
+            if (seg == 0) dev_store(g.part_ml + at * 2, f32x2{best, total});
+        } else {
+            const float scale = total == 0.f ? 0.f : 1.f / total;
+            uint8_t* to = g.out + out_row * g.out_stride + ((uint64_t)q_head * D + seg * kSeg) * 2;
+#pragma unroll
+            for (uint32_t i = 0; i < kSeg / 4; ++i) dev_store(to + i * 8, u32x2{E::pack2(y[4 * i] * scale, y[4 * i + 1] * scale), E::pack2(y[4 * i + 2] * scale, y[4 * i + 3] * scale)});
+            if (g.lse && seg == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(best, total, E::kWeightShift);
+        }
+    }
+}
+
+// ---- many lines ----------------------------------------------------------------------------------
+constexpr int kWideTile = 64;          // tokens of a step
+constexpr int kWideLines = 128;        // 32 a wave
+
+template <class E, int D, int kBits>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const AttendArgs g)
+{
+    constexpr int kK = D / 16, kDims = D / 32;
+    constexpr int kPerRow = kBits == 16 ? D / 8 : D / 32;                // lanes to a row
+    constexpr int kItems = 2 * kWideTile * kPerRow / 256;                // of a thread: K's rows, then V's
+    constexpr uint32_t kPlane = kWideTile * D * 2;
+    __shared__ __align__(16) uint8_t lds[2 * 2 * kPlane];                // [2 buffers][K, V][64 tokens][D]
+    __shared__ RowAt<kBits> rows_at[2][kWideTile];
+    __shared__ uint64_t there_lds[2];
+    __shared__ uint32_t unfinite_lds;                                    // a value was infinite or NaN in a tile that is not whole
+
+    const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t m = lane & 31u, upper = lane >> 5;
+    // Heads vary fastest, so a head stays on an XCD where there are eight, and its tokens in that XCD's cache; the rows that see
+    // the most tokens come first.
+    uint32_t block = blockIdx.x;
+    const uint32_t head = block % g.c.heads;
+    block /= g.c.heads;
+    const uint32_t seq = block % g.b.n_seqs;
+    block /= g.b.n_seqs;
+    const uint32_t split = block % g.n_splits, line_tile = g.line_tiles - 1 - block / g.n_splits;
+    const KvSeq q = kv_sequence(g.b, seq);
+    if (q.bad && threadIdx.x == 0 && split == 0 && head == 0 && line_tile == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
+    const int32_t lines = q.rows * (int32_t)g.group, line0 = (int32_t)line_tile * kWideLines;
+    if (line0 >= lines || split >= splits_of(g, q)) return;
+    const int32_t last_line = line0 + kWideLines < lines ? line0 + kWideLines - 1 : lines - 1;
+    const Range range = token_range(g, q, line0, last_line, split);
+
+    const int32_t line = line0 + (int32_t)(wave * 32 + m);
+    const bool mine = line < lines;
+    const int32_t row = mine ? line / (int32_t)g.group : q.rows - 1, h = mine ? line - row * (int32_t)g.group : 0;
+    const KvSpan see = kv_span(row, q.rows, q.len, g.window, g.all);
+    const uint32_t q_head = head * g.group + (uint32_t)h;
+    // what the wave's first and last lines see
+    const int32_t wave_first = line0 + (int32_t)wave * 32, wave_last = wave_first + 31 < lines ? wave_first + 31 : lines - 1;
+    const bool idle = wave_first >= lines;
+    const KvSpan first = kv_span(idle ? 0 : wave_first / (int32_t)g.group, q.rows, q.len, g.window, g.all);
+    const KvSpan last = kv_span(idle ? 0 : wave_last / (int32_t)g.group, q.rows, q.len, g.window, g.all);
+
+    // tokens that every line of the workgroup sees
+    const int32_t all_lo = kv_span(last_line / (int32_t)g.group, q.rows, q.len, g.window, g.all).lo;
+    const int32_t all_hi = kv_span(line0 / (int32_t)g.group, q.rows, q.len, g.window, g.all).hi;
+
+    u32x4 qf[kK];
+    {
+        const uint8_t* p = g.q + (uint64_t)(q.row0 + row) * g.q_stride + ((uint64_t)q_head * D + upper * 8) * 2;
+#pragma unroll
+        for (int k = 0; k < kK; ++k) qf[k] = dev_load<u32x4>(p + k * 32);
+    }
+    f32x16 o[kDims];
+#pragma unroll
+    for (int d = 0; d < kDims; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float top = -INFINITY, sum = 0.f;
+
+    const int32_t tiles = range.hi > range.lo ? (range.hi - range.lo + kWideTile - 1) / kWideTile : 0;
+    // The first wave looks up where a tile's rows are, a step before they are loaded.
+    auto load_page = [&](int32_t tile) -> uint32_t {
+        const int32_t t = range.lo + tile * kWideTile + (int32_t)lane;
+        return t < range.hi ? (uint32_t)g.b.page_table[(uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift)] : 0u;
+    };
+    auto place_rows = [&](int32_t tile, uint32_t page) {
+        const int32_t t = range.lo + tile * kWideTile + (int32_t)lane;
+        const bool inside = t < range.hi, there = inside && page < g.c.n_pages;
+        rows_at[tile & 1][lane] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
+        if (inside && !there) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
+        const uint64_t all = __ballot(there);
+        if (lane == 0) there_lds[tile & 1] = all;
+    };
+    auto seen_by_all = [&](int32_t t0) -> bool { return t0 >= all_lo && t0 + kWideTile <= all_hi; };
+    if (threadIdx.x == 0) unfinite_lds = 0;                              // before the barriers in front of the first rows
+    u32x4 staged[kItems];
+    uint32_t staged_scale[kItems];
+    auto load_rows = [&](int32_t tile) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const uint32_t item = i * 256 + threadIdx.x, t = item / kPerRow % kWideTile;
+            const RowAt<kBits> at = rows_at[tile & 1][t];
+            const uint8_t* pool = item < (uint32_t)(kWideTile * kPerRow) ? g.c.k : g.c.v;
+            staged[i] = dev_load<u32x4>(pool + at.row + (item % kPerRow) * 16);
+            if constexpr (kBits == 4) staged_scale[i] = dev_load<uint8_t>(pool + at.scale + item % kPerRow);
+        }
+    };
+    auto store_rows = [&](int32_t tile, uint64_t there) {
+        uint8_t* const buffer = lds + (tile & 1) * (2 * kPlane);
+        const bool whole = seen_by_all(range.lo + tile * kWideTile);
+        bool unfinite = false;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const uint32_t item = i * 256 + threadIdx.x, t = item / kPerRow % kWideTile, part = item % kPerRow;
+            const bool is_v = item >= (uint32_t)(kWideTile * kPerRow);
+            uint8_t* const to = buffer + (is_v ? kPlane : 0u) + t * (D * 2);
+            const uint32_t x = is_v ? v_swap<D>(t) : k_swap<D>(t);
+            bool gone = !((there >> t) & 1u);
+            if constexpr (kBits == 16) {
+                u32x4 v = gone ? u32x4{0, 0, 0, 0} : staged[i];
+                if (!whole && is_v) v = finite_only<E>(v, unfinite);
+                *(u32x4*)(to + ((part ^ x) << 4)) = v;
+            } else {
+                if (!whole && is_v && !gone && staged_scale[i] == 255u) gone = unfinite = true;
+                const float scale = scale_of(gone ? 0u : staged_scale[i]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) *(u32x4*)(to + (((part * 4 + c) ^ x) << 4)) = decode8<E>(gone ? 0u : staged[i][c], scale);
+            }
+        }
+        if (unfinite) unfinite_lds = 1;
+    };
+
+    // Two places for addresses and rows: a step reads the next tile's addresses while it works on this tile's rows, then the first
+    // wave writes the addresses of the tile after it and all write the next tile's rows; both places were last read a barrier ago.
+    uint32_t page = 0;
+    uint64_t there = 0;
+    if (tiles > 0) {
+        if (wave == 0) {
+            place_rows(0, load_page(0));
+            page = load_page(1);
+        }
+        __syncthreads();
+        load_rows(0);
+        there = there_lds[0];
+        if (wave == 0) {
+            place_rows(1, page);
+            page = load_page(2);
+        }
+        store_rows(0, there);
+        __syncthreads();
+    }
+    for (int32_t tile = 0; tile < tiles; ++tile) {
+        const int32_t t0 = range.lo + tile * kWideTile;
+        const bool more = tile + 1 < tiles;
+        const uint64_t there_next = there_lds[(tile + 1) & 1];
+        if (more) load_rows(tile + 1);
+        uint8_t* const k_lds = lds + (tile & 1) * (2 * kPlane);
+        uint8_t* const v_lds = k_lds + kPlane;
+        // O^T's first operand: step u takes tokens 16 u + {0, 8} + 4 upper + 0 .. 3
+        const uint32_t i16 = lane & 15u, low = 2 * ((lane >> 4) & 1u) + ((i16 >> 1) & 1u);
+        auto v_operand = [&](int u, int d) -> u32x4 {
+            const uint32_t ta = 16 * u + 4 * upper + (i16 >> 2);
+            const uint8_t *row_a = v_lds + ta * (D * 2) + (i16 & 1u) * 8, *row_b = row_a + 8 * (D * 2);
+            const uint32_t xa = v_swap<D>(ta) ^ low, xb = v_swap<D>(ta + 8) ^ low;
+            const u32x2 a = read_transposed(row_a + (((uint32_t)(4 * d) ^ xa) << 4)), b = read_transposed(row_b + (((uint32_t)(4 * d) ^ xb) << 4));
+            return u32x4{a[0], a[1], b[0], b[1]};
+        };
+        // token of s[a][i]
+        auto sees = [&](int a, int i) -> bool {
+            const int32_t in_tile = a * 32 + 8 * (i >> 2) + 4 * (int32_t)upper + (i & 3), t = t0 + in_tile;
+            return t >= see.lo && t < see.hi && ((there >> in_tile) & 1u);
+        };
+        if (!idle && t0 < last.hi && t0 + kWideTile > first.lo) {
+            f32x16 s[2];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[a][i] = 0.f;
+                const uint32_t t = a * 32 + m, x = k_swap<D>(t);
+                const uint8_t* p = k_lds + t * (D * 2);
+#pragma unroll
+                for (int k = 0; k < kK; ++k) s[a] = E::mfma32(*(const u32x4*)(p + (((uint32_t)(2 * k) + upper) ^ x) * 16), qf[k], s[a]);
+            }
+            if (!(there == ~0ull && t0 >= last.lo && t0 + kWideTile <= first.hi)) {
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[a][i] = sees(a, i) ? s[a][i] : -INFINITY;
+            }
+            float big = s[0][0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) big = fmaxf(big, s[i >> 4][i & 15]);
+            big = max_over32(big) * g.to_log2;
+            if (__any(big > top + kLag)) {
+                const float now = fmaxf(top, big), f = rescale(top, now);
+                top = now;
+                sum = sum * f * f;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) o[d] = o[d] * f * f;
+            }
+            const float against = E::kWeightShift - (top == -INFINITY ? 0.f : top);
+            u32x4 p[4];
+            float add[2] = {0.f, 0.f};
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x0 = __builtin_amdgcn_exp2f(fmaf(s[a][2 * j], g.to_log2, against)), x1 = __builtin_amdgcn_exp2f(fmaf(s[a][2 * j + 1], g.to_log2, against));
+                    add[0] += x0;
+                    add[1] += x1;
+                    p[a * 2 + (j >> 2)][j & 3] = E::pack2(x0, x1);
+                }
+            }
+            sum += add[0] + add[1];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) o[d] = E::mfma32(v_operand(u, d), p[u], o[d]);
+        }
+        if (more) {
+            if (wave == 0 && tile + 2 < tiles) {
+                place_rows(tile + 2, page);
+                page = load_page(tile + 3);
+            }
+            store_rows(tile + 1, there_next);
+        }
+        there = there_next;
+        __syncthreads();
+    }
+
+    if (tiles > 0 && unfinite_lds && !idle) {                            // behind the loop's last barrier
+        for (int32_t t = range.lo; t < range.hi; ++t) {
+            const int32_t t0 = range.lo + (t - range.lo) / kWideTile * kWideTile;
+            if (seen_by_all(t0)) continue;
+            const uint32_t in = (uint32_t)g.b.page_table[(uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift)];
+            if (in >= g.c.n_pages || t < see.lo || t >= see.hi) continue;
+            const RowAt<kBits> at = row_at<D, kBits>(g.c, in, (uint32_t)t, head);
+#pragma unroll
+            for (int d = 0; d < kDims; ++d)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    float x[4] = {o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+                    add_unfinite<E, D, kBits>(x, g.c.v, at, d * 32 + b * 8 + upper * 4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[d][4 * b + i] = x[i];
+                }
+        }
+    }
+    sum = sum_over32(sum);
+    if (!mine) return;
+    const uint64_t out_row = (uint64_t)(q.row0 + row);
+    if (g.part_o) {
+        const uint64_t at = (out_row * g.q_heads + q_head) * g.n_splits + split;
+        if (upper == 0) dev_store(g.part_ml + at * 2, f32x2{top, sum});
+        if (sum == 0.f) return;                                          // join_kernel does not read it
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) dev_store(g.part_o + at * D + d * 32 + b * 8 + upper * 4, f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]});
+    } else {
+        const float scale = sum == 0.f ? 0.f : 1.f / sum;
+        uint8_t* to = g.out + out_row * g.out_stride + ((uint64_t)q_head * D + upper * 4) * 2;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                dev_store(to + (d * 32 + b * 8) * 2, u32x2{E::pack2(o[d][4 * b] * scale, o[d][4 * b + 1] * scale), E::pack2(o[d][4 * b + 2] * scale, o[d][4 * b + 3] * scale)});
+        if (g.lse && upper == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, sum, E::kWeightShift);
+    }
+}
+
+// ---- the splits' parts ---------------------------------------------------------------------------
+// A wave for each row and query head: o = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).
+template <class E, int D>
+__global__ void __launch_bounds__(256) join_kernel(const AttendArgs g)
+{
+    constexpr int kPer = D / 64;                                         // values of a lane
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t seq = blockIdx.y;
+    const KvSeq q = kv_sequence(g.b, seq);
+    const uint64_t x = (uint64_t)blockIdx.x * 4 + wave, row = x / g.q_heads, q_head = x - row * g.q_heads;
+    if (row >= (uint64_t)q.rows) return;
+    const uint64_t out_row = (uint64_t)q.row0 + row, first = (out_row * g.q_heads + q_head) * g.n_splits;
+    const uint32_t n = splits_of(g, q);
+    float top = -INFINITY, sum = 0.f, y[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) y[i] = 0.f;
+    for (uint32_t i = lane; i < n; i += 64) top = fmaxf(top, dev_load<f32x2>(g.part_ml + (first + i) * 2)[0]);
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
+    for (uint32_t i = 0; i < n; ++i) {
+        const f32x2 ml = dev_load<f32x2>(g.part_ml + (first + i) * 2);
+        if (ml[1] == 0.f) continue;
+        const float f = rescale(ml[0], top);
+        sum += ml[1] * f * f;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) y[k] += dev_load<float>(g.part_o + (first + i) * D + lane * kPer + k) * f * f;
+    }
+    const float scale = sum == 0.f ? 0.f : 1.f / sum;
+    uint8_t* to = g.out + out_row * g.out_stride + (q_head * D + lane * kPer) * 2;
+    if constexpr (kPer == 1) dev_store(to, (uint16_t)E::pack2(y[0] * scale, 0.f));
+    else
+#pragma unroll
+        for (int k = 0; k < kPer; k += 2) dev_store(to + k * 2, E::pack2(y[k] * scale, y[k + 1] * scale));
+    if (g.lse && lane == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, sum, E::kWeightShift);
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+struct Shape {
+    uint32_t line_tiles;       // narrow: 16-line tiles of a workgroup (1, 2 or 4); wide: workgroups over the lines
+    bool wide;
+    uint32_t n_splits, split_tokens;
+    uint64_t workspace;
+};
+
+// Which kernel, and how many splits: enough workgroups to fill the 256 compute units several times over, while a split keeps
+// enough tokens for its waves to have a tile in flight beside the one they work on.
+Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_attend_args& a)
+{
+    Shape s{};
+    const uint32_t group = a.q_heads / c.kv_heads;
+    const uint64_t lines = (uint64_t)b.max_rows * group;
+    s.wide = lines > (c.head_dim == 256 ? 32u : 64u);
+    s.line_tiles = s.wide ? (uint32_t)((lines + kWideLines - 1) / kWideLines) : lines <= 16 ? 1 : lines <= 32 ? 2 : 4;
+    uint64_t span = b.max_kv;                                            // most tokens that a sequence's rows see together
+    if (a.window && !(a.flags & TENT_KV_ATTEND_ALL) && (uint64_t)a.window + b.max_rows < span) span = (uint64_t)a.window + b.max_rows;
+    if (a.window && (a.flags & TENT_KV_ATTEND_ALL) && a.window < span) span = a.window;
+    span += kStep;                                                       // the first token is rounded down
+    const uint64_t units = (uint64_t)b.n_seqs * c.kv_heads * (s.wide ? s.line_tiles : 1);
+    const uint64_t wanted = s.wide ? 512 : 1024, least = s.wide ? 512 : 256;
+    uint64_t n = (wanted + units - 1) / units, most = (span + least - 1) / least;
+    n = n > most ? most : n;
+    if (s.wide && units >= 256) n = 1;
+    const uint64_t tokens = ((span + n - 1) / n + 127) / 128 * 128;
+    s.split_tokens = (uint32_t)tokens;
+    s.n_splits = (uint32_t)((span + tokens - 1) / tokens);
+    if (s.n_splits > 1) s.workspace = (uint64_t)b.n_rows * a.q_heads * s.n_splits * (c.head_dim + 2) * 4;
+    return s;
+}
+
+int check(const tent_kv_cache* cache, const tent_kv_batch* batch, const tent_kv_attend_args* args)
+{
+    int rc = kv_check_cache(cache);
+    if (rc == TENT_OK) rc = kv_check_batch(cache, batch);
+    if (rc != TENT_OK) return rc;
+    if (!args || (args->flags & ~(uint32_t)TENT_KV_ATTEND_ALL)) return TENT_ERR_INVALID;
+    if (args->q_heads < 1 || args->q_heads > TENT_KV_MAX_HEADS || args->q_heads % cache->kv_heads) return TENT_ERR_RANGE;
+    if (!(args->scale > 0.f) || args->scale > 3.4e38f || args->window > (1u << 30)) return TENT_ERR_RANGE;
+    return TENT_OK;
+}
+
+uint64_t blocks_of(const Shape& s, const AttendArgs& g)
+{
+    if (s.wide) return (uint64_t)s.line_tiles * s.n_splits * g.b.n_seqs * g.c.heads;
+    return ((uint64_t)g.b.n_seqs * s.n_splits + 7) / 8 * 8 * g.c.heads;
+}
+
+template <class E, int D, int kBits>
+int launch(const Shape& s, const AttendArgs& g, hipStream_t stream)
+{
+    const uint64_t blocks = blocks_of(s, g), join = ((uint64_t)g.b.max_rows * g.q_heads + 3) / 4;
+    if (blocks > 0x7FFFFFFFull || join > 0x7FFFFFFFull) return TENT_ERR_RANGE;
+    const dim3 grid((uint32_t)blocks), threads(256);
+    if (s.wide) {
+        hipLaunchKernelGGL((wide_kernel<E, D, kBits>), grid, threads, 0, stream, g);
+    } else if (s.line_tiles == 1) {
+        hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 1>), grid, threads, 0, stream, g);
+    } else if (s.line_tiles == 2) {
+        hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 2>), grid, threads, 0, stream, g);
+    } else {
+        if constexpr (D != 256) hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 4>), grid, threads, 0, stream, g);
+    }
+    if (hipGetLastError() != hipSuccess) return TENT_ERR_HIP;
+    if (g.part_o) {
+        hipLaunchKernelGGL((join_kernel<E, D>), dim3((uint32_t)join, g.b.n_seqs), threads, 0, stream, g);
+        if (hipGetLastError() != hipSuccess) return TENT_ERR_HIP;
+    }
+    return TENT_OK;
+}
+
+}  // namespace
+}  // namespace tent
+
+using namespace tent;
+
+extern "C" int tent_kv_attend_workspace(const tent_kv_cache* cache, const tent_kv_batch* batch, const tent_kv_attend_args* args,
+                                        uint64_t* bytes)
+{
+    const int rc = check(cache, batch, args);
+    if (rc != TENT_OK) return rc;
+    if (!bytes) return TENT_ERR_INVALID;
+    *bytes = batch->n_seqs == 0 || batch->n_rows == 0 ? 0 : shape_of(*cache, *batch, *args).workspace;
+    return TENT_OK;
+}
+
+extern "C" int tent_kv_attend(const tent_kv_cache* cache, const tent_kv_batch* batch, const tent_kv_attend_args* args, void* stream)
+{
+    int rc = check(cache, batch, args);
+    if (rc != TENT_OK) return rc;
+    if (batch->n_seqs == 0 || batch->n_rows == 0) return TENT_OK;
+    const uint32_t D = cache->head_dim;
+    if ((rc = kv_check_rows(args->q, args->q_stride, args->q_heads, D, batch->n_rows)) != TENT_OK) return rc;
+    if ((rc = kv_check_rows(args->out, args->out_stride, args->q_heads, D, batch->n_rows)) != TENT_OK) return rc;
+    if ((uintptr_t)args->lse & 3u) return TENT_ERR_INVALID;
+    const Shape s = shape_of(*cache, *batch, *args);
+    if (s.workspace && (!args->workspace || !kv_aligned(args->workspace))) return TENT_ERR_INVALID;
+    if (s.workspace > args->workspace_bytes) return TENT_ERR_RANGE;
+    AttendArgs g{};
+    g.c = kv_cache_dev(*cache);
+    g.b = *batch;
+    g.q = static_cast<const uint8_t*>(args->q);
+    g.out = static_cast<uint8_t*>(args->out);
+    g.lse = args->lse;
+    g.q_stride = args->q_stride * 2;
+    g.out_stride = args->out_stride * 2;
+    g.q_heads = args->q_heads;
+    g.group = args->q_heads / cache->kv_heads;
+    g.window = args->window;
+    g.all = args->flags & TENT_KV_ATTEND_ALL ? 1 : 0;
+    g.to_log2 = args->scale * kLog2e;
+    g.n_splits = s.n_splits;
+    g.split_tokens = s.split_tokens;
+    g.line_tiles = s.line_tiles;
+    if (s.workspace) {
+        g.part_o = static_cast<float*>(args->workspace);
+        g.part_ml = g.part_o + (uint64_t)batch->n_rows * args->q_heads * s.n_splits * D;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+#define TENT_ATTEND(dim)                                                                                              \
+    (cache->type == TENT_BF16 ? (cache->bits == 16 ? launch<Bf16, dim, 16>(s, g, st) : launch<Bf16, dim, 4>(s, g, st)) \
+                              : (cache->bits == 16 ? launch<Fp16, dim, 16>(s, g, st) : launch<Fp16, dim, 4>(s, g, st)))
+    return D == 64 ? TENT_ATTEND(64) : D == 128 ? TENT_ATTEND(128) : TENT_ATTEND(256);
+}

@@ -1,0 +1,417 @@
+// Operators that fill, shrink and read the pages of a key/value cache: tent_kv_append, tent_kv_pack, tent_kv_read.
+//
+// All three move each value once and compute little: HBM bounds them, and latency where there are few rows.  A lane
+// works on eight values (16 bytes of a 16-bit row, 4 bytes of codes; four lanes in a row share a block's scale).
+#include "kv_elem.h"
+
+namespace tent {
+namespace {
+
+// Where the rows of a workgroup lie: found by its first lanes, used by all of it.
+constexpr uint32_t kMaxRowTile = 16;
+struct RowPlace {
+    int64_t page;              // byte offset of the page; negative: the row is left out
+    uint32_t slot;             // token in the page
+    uint32_t position;
+    bool live;                 // the row belongs to a sequence that is not left out, at a position >= 0
+};
+
+// The last sequence whose row_start is at most `row`: 64 places at a time, one wave.
+__device__ __forceinline__ uint32_t find_sequence(const tent_kv_batch& b, int32_t row, uint32_t lane)
+{
+    uint32_t lo = 0, n = b.n_seqs;
+    while (n > 1) {
+        const uint32_t step = (n + 63) / 64, at = lane * step;
+        const bool below = at < n && b.row_start[lo + at] <= row;
+        const uint32_t below_n = (uint32_t)__popcll(__ballot(below));   // row_start ascends: a prefix of the lanes
+        if (below_n == 0) return lo;
+        lo += (below_n - 1) * step;
+        n -= (below_n - 1) * step;
+        n = n < step ? n : step;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ void find_rows(RowPlace* to, const KvCache& c, const tent_kv_batch& b, uint32_t row0, uint32_t n)
+{
+    if (threadIdx.x < 64) {
+        uint32_t s = find_sequence(b, (int32_t)row0, threadIdx.x);
+        if (threadIdx.x < n) {
+            const int32_t row = (int32_t)(row0 + threadIdx.x);
+            while (s + 1 < b.n_seqs && b.row_start[s + 1] <= row) ++s;
+            const KvSeq q = kv_sequence(b, s);
+            RowPlace p{-1, 0, 0, false};
+            if (q.bad) kv_note(b.errors, TENT_KV_BAD_SEQUENCE);
+            else if (row >= q.row0 && row < q.row0 + q.rows) {
+                const int32_t position = q.len - q.rows + (row - q.row0);
+                if (position < 0) kv_note(b.errors, TENT_KV_BAD_POSITION);
+                else {
+                    p = RowPlace{kv_page_of(c, b, s, (uint32_t)position), (uint32_t)position & ((1u << c.page_shift) - 1u), (uint32_t)position, true};
+                    if (p.page < 0) kv_note(b.errors, TENT_KV_BAD_PAGE);
+                }
+            }
+            to[threadIdx.x] = p;
+        }
+    }
+    __syncthreads();
+}
+
+// Byte offsets inside a page of the eight values of chunk `chunk` of a head.
+template <int D>
+__device__ __forceinline__ uint32_t at16(uint32_t slot, uint32_t heads, uint32_t head, uint32_t chunk)
+{
+    return ((slot * heads + head) * D + chunk * 8) * 2;
+}
+template <int D>
+__device__ __forceinline__ uint32_t at_codes(uint32_t slot, uint32_t heads, uint32_t head, uint32_t chunk)
+{
+    return (slot * heads + head) * (D / 2) + chunk * 4;
+}
+template <int D>
+__device__ __forceinline__ uint32_t at_scale(uint32_t slot, uint32_t heads, uint32_t head, uint32_t chunk, uint32_t page_shift)
+{
+    return ((heads * (D / 2)) << page_shift) + (slot * heads + head) * (D / 32) + chunk / 4;
+}
+
+// Writes eight values of a row to its page.  Lanes of a block of 32 come here together.
+template <class E, int D, int kBits>
+__device__ __forceinline__ void put8(uint8_t* page, uint32_t page_shift, uint32_t slot, uint32_t heads, uint32_t head, uint32_t chunk, u32x4 v)
+{
+    if constexpr (kBits == 16) {
+        dev_store(page + at16<D>(slot, heads, head, chunk), v);
+    } else {
+        uint32_t byte;
+        const uint32_t codes = encode8<E>(v, byte);
+        dev_store(page + at_codes<D>(slot, heads, head, chunk), codes);
+        if ((chunk & 3u) == 0) dev_store(page + at_scale<D>(slot, heads, head, chunk, page_shift), (uint8_t)byte);
+    }
+}
+
+template <int kWidth, class F>
+__device__ __forceinline__ F sum_lanes(F x)
+{
+#pragma unroll
+    for (int m = 1; m < kWidth; m <<= 1) x += __shfl_xor(x, m, 64);
+    return x;
+}
+
+// A 64-bit value rounded to 32 bits.  The rounding stands by itself: without the barrier the compiler rounds to 16 bits at once,
+// which differs where the 32-bit value is a tie.
+__device__ __forceinline__ float in_32(float x) { return x; }
+__device__ __forceinline__ float in_32(double x)
+{
+    float y = (float)x;
+    __asm__("" : "+v"(y));
+    return y;
+}
+
+struct AppendArgs {
+    tent_kv_append_args a;
+    KvCache c;
+    tent_kv_batch b;
+    uint32_t row_tile;
+};
+
+// Eight values of a head, normalised and turned.  F: float for queries; double for keys, so that a value next to the border of
+// two codes falls on its own side.  `w`, `cs`: this lane's weights and, for its dimensions, cosines and sines.
+template <class E, int D, class F>
+__device__ __forceinline__ u32x4 norm_rotate(const tent_kv_append_args& a, const uint8_t* head, uint32_t chunk, const void* weight,
+                                             const float* cs)
+{
+    constexpr uint32_t kChunks = D / 8;
+    const uint32_t half = a.rope_dim / 16;                               // chunks of one half
+    const bool turned = a.rope && chunk < 2 * half;
+    const bool pairs = a.flags & TENT_KV_ROPE_PAIRS;
+    const uint32_t partner = turned && !pairs ? (chunk < half ? chunk + half : chunk - half) : chunk;
+    const u32x4 raw = dev_load<u32x4>(head + chunk * 16);
+    const u32x4 raw2 = turned && !pairs ? dev_load<u32x4>(head + partner * 16) : raw;
+    if (!weight && !turned) return raw;
+    F x[8], y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = (F)E::to_float(raw[i] & 0xFFFFu);
+        x[2 * i + 1] = (F)E::to_float(raw[i] >> 16);
+        y[2 * i] = (F)E::to_float(raw2[i] & 0xFFFFu);
+        y[2 * i + 1] = (F)E::to_float(raw2[i] >> 16);
+    }
+    if (weight) {
+        F sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
+        sum = sum_lanes<kChunks>(sum);
+        const F r = (F)1 / sqrt(sum * ((F)1 / D) + (F)a.eps);
+        const u32x4 w = dev_load<u32x4>((const uint8_t*)weight + chunk * 16), w2 = dev_load<u32x4>((const uint8_t*)weight + partner * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] *= r * (F)E::to_float(w[i] & 0xFFFFu);
+            x[2 * i + 1] *= r * (F)E::to_float(w[i] >> 16);
+            y[2 * i] *= r * (F)E::to_float(w2[i] & 0xFFFFu);
+            y[2 * i + 1] *= r * (F)E::to_float(w2[i] >> 16);
+        }
+    }
+    if (turned) {
+        if (pairs) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const F c = (F)cs[i], s = (F)cs[4 + i], p = x[2 * i], q = x[2 * i + 1];
+                x[2 * i] = p * c - q * s;
+                x[2 * i + 1] = q * c + p * s;
+            }
+        } else {
+            const F sign = chunk < half ? (F)-1 : (F)1;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = x[i] * (F)cs[i] + sign * y[i] * (F)cs[8 + i];
+        }
+    }
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = E::pack2(in_32(x[2 * i]), in_32(x[2 * i + 1]));
+    return out;
+}
+
+// A workgroup takes `row_tile` rows: their places first, then all heads of a row (queries, keys, values), a chunk of eight a
+// lane.  A lane keeps its chunk number over the heads, as the workgroup is a multiple of a head's lanes, and so its cosines.
+template <class E, int D, int kBits>
+__global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
+{
+    __shared__ RowPlace place[kMaxRowTile];
+    constexpr uint32_t kChunks = D / 8;
+    const tent_kv_append_args& a = g.a;
+    const uint32_t row0 = blockIdx.x * g.row_tile;
+    const uint32_t n = g.b.n_rows - row0 < g.row_tile ? g.b.n_rows - row0 : g.row_tile;
+    find_rows(place, g.c, g.b, row0, n);
+    const uint32_t chunk = threadIdx.x % kChunks, heads = a.q_heads + 2 * g.c.heads;
+    for (uint32_t r = 0; r < n; ++r) {
+        const RowPlace p = place[r];
+        if (!p.live) continue;
+        const uint64_t row = row0 + r;
+        float cs[16];
+        if (a.rope) {
+            const uint32_t at = a.positions ? (uint32_t)a.positions[row] : p.position;
+            if (at >= a.rope_rows) {
+                if (threadIdx.x == 0) kv_note(g.b.errors, TENT_KV_BAD_POSITION);
+                continue;
+            }
+            const uint32_t half = a.rope_dim / 16;
+            if (chunk < 2 * half) {
+                const bool pairs = a.flags & TENT_KV_ROPE_PAIRS;
+                const float* t = a.rope + (uint64_t)at * a.rope_dim + (pairs ? chunk * 4 : (chunk < half ? chunk : chunk - half) * 8);
+                const f32x4 c0 = dev_load<f32x4>(t), s0 = dev_load<f32x4>(t + a.rope_dim / 2);
+                const f32x4 c1 = pairs ? s0 : dev_load<f32x4>(t + 4), s1 = pairs ? s0 : dev_load<f32x4>(t + a.rope_dim / 2 + 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    cs[i] = c0[i];
+                    cs[4 + i] = c1[i];
+                    cs[8 + i] = s0[i];
+                    cs[12 + i] = s1[i];
+                }
+            }
+        }
+        for (uint32_t h = threadIdx.x / kChunks; h < heads; h += blockDim.x / kChunks) {
+            if (h < a.q_heads) {
+                const u32x4 y = norm_rotate<E, D, float>(a, (const uint8_t*)a.q + (row * a.q_stride + (uint64_t)h * D) * 2, chunk, a.q_weight, cs);
+                dev_store((uint8_t*)a.q_out + (row * a.q_out_stride + (uint64_t)h * D + chunk * 8) * 2, y);
+            } else if (p.page >= 0) {
+                uint32_t kh = h - a.q_heads;
+                if (kh < g.c.heads) {
+                    const u32x4 y = norm_rotate<E, D, double>(a, (const uint8_t*)a.k + (row * a.k_stride + (uint64_t)kh * D) * 2, chunk, a.k_weight, cs);
+                    put8<E, D, kBits>(g.c.k + p.page, g.c.page_shift, p.slot, g.c.heads, kh, chunk, y);
+                } else {
+                    kh -= g.c.heads;
+                    const u32x4 y = dev_load<u32x4>((const uint8_t*)a.v + (row * a.v_stride + (uint64_t)kh * D + chunk * 8) * 2);
+                    put8<E, D, kBits>(g.c.v + p.page, g.c.page_shift, p.slot, g.c.heads, kh, chunk, y);
+                }
+            }
+        }
+    }
+}
+
+struct ReadArgs {
+    KvCache c;
+    tent_kv_batch b;
+    uint8_t *k, *v;
+    uint64_t stride;           // bytes
+    uint32_t row_tile;
+};
+
+template <class E, int D, int kBits>
+__global__ void __launch_bounds__(256) read_kernel(const ReadArgs g)
+{
+    __shared__ RowPlace place[kMaxRowTile];
+    constexpr uint32_t kChunks = D / 8;
+    const uint32_t row0 = blockIdx.x * g.row_tile;
+    const uint32_t n = g.b.n_rows - row0 < g.row_tile ? g.b.n_rows - row0 : g.row_tile;
+    find_rows(place, g.c, g.b, row0, n);
+    const uint32_t one = g.c.heads * kChunks;                            // chunks of K of a row
+    for (uint32_t i = threadIdx.x; i < n * 2 * one; i += blockDim.x) {
+        const uint32_t r = i / (2 * one), x = i - r * 2 * one;
+        const bool is_v = x >= one;
+        const uint32_t y = is_v ? x - one : x, head = y / kChunks, chunk = y % kChunks;
+        const RowPlace p = place[r];
+        if (!p.live) continue;
+        u32x4 value = {0, 0, 0, 0};
+        if (p.page >= 0) {
+            const uint8_t* page = (is_v ? g.c.v : g.c.k) + p.page;
+            if constexpr (kBits == 16) {
+                value = dev_load<u32x4>(page + at16<D>(p.slot, g.c.heads, head, chunk));
+            } else {
+                const uint32_t codes = dev_load<uint32_t>(page + at_codes<D>(p.slot, g.c.heads, head, chunk));
+                const uint32_t byte = dev_load<uint8_t>(page + at_scale<D>(p.slot, g.c.heads, head, chunk, g.c.page_shift));
+                value = decode8<E>(codes, scale_of(byte));
+            }
+        }
+        dev_stream((is_v ? g.v : g.k) + (row0 + r) * g.stride + (uint64_t)y * 16, value);
+    }
+}
+
+struct PackArgs {
+    KvCache src, dst;
+    const int32_t *src_pages, *dst_pages;
+    int32_t* errors;
+    uint32_t n_pages, parts;   // workgroups for one page of one pool
+};
+
+// A workgroup takes kPackChunks chunks a lane of one page of K or V.
+constexpr uint32_t kPackChunks = 4;
+template <class E, int D>
+__global__ void __launch_bounds__(256) pack_kernel(const PackArgs g)
+{
+    constexpr uint32_t kChunks = D / 8;
+    const uint32_t part = blockIdx.x % g.parts, at = blockIdx.x / g.parts;
+    const bool is_v = at >= g.n_pages;
+    const uint32_t i = is_v ? at - g.n_pages : at;
+    const uint32_t from = (uint32_t)g.src_pages[i], to = (uint32_t)g.dst_pages[i];
+    if (from >= g.src.n_pages || to >= g.dst.n_pages) {
+        if (threadIdx.x == 0) kv_note(g.errors, TENT_KV_BAD_PAGE);
+        return;
+    }
+    const uint8_t* src = (is_v ? g.src.v : g.src.k) + from * g.src.page_stride;
+    uint8_t* dst = (is_v ? g.dst.v : g.dst.k) + to * g.dst.page_stride;
+    const uint32_t n = (g.src.heads * kChunks) << g.src.page_shift;      // a multiple of the 8 lanes that share two blocks
+    const uint32_t scales = ((g.src.heads * (D / 2)) << g.src.page_shift);
+    const uint32_t first = part * blockDim.x * kPackChunks + threadIdx.x;
+    u32x4 v[kPackChunks];
+#pragma unroll
+    for (uint32_t k = 0; k < kPackChunks; ++k) {
+        const uint32_t x = first + k * blockDim.x;
+        if (x < n) v[k] = dev_load<u32x4>(src + (uint64_t)x * 16);
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kPackChunks; ++k) {
+        const uint32_t x = first + k * blockDim.x;
+        if (x >= n) continue;
+        uint32_t byte;
+        const uint32_t codes = encode8<E>(v[k], byte);
+        dev_store(dst + (uint64_t)x * 4, codes);
+        if ((x & 3u) == 0) dev_store(dst + scales + x / 4, (uint8_t)byte);
+    }
+}
+
+// Rows of a workgroup: as many as leave about four workgroups for each of the 256 compute units.
+uint32_t row_tile(uint32_t n_rows)
+{
+    const uint32_t n = n_rows / 1024;
+    return n < 1 ? 1 : n > kMaxRowTile ? kMaxRowTile : n;
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? TENT_OK : TENT_ERR_HIP; }
+
+template <class E, int D, int kBits>
+int launch_append(const AppendArgs& g, hipStream_t s)
+{
+    const uint32_t lanes = (g.a.q_heads + 2 * g.c.heads) * (D / 8);
+    const uint32_t threads = lanes >= 256 ? 256 : (lanes + 63) / 64 * 64;
+    hipLaunchKernelGGL((append_kernel<E, D, kBits>), dim3((g.b.n_rows + g.row_tile - 1) / g.row_tile), dim3(threads), 0, s, g);
+    return launched();
+}
+template <class E, int D, int kBits>
+int launch_read(const ReadArgs& g, hipStream_t s)
+{
+    hipLaunchKernelGGL((read_kernel<E, D, kBits>), dim3((g.b.n_rows + g.row_tile - 1) / g.row_tile), dim3(256), 0, s, g);
+    return launched();
+}
+template <class E, int D>
+int launch_pack(PackArgs g, hipStream_t s)
+{
+    const uint32_t n = (g.src.heads * (D / 8)) << g.src.page_shift;
+    g.parts = (n + 256 * kPackChunks - 1) / (256 * kPackChunks);
+    const uint64_t blocks = (uint64_t)2 * g.n_pages * g.parts;
+    if (blocks > 0x7FFFFFFFull) return TENT_ERR_RANGE;
+    hipLaunchKernelGGL((pack_kernel<E, D>), dim3((uint32_t)blocks), dim3(256), 0, s, g);
+    return launched();
+}
+
+}  // namespace
+}  // namespace tent
+
+using namespace tent;
+
+#define TENT_KV_DIM(dim, call) ((dim) == 64 ? call(64) : (dim) == 128 ? call(128) : call(256))
+
+extern "C" uint64_t tent_kv_packed_page(uint32_t page_tokens, uint32_t kv_heads, uint32_t head_dim)
+{
+    if (!kv_sizes_ok(page_tokens, kv_heads, head_dim)) return 0;
+    return (kv_page_bytes(page_tokens, kv_heads, head_dim, 4) + 15) / 16 * 16;
+}
+
+extern "C" int tent_kv_append(const tent_kv_cache* cache, const tent_kv_batch* batch, const tent_kv_append_args* args, void* stream)
+{
+    int rc = kv_check_cache(cache);
+    if (rc == TENT_OK) rc = kv_check_batch(cache, batch);
+    if (rc != TENT_OK) return rc;
+    if (!args || args->reserved || (args->flags & ~(uint32_t)TENT_KV_ROPE_PAIRS)) return TENT_ERR_INVALID;
+    if (batch->n_seqs == 0 || batch->n_rows == 0) return TENT_OK;
+    const uint32_t D = cache->head_dim, n = batch->n_rows;
+    if ((rc = kv_check_rows(args->k, args->k_stride, cache->kv_heads, D, n)) != TENT_OK) return rc;
+    if ((rc = kv_check_rows(args->v, args->v_stride, cache->kv_heads, D, n)) != TENT_OK) return rc;
+    if (args->q_heads > TENT_KV_MAX_HEADS) return TENT_ERR_RANGE;
+    if (args->q_heads) {
+        if ((rc = kv_check_rows(args->q, args->q_stride, args->q_heads, D, n)) != TENT_OK) return rc;
+        if ((rc = kv_check_rows(args->q_out, args->q_out_stride, args->q_heads, D, n)) != TENT_OK) return rc;
+        if (args->q == args->q_out && args->q_stride != args->q_out_stride) return TENT_ERR_INVALID;
+    }
+    if (!kv_aligned(args->q_weight) || !kv_aligned(args->k_weight) || !kv_aligned(args->rope)) return TENT_ERR_INVALID;
+    if (!(args->eps >= 0.f) || args->eps > 3.4e38f) return TENT_ERR_RANGE;
+    if (args->rope && (args->rope_rows < 1 || args->rope_dim < 16 || args->rope_dim > D || args->rope_dim % 16)) return TENT_ERR_RANGE;
+    if ((uintptr_t)args->positions & 3u) return TENT_ERR_INVALID;
+    const AppendArgs g{*args, kv_cache_dev(*cache), *batch, row_tile(n)};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+#define TENT_APPEND(dim)                                                                                   \
+    (cache->type == TENT_BF16 ? (cache->bits == 16 ? launch_append<Bf16, dim, 16>(g, s) : launch_append<Bf16, dim, 4>(g, s)) \
+                              : (cache->bits == 16 ? launch_append<Fp16, dim, 16>(g, s) : launch_append<Fp16, dim, 4>(g, s)))
+    return TENT_KV_DIM(D, TENT_APPEND);
+}
+
+extern "C" int tent_kv_read(const tent_kv_cache* cache, const tent_kv_batch* batch, void* k_out, void* v_out, uint64_t out_stride,
+                            void* stream)
+{
+    int rc = kv_check_cache(cache);
+    if (rc == TENT_OK) rc = kv_check_batch(cache, batch);
+    if (rc != TENT_OK) return rc;
+    if (batch->n_seqs == 0 || batch->n_rows == 0) return TENT_OK;
+    if ((rc = kv_check_rows(k_out, out_stride, cache->kv_heads, cache->head_dim, batch->n_rows)) != TENT_OK) return rc;
+    if ((rc = kv_check_rows(v_out, out_stride, cache->kv_heads, cache->head_dim, batch->n_rows)) != TENT_OK) return rc;
+    const ReadArgs g{kv_cache_dev(*cache), *batch, static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out), out_stride * 2, row_tile(batch->n_rows)};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+#define TENT_READ(dim)                                                                                     \
+    (cache->type == TENT_BF16 ? (cache->bits == 16 ? launch_read<Bf16, dim, 16>(g, s) : launch_read<Bf16, dim, 4>(g, s)) \
+                              : (cache->bits == 16 ? launch_read<Fp16, dim, 16>(g, s) : launch_read<Fp16, dim, 4>(g, s)))
+    return TENT_KV_DIM(cache->head_dim, TENT_READ);
+}
+
+extern "C" int tent_kv_pack(const tent_kv_cache* src, const tent_kv_cache* dst, const int32_t* src_pages, const int32_t* dst_pages,
+                            uint32_t n_pages, int32_t* errors, void* stream)
+{
+    int rc = kv_check_cache(src);
+    if (rc == TENT_OK) rc = kv_check_cache(dst);
+    if (rc != TENT_OK) return rc;
+    if (src->bits != 16 || dst->bits != 4) return TENT_ERR_INVALID;
+    if (src->page_tokens != dst->page_tokens || src->kv_heads != dst->kv_heads || src->head_dim != dst->head_dim || src->type != dst->type) return TENT_ERR_RANGE;
+    if (n_pages == 0) return TENT_OK;
+    if (!src_pages || !dst_pages || (((uintptr_t)src_pages | (uintptr_t)dst_pages | (uintptr_t)errors) & 3u)) return TENT_ERR_INVALID;
+    if (n_pages > 0x7FFFFFFFu) return TENT_ERR_RANGE;
+    const PackArgs g{kv_cache_dev(*src), kv_cache_dev(*dst), src_pages, dst_pages, errors, n_pages, 0};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+#define TENT_PACK(dim) (src->type == TENT_BF16 ? launch_pack<Bf16, dim>(g, s) : launch_pack<Fp16, dim>(g, s))
+    return TENT_KV_DIM(src->head_dim, TENT_PACK);
+}
