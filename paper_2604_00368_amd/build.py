@@ -17,6 +17,9 @@ HIPCC_FLAGS = [
     # "'-packed-fp32-ops' is not a recognized feature for this target (ignoring feature)" per file, which
     # is harmless.
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+    # Sums of matrix products stay in vector registers: kernels that rescale them between products would copy them out of the
+    # accumulation registers and back in every step.
+    "-mllvm", "-amdgpu-mfma-vgpr-form=1",
 ]
 
 

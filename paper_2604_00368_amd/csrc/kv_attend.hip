@@ -101,18 +101,23 @@ __device__ __forceinline__ float sum_over16(float x) { return x + __shfl_xor(x, 
 // 0.  Sums are multiplied by it twice: the power itself may be below the least normal number where the product is not.
 __device__ __forceinline__ float rescale(float a, float b) { return a == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(0.5f * (a - b)); }
 
-// Sixteen-byte chunks of a token's row change places in LDS by the token, so that the rows' writes, the reads of K's rows by
-// 16 or 32 lanes and the transposing reads of V (four tokens by 16 or 32 dimensions) each spread over all banks.
+// Where a token's row has its 16-byte chunk `chunk` in LDS (as a chunk number): eight chunks cover all banks once, and eight
+// lanes of a 16-byte access, or 32 of a transposing one, go at a time.  Blocks of 32 dimensions (chunk / 4) and, by the token,
+// the chunks' lowest three bits are mixed so that each of these is spread evenly: rows written by lanes side by side (four
+// chunks apart from 4-bit pages, one apart from 16-bit ones), K read by lanes of one token each, V's transposing reads of four
+// tokens by 16 or 32 dimensions.
 template <int D>
-__device__ __forceinline__ uint32_t v_swap(uint32_t t)
+__device__ __forceinline__ constexpr uint32_t spread(uint32_t chunk)
 {
-    return D == 64 ? ((t >> 1) & 1u) << 2 | ((t >> 2) & 3u) : (t & 3u) << 2 | ((t >> 2) & 3u);
+    return D == 64 ? chunk : (chunk & 16u) | (chunk & 2u) << 2 | (chunk >> 1 & 6u) | (chunk & 1u);
 }
 template <int D>
-__device__ __forceinline__ uint32_t k_swap(uint32_t t)
+__device__ __forceinline__ constexpr uint32_t gather(uint32_t place)     // the inverse
 {
-    return D == 64 ? (t >> 1) & 7u : t & 15u;
+    return D == 64 ? place : (place & 16u) | (place & 6u) << 1 | (place >> 2 & 2u) | (place & 1u);
 }
+__device__ __forceinline__ uint32_t k_swap(uint32_t t) { return t & 7u; }
+__device__ __forceinline__ uint32_t v_swap(uint32_t t) { return (t & 1u) * 5u | (t & 2u); }
 
 // The lanes of 16 give the addresses of four values each, rows of 16 in the order of the lanes; lane i gets value i of each row.
 __device__ __forceinline__ u32x2 read_transposed(const uint8_t* p)
@@ -166,19 +171,39 @@ __device__ __forceinline__ float lse_of(float top, float sum, float shift)
 constexpr int kWaves = 4;
 constexpr int kTile = 32;              // tokens of a wave's step
 
-// One tile of a wave in registers.  K: lane (m = lane % 16, quad = lane / 16) has, for half 0 and 1, the token
-// 8 (m / 4) + 4 half + m % 4 and its dimensions (D / 4) quad ..: after the product, quad holds tokens 8 quad .. 8 quad + 7.
-// V: a token's row in lanes side by side, 16 bytes each.
+// Scale bytes as the aligned word that holds them, and how far up they are in it.  A byte's load would be extended to a register
+// where it is loaded, behind a wait for it; this is taken apart where it is used.
+struct ScaleWord { uint32_t word, shift; };
+__device__ __forceinline__ ScaleWord load_scale(const uint8_t* p)
+{
+    const uintptr_t at = (uintptr_t)p;
+    return ScaleWord{dev_load<uint32_t>((const void*)(at & ~(uintptr_t)3)), (uint32_t)(at & 3u) * 8u};
+}
+__device__ __forceinline__ uint32_t byte_of(const ScaleWord& s, uint32_t i = 0) { return s.word >> (s.shift + 8 * i) & 0xFFu; }
+
+// One tile of a wave in registers, as it is loaded: a token's row in lanes side by side, 16 bytes each.
 template <int D, int kBits>
 struct Tile {
-    static constexpr int kPerRow = kBits == 16 ? D / 8 : D / 32;         // lanes to a row of V
+    static constexpr int kPerRow = kBits == 16 ? D / 8 : D / 32;         // lanes to a row
     static constexpr int kPasses = kTile * kPerRow / 64;
-    static constexpr int kWords = kBits == 16 ? D / 8 : D / 32;          // registers of a lane's part of a row of K
-    uint32_t k[2][kWords];
-    uint32_t k_scale[2];
-    u32x4 v[kPasses];
-    uint32_t v_scale[kPasses];
+    static constexpr int kTokens = 64 / kPerRow;                         // tokens of a pass
+    static constexpr int kWords = D == 256 ? 2 : 1;                      // words that hold a row's scale bytes
+    u32x4 k[kPasses], v[kPasses];
+    uint32_t scale[kWords];                                              // of token lane % 32, K in the lower half of the lanes, V in the upper
+    uint32_t shift;                                                      // where its bytes begin in the word: two of them need not at the first
 };
+
+// What the first product reads of K.  Lane (m = lane % 16, quad = lane / 16) takes token 8 (m / 4) + 4 half + m % 4 for half 0 and
+// 1: after the product, quad holds tokens 8 quad .. 8 quad + 7.
+__device__ __forceinline__ uint32_t k_token(uint32_t m, uint32_t half) { return 8 * (m >> 2) + 4 * half + (m & 3u); }
+// Eight lanes side by side, each of a token of its own, are to read from all banks: rows of 16 bits as in `spread`, rows of codes
+// are D / 32 chunks long.
+template <int D, int kBits>
+__device__ __forceinline__ uint32_t k_place(uint32_t t, uint32_t chunk)
+{
+    if constexpr (kBits == 16) return t * (D * 2) + ((spread<D>(chunk) ^ ((t & 3u) | (t >> 1 & 4u))) << 4);
+    else return t * (D / 2) + ((chunk ^ (D == 64 ? t >> 3 & 1u : D == 128 ? (t >> 1 & 1u) | (t >> 2 & 2u) : (t & 3u) | (t >> 1 & 4u))) << 4);
+}
 
 template <class E, int D, int kBits, int kLineTiles>
 __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
@@ -193,11 +218,13 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
 
     const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t m = lane & 15u, quad = lane >> 4;
-    // All heads of a (sequence, split) go to one XCD one after the other: the heads of a token share lines of its page.
+    // All heads of a (sequence, split) go to one XCD one after the other: the heads of a token share lines of its page.  The later
+    // splits, which short sequences do not have, come last, and each of them begins with another sequence: otherwise the XCDs that
+    // get them, or get the long sequences, would have more or less to do than the others.
     const uint32_t eight = blockIdx.x / (8 * g.c.heads), in_eight = blockIdx.x - eight * 8 * g.c.heads;
     const uint32_t unit = eight * 8 + in_eight % 8, head = in_eight / 8;
     if (unit >= g.b.n_seqs * g.n_splits) return;
-    const uint32_t seq = unit / g.n_splits, split = unit - seq * g.n_splits;
+    const uint32_t split = unit / g.b.n_seqs, seq = (unit + split) % g.b.n_seqs;
     const KvSeq q = kv_sequence(g.b, seq);
     if (q.bad && threadIdx.x == 0 && split == 0 && head == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
     if (q.rows == 0 || split >= splits_of(g, q)) return;
@@ -212,9 +239,10 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
         const int32_t line = rt * 16 + (int32_t)m;
         const int32_t row = line < lines ? line / (int32_t)g.group : 0, h = line < lines ? line - row * (int32_t)g.group : 0;
         see[rt] = kv_span(row, q.rows, q.len, g.window, g.all);
-        const uint8_t* p = g.q + (uint64_t)(q.row0 + row) * g.q_stride + ((uint64_t)(head * g.group + h) * D + quad * (D / 4)) * 2;
+        // dims in the order of K's operand: a lane has every fourth eight of a 16-bit row, and D / 4 in a row of codes
+        const uint8_t* p = g.q + (uint64_t)(q.row0 + row) * g.q_stride + ((uint64_t)(head * g.group + h) * D + quad * (kBits == 16 ? 8 : D / 4)) * 2;
 #pragma unroll
-        for (int k = 0; k < kK; ++k) qf[rt][k] = dev_load<u32x4>(p + k * 16);
+        for (int k = 0; k < kK; ++k) qf[rt][k] = dev_load<u32x4>(p + k * (kBits == 16 ? 64 : 16));
     }
     // tokens that every line sees
     const int32_t all_lo = kv_span(q.rows - 1, q.rows, q.len, g.window, g.all).lo, all_hi = kv_span(0, q.rows, q.len, g.window, g.all).hi;
@@ -233,112 +261,138 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
 
     // Waves take tiles in turn.  Page numbers are loaded two of a wave's tiles ahead, rows one ahead.
     const int32_t tiles = (range.hi - range.lo + kTile - 1) / kTile;
+    // Nothing of that stands behind a condition in the loop: the compiler then knows how many loads are behind the one that it
+    // waits for, and does not wait for them.  Past the last tile they go to a row that is there.
+    bool bad_page = false;
     auto load_page = [&](int32_t tile) -> uint32_t {
-        const int32_t t = range.lo + tile * kTile + (int32_t)(lane & 31u);
-        return t < range.hi ? (uint32_t)g.b.page_table[(uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift)] : 0u;
+        const int32_t t = min(range.lo + tile * kTile + (int32_t)(lane & 31u), range.hi - 1);
+        return dev_load<uint32_t>(g.b.page_table + (uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift));
     };
-    // Puts the places of a tile's rows into LDS and says which of its tokens are there; the others get the place of a row that is.
+    // Puts the places of a tile's rows into LDS and says which of its tokens are there.
     auto place_rows = [&](int32_t tile, uint32_t page) -> uint32_t {
         const int32_t t = range.lo + tile * kTile + (int32_t)(lane & 31u);
         const bool inside = t < range.hi, there = inside && page < g.c.n_pages;
-        if (lane < 32) {
-            rows_at[wave][lane] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
-            if (inside && !there) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
-        }
+        bad_page |= inside && !there;
+        if (lane < 32) rows_at[wave][lane] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
         same_wave_order();
         return (uint32_t)__ballot(there);
     };
-    T tile_now;
-    auto load_k = [&]() {
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            const RowAt<kBits> at = rows_at[wave][8 * (m >> 2) + 4 * a + (m & 3)];
-            const uint8_t* p = g.c.k + at.row + quad * (T::kWords * 4);
-            if constexpr (T::kWords == 2) {
-                const u32x2 w = dev_load<u32x2>(p);
-                tile_now.k[a][0] = w[0];
-                tile_now.k[a][1] = w[1];
-            } else {
-#pragma unroll
-                for (int i = 0; i < T::kWords / 4; ++i) {
-                    const u32x4 w = dev_load<u32x4>(p + i * 16);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) tile_now.k[a][i * 4 + j] = w[j];
-                }
-            }
-            if constexpr (kBits == 4) {
-                const uint8_t* sp = g.c.k + at.scale + quad * (D / 4) / 32;
-                tile_now.k_scale[a] = D == 256 ? dev_load<uint16_t>(sp) : dev_load<uint8_t>(sp);
-            }
-        }
-    };
-    auto load_v = [&]() {
+    T now;
+    auto load_rows = [&](u32x4* to, const uint8_t* pool) {
 #pragma unroll
         for (int i = 0; i < T::kPasses; ++i) {
-            const RowAt<kBits> at = rows_at[wave][i * (64 / T::kPerRow) + lane / T::kPerRow];
-            tile_now.v[i] = dev_load<u32x4>(g.c.v + at.row + (lane % T::kPerRow) * 16);
-            if constexpr (kBits == 4) tile_now.v_scale[i] = dev_load<uint8_t>(g.c.v + at.scale + lane % T::kPerRow);
+            const uint32_t part = lane % T::kPerRow;
+            to[i] = dev_load<u32x4>(pool + rows_at[wave][i * T::kTokens + lane / T::kPerRow].row + (kBits == 16 ? gather<D>(part) : part) * 16);
         }
     };
+    auto load_scales = [&]() {
+        if constexpr (kBits == 4) {
+            // whole words: a byte's load would be extended to a register where it is loaded, behind a wait for it
+            const uintptr_t at = (uintptr_t)(lane < 32 ? g.c.k : g.c.v) + rows_at[wave][lane & 31u].scale;
+            if constexpr (T::kWords == 2) {
+                const u32x2 w = dev_load<u32x2>((const void*)at);
+                now.scale[0] = w[0];
+                now.scale[1] = w[1];
+                now.shift = 0;
+            } else {
+                now.scale[0] = dev_load<uint32_t>((const void*)(at & ~(uintptr_t)3));
+                now.shift = (uint32_t)(at & 3u) * 8;
+            }
+        }
+    };
+    // Scale byte `block` of token t of K (of V for t from 32 on), from the lane that has loaded it.
+    auto scale_at = [&](uint32_t t, uint32_t block) -> uint32_t {
+        uint32_t w = (uint32_t)__builtin_amdgcn_ds_bpermute((int)(t * 4), (int)(now.scale[0] >> now.shift));
+        if constexpr (T::kWords == 2) {
+            const uint32_t upper = (uint32_t)__builtin_amdgcn_ds_bpermute((int)(t * 4), (int)now.scale[1]);
+            w = block >= 4 ? upper : w;
+        }
+        return w >> (8 * (block & 3u)) & 0xFFu;
+    };
+    // K's rows and V's take the same place one after the other.
     uint8_t* const v_lds = lds + wave * (kTile * D * 2);
+    uint8_t* const k_lds = v_lds;
     uint32_t there = 0, next_page = 0;
     bool unfinite = false;                                               // this lane met a value that is infinite or NaN in a tile that is not whole
-    if ((int32_t)wave < tiles) {
+    if (tiles > 0) {
         there = place_rows((int32_t)wave, load_page((int32_t)wave));
-        load_k();
-        load_v();
-        next_page = load_page((int32_t)wave + kWaves);
+        next_page = load_page((int32_t)wave + kWaves);                   // in front of the rows, as in the loop
+        load_rows(now.k, g.c.k);
+        load_scales();
+        load_rows(now.v, g.c.v);
     }
     for (int32_t tile = (int32_t)wave; tile < tiles; tile += kWaves) {
         const int32_t t0 = range.lo + tile * kTile;
-        const bool more = tile + kWaves < tiles;
-        uint32_t there_next = 0;
         same_wave_order();
-        if (more) {
-            there_next = place_rows(tile + kWaves, next_page);
-            next_page = load_page(tile + 2 * kWaves);
-        }
+        const uint32_t there_next = place_rows(tile + kWaves, next_page);
+        next_page = load_page(tile + 2 * kWaves);
         // S^T
+#pragma unroll
+        for (int i = 0; i < T::kPasses; ++i) {
+            const uint32_t t = i * T::kTokens + lane / T::kPerRow, part = lane % T::kPerRow;
+            *(u32x4*)(k_lds + k_place<D, kBits>(t, kBits == 16 ? gather<D>(part) : part)) = now.k[i];
+        }
+        load_rows(now.k, g.c.k);
+        __builtin_amdgcn_sched_barrier(0);                               // the next rows are on their way before anything waits for V's
+        same_wave_order();
         f32x4 s[kLineTiles][2];
 #pragma unroll
         for (int rt = 0; rt < kLineTiles; ++rt) s[rt][0] = s[rt][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
+            const uint32_t t = k_token(m, a);
+            u32x4 kf[kK];
+            if constexpr (kBits == 16) {
 #pragma unroll
-            for (int k = 0; k < kK; ++k) {
-                u32x4 kf;
-                if constexpr (kBits == 16) kf = u32x4{tile_now.k[a][k * 4], tile_now.k[a][k * 4 + 1], tile_now.k[a][k * 4 + 2], tile_now.k[a][k * 4 + 3]};
-                else kf = decode8<E>(tile_now.k[a][k], scale_of(tile_now.k_scale[a] >> (8 * (k / 4)) & 0xFFu));
+                for (int k = 0; k < kK; ++k) kf[k] = *(const u32x4*)(k_lds + k_place<D, 16>(t, 4 * k + quad));
+            } else if constexpr (D == 64) {
+                const u32x2 c = *(const u32x2*)(k_lds + k_place<D, 4>(t, quad >> 1) + (quad & 1u) * 8);
+                const float scale = scale_of(scale_at(t, quad >> 1));
+                kf[0] = decode8<E>(c[0], scale);
+                kf[1] = decode8<E>(c[1], scale);
+            } else {
 #pragma unroll
-                for (int rt = 0; rt < kLineTiles; ++rt) s[rt][a] = E::mfma16(kf, qf[rt][k], s[rt][a]);
+                for (int b = 0; b < D / 128; ++b) {
+                    const u32x4 c = *(const u32x4*)(k_lds + k_place<D, 4>(t, quad * (D / 128) + b));
+                    const float scale = scale_of(scale_at(t, quad * (D / 128) + b));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) kf[b * 4 + k] = decode8<E>(c[k], scale);
+                }
             }
+#pragma unroll
+            for (int k = 0; k < kK; ++k)
+#pragma unroll
+                for (int rt = 0; rt < kLineTiles; ++rt) s[rt][a] = E::mfma16(kf[k], qf[rt][k], s[rt][a]);
         }
-        if (more) load_k();
+        same_wave_order();
         // V's rows to LDS, tokens that are not there as zeros
         const bool whole = there == 0xFFFFFFFFu && seen_by_all(t0);
 #pragma unroll
         for (int i = 0; i < T::kPasses; ++i) {
-            const uint32_t t = i * (64 / T::kPerRow) + lane / T::kPerRow, part = lane % T::kPerRow, x = v_swap<D>(t);
+            const uint32_t t = i * T::kTokens + lane / T::kPerRow, part = lane % T::kPerRow, x = v_swap(t);
             bool gone = !whole && !((there >> t) & 1u);
             if constexpr (kBits == 16) {
-                u32x4 v = tile_now.v[i];
+                u32x4 v = now.v[i];
                 if (!whole) v = gone ? u32x4{0, 0, 0, 0} : finite_only<E>(v, unfinite);
                 *(u32x4*)(v_lds + t * (D * 2) + ((part ^ x) << 4)) = v;
             } else {
-                if (!whole && !gone && tile_now.v_scale[i] == 255u) gone = unfinite = true;
-                const float scale = scale_of(gone ? 0u : tile_now.v_scale[i]);
+                const uint32_t byte = scale_at(32 + t, part);
+                if (!whole && !gone && byte == 255u) gone = unfinite = true;
+                const float scale = scale_of(gone ? 0u : byte);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) *(u32x4*)(v_lds + t * (D * 2) + (((part * 4 + c) ^ x) << 4)) = decode8<E>(gone ? 0u : tile_now.v[i][c], scale);
+                for (int c = 0; c < 4; ++c) *(u32x4*)(v_lds + t * (D * 2) + ((spread<D>(part * 4 + c) ^ x) << 4)) = decode8<E>(gone ? 0u : now.v[i][c], scale);
             }
         }
+        load_scales();
+        load_rows(now.v, g.c.v);
+        __builtin_amdgcn_sched_barrier(0);
         same_wave_order();
-        if (more) load_v();
         // O^T's first operand: tokens 8 quad .. 8 quad + 7 of 16 dimensions
         const uint32_t vt = 8 * quad + (m >> 2);
         const uint8_t *row_a = v_lds + vt * (D * 2) + (m & 1u) * 8, *row_b = row_a + 4 * (D * 2);
-        const uint32_t xa = v_swap<D>(vt) ^ ((m >> 1) & 1u), xb = v_swap<D>(vt + 4) ^ ((m >> 1) & 1u);
+        const uint32_t x = v_swap(vt) ^ ((m >> 1) & 1u);                  // the same four tokens on
         auto v_operand = [&](int d) -> u32x4 {
-            const u32x2 a = read_transposed(row_a + (((uint32_t)(2 * d) ^ xa) << 4)), b = read_transposed(row_b + (((uint32_t)(2 * d) ^ xb) << 4));
+            const u32x2 a = read_transposed(row_a + ((spread<D>(2 * d) ^ x) << 4)), b = read_transposed(row_b + ((spread<D>(2 * d) ^ x) << 4));
             return u32x4{a[0], a[1], b[0], b[1]};
         };
         // this lane has tokens t0 + 8 quad + 0 .. 7 of its lines
@@ -382,11 +436,14 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
         there = there_next;
     }
 
+    if (bad_page) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
     if (__any(unfinite)) {
+#pragma unroll 1
         for (int32_t tile = (int32_t)wave; tile < tiles; tile += kWaves) {
             const int32_t t0 = range.lo + tile * kTile;
             there = place_rows(tile, load_page(tile));
             if (there == 0xFFFFFFFFu && seen_by_all(t0)) continue;
+#pragma unroll 1
             for (int32_t t = 0; t < kTile; ++t) {
                 if (!((there >> t) & 1u)) continue;
                 const RowAt<kBits> at = rows_at[wave][t];
@@ -523,31 +580,33 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
     float top = -INFINITY, sum = 0.f;
 
     const int32_t tiles = range.hi > range.lo ? (range.hi - range.lo + kWideTile - 1) / kWideTile : 0;
+    bool bad_page = false;
     // The first wave looks up where a tile's rows are, a step before they are loaded.
     auto load_page = [&](int32_t tile) -> uint32_t {
-        const int32_t t = range.lo + tile * kWideTile + (int32_t)lane;
-        return t < range.hi ? (uint32_t)g.b.page_table[(uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift)] : 0u;
+        const int32_t t = min(range.lo + tile * kWideTile + (int32_t)lane, range.hi - 1);
+        return dev_load<uint32_t>(g.b.page_table + (uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift));
     };
     auto place_rows = [&](int32_t tile, uint32_t page) {
         const int32_t t = range.lo + tile * kWideTile + (int32_t)lane;
         const bool inside = t < range.hi, there = inside && page < g.c.n_pages;
         rows_at[tile & 1][lane] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
-        if (inside && !there) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
+        bad_page |= inside && !there;
         const uint64_t all = __ballot(there);
         if (lane == 0) there_lds[tile & 1] = all;
     };
     auto seen_by_all = [&](int32_t t0) -> bool { return t0 >= all_lo && t0 + kWideTile <= all_hi; };
     if (threadIdx.x == 0) unfinite_lds = 0;                              // before the barriers in front of the first rows
     u32x4 staged[kItems];
-    uint32_t staged_scale[kItems];
+    ScaleWord staged_scale[kItems];
     auto load_rows = [&](int32_t tile) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
             const uint32_t item = i * 256 + threadIdx.x, t = item / kPerRow % kWideTile;
             const RowAt<kBits> at = rows_at[tile & 1][t];
             const uint8_t* pool = item < (uint32_t)(kWideTile * kPerRow) ? g.c.k : g.c.v;
-            staged[i] = dev_load<u32x4>(pool + at.row + (item % kPerRow) * 16);
-            if constexpr (kBits == 4) staged_scale[i] = dev_load<uint8_t>(pool + at.scale + item % kPerRow);
+            const uint32_t part = item % kPerRow;
+            staged[i] = dev_load<u32x4>(pool + at.row + (kBits == 16 ? gather<D>(part) : part) * 16);
+            if constexpr (kBits == 4) staged_scale[i] = load_scale(pool + at.scale + part);
         }
     };
     auto store_rows = [&](int32_t tile, uint64_t there) {
@@ -559,17 +618,18 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             const uint32_t item = i * 256 + threadIdx.x, t = item / kPerRow % kWideTile, part = item % kPerRow;
             const bool is_v = item >= (uint32_t)(kWideTile * kPerRow);
             uint8_t* const to = buffer + (is_v ? kPlane : 0u) + t * (D * 2);
-            const uint32_t x = is_v ? v_swap<D>(t) : k_swap<D>(t);
+            const uint32_t x = is_v ? v_swap(t) : k_swap(t);
             bool gone = !((there >> t) & 1u);
             if constexpr (kBits == 16) {
                 u32x4 v = gone ? u32x4{0, 0, 0, 0} : staged[i];
                 if (!whole && is_v) v = finite_only<E>(v, unfinite);
                 *(u32x4*)(to + ((part ^ x) << 4)) = v;
             } else {
-                if (!whole && is_v && !gone && staged_scale[i] == 255u) gone = unfinite = true;
-                const float scale = scale_of(gone ? 0u : staged_scale[i]);
+                const uint32_t byte = byte_of(staged_scale[i]);
+                if (!whole && is_v && !gone && byte == 255u) gone = unfinite = true;
+                const float scale = scale_of(gone ? 0u : byte);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) *(u32x4*)(to + (((part * 4 + c) ^ x) << 4)) = decode8<E>(gone ? 0u : staged[i][c], scale);
+                for (int c = 0; c < 4; ++c) *(u32x4*)(to + ((spread<D>(part * 4 + c) ^ x) << 4)) = decode8<E>(gone ? 0u : staged[i][c], scale);
             }
         }
         if (unfinite) unfinite_lds = 1;
@@ -606,8 +666,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         auto v_operand = [&](int u, int d) -> u32x4 {
             const uint32_t ta = 16 * u + 4 * upper + (i16 >> 2);
             const uint8_t *row_a = v_lds + ta * (D * 2) + (i16 & 1u) * 8, *row_b = row_a + 8 * (D * 2);
-            const uint32_t xa = v_swap<D>(ta) ^ low, xb = v_swap<D>(ta + 8) ^ low;
-            const u32x2 a = read_transposed(row_a + (((uint32_t)(4 * d) ^ xa) << 4)), b = read_transposed(row_b + (((uint32_t)(4 * d) ^ xb) << 4));
+            const uint32_t at = (spread<D>(4 * d) ^ spread<D>(low) ^ v_swap(ta)) << 4;      // the same eight tokens on
+            const u32x2 a = read_transposed(row_a + at), b = read_transposed(row_b + at);
             return u32x4{a[0], a[1], b[0], b[1]};
         };
         // token of s[a][i]
@@ -621,10 +681,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             for (int a = 0; a < 2; ++a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[a][i] = 0.f;
-                const uint32_t t = a * 32 + m, x = k_swap<D>(t);
+                const uint32_t t = a * 32 + m, x = spread<D>(upper) ^ k_swap(t);
                 const uint8_t* p = k_lds + t * (D * 2);
 #pragma unroll
-                for (int k = 0; k < kK; ++k) s[a] = E::mfma32(*(const u32x4*)(p + (((uint32_t)(2 * k) + upper) ^ x) * 16), qf[k], s[a]);
+                for (int k = 0; k < kK; ++k) s[a] = E::mfma32(*(const u32x4*)(p + ((spread<D>(2 * k) ^ x) << 4)), qf[k], s[a]);
             }
             if (!(there == ~0ull && t0 >= last.lo && t0 + kWideTile <= first.hi)) {
 #pragma unroll
@@ -673,7 +733,9 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         __syncthreads();
     }
 
+    if (bad_page) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
     if (tiles > 0 && unfinite_lds && !idle) {                            // behind the loop's last barrier
+#pragma unroll 1
         for (int32_t t = range.lo; t < range.hi; ++t) {
             const int32_t t0 = range.lo + (t - range.lo) / kWideTile * kWideTile;
             if (seen_by_all(t0)) continue;
@@ -715,39 +777,58 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
 }
 
 // ---- the splits' parts ---------------------------------------------------------------------------
-// A wave for each row and query head: o = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).
+// A workgroup for each row and query head, its waves take parts in turn: o = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).
 template <class E, int D>
 __global__ void __launch_bounds__(256) join_kernel(const AttendArgs g)
 {
-    constexpr int kPer = D / 64;                                         // values of a lane
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t seq = blockIdx.y;
-    const KvSeq q = kv_sequence(g.b, seq);
-    const uint64_t x = (uint64_t)blockIdx.x * 4 + wave, row = x / g.q_heads, q_head = x - row * g.q_heads;
-    if (row >= (uint64_t)q.rows) return;
+    constexpr int kPer = D / 64, kAhead = 4;                             // values of a lane; parts that a wave has in flight
+    __shared__ float o_lds[kWaves][D], sum_lds[kWaves];
+    const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t row = blockIdx.x / g.q_heads, q_head = blockIdx.x - row * g.q_heads;
+    const KvSeq q = kv_sequence(g.b, blockIdx.y);
+    if ((int32_t)row >= q.rows) return;
     const uint64_t out_row = (uint64_t)q.row0 + row, first = (out_row * g.q_heads + q_head) * g.n_splits;
     const uint32_t n = splits_of(g, q);
     float top = -INFINITY, sum = 0.f, y[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) y[i] = 0.f;
+    for (int k = 0; k < kPer; ++k) y[k] = 0.f;
     for (uint32_t i = lane; i < n; i += 64) top = fmaxf(top, dev_load<f32x2>(g.part_ml + (first + i) * 2)[0]);
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
-    for (uint32_t i = 0; i < n; ++i) {
-        const f32x2 ml = dev_load<f32x2>(g.part_ml + (first + i) * 2);
-        if (ml[1] == 0.f) continue;
-        const float f = rescale(ml[0], top);
-        sum += ml[1] * f * f;
+    for (uint32_t i = wave; i < n; i += kWaves * kAhead) {
+        f32x2 ml[kAhead];
+        float part[kAhead][kPer];
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) y[k] += dev_load<float>(g.part_o + (first + i) * D + lane * kPer + k) * f * f;
+        for (int a = 0; a < kAhead; ++a) {
+            const uint64_t at = first + min(i + a * kWaves, n - 1);
+            ml[a] = dev_load<f32x2>(g.part_ml + at * 2);
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) part[a][k] = dev_load<float>(g.part_o + at * D + lane * kPer + k);
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            if (i + a * kWaves >= n || ml[a][1] == 0.f) continue;        // an empty part has a sum of 0 and no output
+            const float f = rescale(ml[a][0], top);
+            sum += ml[a][1] * f * f;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) y[k] += part[a][k] * f * f;
+        }
     }
-    const float scale = sum == 0.f ? 0.f : 1.f / sum;
-    uint8_t* to = g.out + out_row * g.out_stride + (q_head * D + lane * kPer) * 2;
-    if constexpr (kPer == 1) dev_store(to, (uint16_t)E::pack2(y[0] * scale, 0.f));
-    else
 #pragma unroll
-        for (int k = 0; k < kPer; k += 2) dev_store(to + k * 2, E::pack2(y[k] * scale, y[k + 1] * scale));
-    if (g.lse && lane == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, sum, E::kWeightShift);
+    for (int k = 0; k < kPer; ++k) o_lds[wave][lane * kPer + k] = y[k];
+    if (lane == 0) sum_lds[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x >= D / 2) return;                                    // two values a thread
+    float total = 0.f, a = 0.f, b = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        total += sum_lds[w];
+        a += o_lds[w][threadIdx.x * 2];
+        b += o_lds[w][threadIdx.x * 2 + 1];
+    }
+    const float scale = total == 0.f ? 0.f : 1.f / total;
+    dev_store(g.out + out_row * g.out_stride + ((uint64_t)q_head * D + threadIdx.x * 2) * 2, E::pack2(a * scale, b * scale));
+    if (g.lse && threadIdx.x == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, total, E::kWeightShift);
 }
 
 // ---- host ----------------------------------------------------------------------------------------
@@ -772,7 +853,7 @@ Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_att
     if (a.window && (a.flags & TENT_KV_ATTEND_ALL) && a.window < span) span = a.window;
     span += kStep;                                                       // the first token is rounded down
     const uint64_t units = (uint64_t)b.n_seqs * c.kv_heads * (s.wide ? s.line_tiles : 1);
-    const uint64_t wanted = s.wide ? 512 : 1024, least = s.wide ? 512 : 256;
+    const uint64_t wanted = s.wide ? 512 : 1536, least = s.wide ? 512 : 256;
     uint64_t n = (wanted + units - 1) / units, most = (span + least - 1) / least;
     n = n > most ? most : n;
     if (s.wide && units >= 256) n = 1;
@@ -803,7 +884,7 @@ uint64_t blocks_of(const Shape& s, const AttendArgs& g)
 template <class E, int D, int kBits>
 int launch(const Shape& s, const AttendArgs& g, hipStream_t stream)
 {
-    const uint64_t blocks = blocks_of(s, g), join = ((uint64_t)g.b.max_rows * g.q_heads + 3) / 4;
+    const uint64_t blocks = blocks_of(s, g), join = (uint64_t)g.b.max_rows * g.q_heads;
     if (blocks > 0x7FFFFFFFull || join > 0x7FFFFFFFull) return TENT_ERR_RANGE;
     const dim3 grid((uint32_t)blocks), threads(256);
     if (s.wide) {
