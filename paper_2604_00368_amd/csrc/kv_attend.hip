@@ -94,6 +94,11 @@ __device__ __forceinline__ float max_over16(float x)
     const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
     return fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1]));
 }
+// A value that all lanes of a wave have, for branches that the wave takes as a whole.
+__device__ __forceinline__ uint64_t same_in_wave(uint64_t x)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
 __device__ __forceinline__ float sum_over32(float x) { return x + __shfl_xor(x, 32, 64); }
 __device__ __forceinline__ float sum_over16(float x) { return x + __shfl_xor(x, 16, 64); }
 
@@ -143,6 +148,10 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 v, bool& other)
     }
     return v;
 }
+
+// Waits for loaded values.  Without it the wait stands in front of their first use, in a loop, where it is a wait for the loop's own
+// loads from the second time on.
+__device__ __forceinline__ void arrived(u32x4& v) { __asm__ volatile("" : "+v"(v)); }
 
 // Adds the values that are not finite among four of a row of V that a line sees: dims `dim` .. `dim` + 3.
 template <class E, int D, int kBits>
@@ -571,6 +580,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         const uint8_t* p = g.q + (uint64_t)(q.row0 + row) * g.q_stride + ((uint64_t)q_head * D + upper * 8) * 2;
 #pragma unroll
         for (int k = 0; k < kK; ++k) qf[k] = dev_load<u32x4>(p + k * 32);
+#pragma unroll
+        for (int k = 0; k < kK; ++k) arrived(qf[k]);
     }
     f32x16 o[kDims];
 #pragma unroll
@@ -609,30 +620,45 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             if constexpr (kBits == 4) staged_scale[i] = load_scale(pool + at.scale + part);
         }
     };
+    // K's rows go as they are: scores of tokens that a line does not see are replaced.  V's do where every line sees the whole tile.
     auto store_rows = [&](int32_t tile, uint64_t there) {
         uint8_t* const buffer = lds + (tile & 1) * (2 * kPlane);
-        const bool whole = seen_by_all(range.lo + tile * kWideTile);
-        bool unfinite = false;
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
+        auto put = [&](int i, auto clean) {
             const uint32_t item = i * 256 + threadIdx.x, t = item / kPerRow % kWideTile, part = item % kPerRow;
-            const bool is_v = item >= (uint32_t)(kWideTile * kPerRow);
+            const bool is_v = kItems == 1 ? item >= 128u : i >= kItems / 2;
             uint8_t* const to = buffer + (is_v ? kPlane : 0u) + t * (D * 2);
             const uint32_t x = is_v ? v_swap(t) : k_swap(t);
-            bool gone = !((there >> t) & 1u);
+            u32x4 v = staged[i];
             if constexpr (kBits == 16) {
-                u32x4 v = gone ? u32x4{0, 0, 0, 0} : staged[i];
-                if (!whole && is_v) v = finite_only<E>(v, unfinite);
+                if (is_v) clean(v, t);
                 *(u32x4*)(to + ((part ^ x) << 4)) = v;
             } else {
-                const uint32_t byte = byte_of(staged_scale[i]);
-                if (!whole && is_v && !gone && byte == 255u) gone = unfinite = true;
-                const float scale = scale_of(gone ? 0u : byte);
+                uint32_t byte = byte_of(staged_scale[i]);
+                if (is_v) clean(v, byte, t);
+                const float scale = scale_of(byte);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) *(u32x4*)(to + ((spread<D>(part * 4 + c) ^ x) << 4)) = decode8<E>(gone ? 0u : staged[i][c], scale);
+                for (int c = 0; c < 4; ++c) *(u32x4*)(to + ((spread<D>(part * 4 + c) ^ x) << 4)) = decode8<E>(v[c], scale);
             }
+        };
+        if (there == ~0ull && seen_by_all(range.lo + tile * kWideTile)) {
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) put(i, [](auto&&...) {});
+        } else {
+            bool unfinite = false;
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+                if constexpr (kBits == 16) {
+                    put(i, [&](u32x4& v, uint32_t t) { v = (there >> t) & 1u ? finite_only<E>(v, unfinite) : u32x4{0, 0, 0, 0}; });
+                } else {
+                    put(i, [&](u32x4& v, uint32_t& byte, uint32_t t) {
+                        bool gone = !((there >> t) & 1u);
+                        if (!gone && byte == 255u) gone = unfinite = true;
+                        if (gone) { v = u32x4{0, 0, 0, 0}; byte = 0; }
+                    });
+                }
+            }
+            if (unfinite) unfinite_lds = 1;
         }
-        if (unfinite) unfinite_lds = 1;
     };
 
     // Two places for addresses and rows: a step reads the next tile's addresses while it works on this tile's rows, then the first
@@ -646,7 +672,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         }
         __syncthreads();
         load_rows(0);
-        there = there_lds[0];
+        there = same_in_wave(there_lds[0]);
         if (wave == 0) {
             place_rows(1, page);
             page = load_page(2);
@@ -657,7 +683,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
     for (int32_t tile = 0; tile < tiles; ++tile) {
         const int32_t t0 = range.lo + tile * kWideTile;
         const bool more = tile + 1 < tiles;
-        const uint64_t there_next = there_lds[(tile + 1) & 1];
+        const uint64_t there_next = same_in_wave(there_lds[(tile + 1) & 1]);
         if (more) load_rows(tile + 1);
         uint8_t* const k_lds = lds + (tile & 1) * (2 * kPlane);
         uint8_t* const v_lds = k_lds + kPlane;
@@ -670,27 +696,30 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             const u32x2 a = read_transposed(row_a + at), b = read_transposed(row_b + at);
             return u32x4{a[0], a[1], b[0], b[1]};
         };
-        // token of s[a][i]
-        auto sees = [&](int a, int i) -> bool {
-            const int32_t in_tile = a * 32 + 8 * (i >> 2) + 4 * (int32_t)upper + (i & 3), t = t0 + in_tile;
-            return t >= see.lo && t < see.hi && ((there >> in_tile) & 1u);
-        };
         if (!idle && t0 < last.hi && t0 + kWideTile > first.lo) {
             f32x16 s[2];
 #pragma unroll
-            for (int a = 0; a < 2; ++a) {
+            for (int a = 0; a < 2; ++a)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[a][i] = 0.f;
-                const uint32_t t = a * 32 + m, x = spread<D>(upper) ^ k_swap(t);
-                const uint8_t* p = k_lds + t * (D * 2);
+            const uint32_t x = spread<D>(upper) ^ k_swap(m);             // the same 32 tokens on
+            const uint8_t* p0 = k_lds + m * (D * 2);
 #pragma unroll
-                for (int k = 0; k < kK; ++k) s[a] = E::mfma32(*(const u32x4*)(p + ((spread<D>(2 * k) ^ x) << 4)), qf[k], s[a]);
-            }
+            for (int k = 0; k < kK; ++k)
+#pragma unroll
+                for (int a = 0; a < 2; ++a) s[a] = E::mfma32(*(const u32x4*)(p0 + a * (32 * D * 2) + ((spread<D>(2 * k) ^ x) << 4)), qf[k], s[a]);
             if (!(there == ~0ull && t0 >= last.lo && t0 + kWideTile <= first.hi)) {
+                // the tile's tokens that this line sees; s[a][i] is token 32 a + 8 (i / 4) + 4 upper + i % 4
+                uint64_t seen = there;
+                if (see.hi < t0 + kWideTile) seen = see.hi > t0 ? seen & ~(~0ull << (see.hi - t0)) : 0;
+                if (see.lo > t0) seen = see.lo < t0 + kWideTile ? seen & ~0ull << (see.lo - t0) : 0;
+                seen >>= 4 * upper;
 #pragma unroll
-                for (int a = 0; a < 2; ++a)
+                for (int a = 0; a < 2; ++a) {
+                    const uint32_t half = (uint32_t)(seen >> (32 * a));
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[a][i] = sees(a, i) ? s[a][i] : -INFINITY;
+                    for (int i = 0; i < 16; ++i) s[a][i] = half & (1u << (8 * (i >> 2) + (i & 3))) ? s[a][i] : -INFINITY;
+                }
             }
             float big = s[0][0];
 #pragma unroll
