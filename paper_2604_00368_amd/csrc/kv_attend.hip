@@ -149,6 +149,13 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 v, bool& other)
     return v;
 }
 
+// 16 bytes a lane from device memory to LDS, where lane i's go to `to` + 16 i; `to` is the same in the wave.
+__device__ __forceinline__ void load_to_lds(const uint8_t* from, uint8_t* to)
+{
+    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+__device__ __forceinline__ void loads_to_lds_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }      // vmcnt(0)
+
 // Waits for loaded values.  Without it the wait stands in front of their first use, in a loop, where it is a wait for the loop's own
 // loads from the second time on.
 __device__ __forceinline__ void arrived(u32x4& v) { __asm__ volatile("" : "+v"(v)); }
@@ -538,9 +545,11 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
     constexpr int kPerRow = kBits == 16 ? D / 8 : D / 32;                // lanes to a row
     constexpr int kItems = 2 * kWideTile * kPerRow / 256;                // of a thread: K's rows, then V's
     constexpr uint32_t kPlane = kWideTile * D * 2;
-    __shared__ __align__(16) uint8_t lds[2 * 2 * kPlane];                // [2 buffers][K, V][64 tokens][D]
-    __shared__ RowAt<kBits> rows_at[2][kWideTile];
-    __shared__ uint64_t there_lds[2];
+    // Two places for a tile of K and two for one of V, [64 tokens][D] each.  They are variables of their own, and which of them a step
+    // loads to is known when it is compiled: a read of LDS would otherwise wait for every load to LDS that is on its way.
+    __shared__ __align__(16) uint8_t k_even[kPlane], k_odd[kPlane], v_even[kPlane], v_odd[kPlane];
+    __shared__ RowAt<kBits> rows_at[4][kWideTile];
+    __shared__ uint64_t there_lds[4];
     __shared__ uint32_t unfinite_lds;                                    // a value was infinite or NaN in a tile that is not whole
 
     const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -592,7 +601,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
 
     const int32_t tiles = range.hi > range.lo ? (range.hi - range.lo + kWideTile - 1) / kWideTile : 0;
     bool bad_page = false;
-    // The first wave looks up where a tile's rows are, a step before they are loaded.
+    // The first wave looks up where a tile's rows are, a step before they are loaded.  Past the last tile they are where some page is.
     auto load_page = [&](int32_t tile) -> uint32_t {
         const int32_t t = min(range.lo + tile * kWideTile + (int32_t)lane, range.hi - 1);
         return dev_load<uint32_t>(g.b.page_table + (uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift));
@@ -600,117 +609,134 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
     auto place_rows = [&](int32_t tile, uint32_t page) {
         const int32_t t = range.lo + tile * kWideTile + (int32_t)lane;
         const bool inside = t < range.hi, there = inside && page < g.c.n_pages;
-        rows_at[tile & 1][lane] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
+        rows_at[tile & 3][lane] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
         bad_page |= inside && !there;
         const uint64_t all = __ballot(there);
-        if (lane == 0) there_lds[tile & 1] = all;
+        if (lane == 0) there_lds[tile & 3] = all;
     };
     auto seen_by_all = [&](int32_t t0) -> bool { return t0 >= all_lo && t0 + kWideTile <= all_hi; };
     if (threadIdx.x == 0) unfinite_lds = 0;                              // before the barriers in front of the first rows
-    u32x4 staged[kItems];
-    ScaleWord staged_scale[kItems];
-    auto load_rows = [&](int32_t tile) {
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const uint32_t item = i * 256 + threadIdx.x, t = item / kPerRow % kWideTile;
-            const RowAt<kBits> at = rows_at[tile & 1][t];
-            const uint8_t* pool = item < (uint32_t)(kWideTile * kPerRow) ? g.c.k : g.c.v;
-            const uint32_t part = item % kPerRow;
-            staged[i] = dev_load<u32x4>(pool + at.row + (kBits == 16 ? gather<D>(part) : part) * 16);
-            if constexpr (kBits == 4) staged_scale[i] = load_scale(pool + at.scale + part);
-        }
-    };
-    // K's rows go as they are: scores of tokens that a line does not see are replaced.  V's do where every line sees the whole tile.
-    auto store_rows = [&](int32_t tile, uint64_t there) {
-        uint8_t* const buffer = lds + (tile & 1) * (2 * kPlane);
-        auto put = [&](int i, auto clean) {
-            const uint32_t item = i * 256 + threadIdx.x, t = item / kPerRow % kWideTile, part = item % kPerRow;
-            const bool is_v = kItems == 1 ? item >= 128u : i >= kItems / 2;
-            uint8_t* const to = buffer + (is_v ? kPlane : 0u) + t * (D * 2);
-            const uint32_t x = is_v ? v_swap(t) : k_swap(t);
-            u32x4 v = staged[i];
+    // 16 bits: rows go straight to LDS, a wave's 64 chunks in the order of its lanes, so a lane picks the chunk that belongs in its
+    // place.  4 bits: by way of registers, where they are decoded.
+    u32x4 staged[kBits == 4 ? kItems : 1];
+    ScaleWord staged_scale[kBits == 4 ? kItems : 1];
+    // K's rows of one tile and V's of another, where there are such.
+    auto load_rows = [&](int32_t k_tile, uint8_t* k_to, int32_t v_tile, uint8_t* v_to) {
+        constexpr uint32_t kRows = 256 / kPerRow;                        // of an item; eight at least, so a lane's place in its row stays
+        const uint32_t part = threadIdx.x % kPerRow, t_in = threadIdx.x / kPerRow % kWideTile;
+        auto load = [&](int i) {
+            const bool is_v = kItems == 1 ? threadIdx.x >= 128u : i >= kItems / 2;
+            const RowAt<kBits> at = rows_at[(is_v ? v_tile : k_tile) & 3][t_in + i * kRows % kWideTile];
+            const uint8_t* pool = is_v ? g.c.v : g.c.k;
             if constexpr (kBits == 16) {
-                if (is_v) clean(v, t);
-                *(u32x4*)(to + ((part ^ x) << 4)) = v;
+                static_assert(kRows % 8 == 0, "places in a row repeat every eight rows");
+                const uint32_t chunk = gather<D>(part ^ (is_v ? v_swap(t_in) : k_swap(t_in)));
+                load_to_lds(pool + chunk * 16 + at.row, (is_v ? v_to : k_to) + (uint32_t)i % (kItems / 2) * 4096u + wave * 1024u);
             } else {
-                uint32_t byte = byte_of(staged_scale[i]);
-                if (is_v) clean(v, byte, t);
-                const float scale = scale_of(byte);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) *(u32x4*)(to + ((spread<D>(part * 4 + c) ^ x) << 4)) = decode8<E>(v[c], scale);
+                staged[i] = dev_load<u32x4>(pool + at.row + part * 16);
+                staged_scale[i] = load_scale(pool + at.scale + part);
             }
         };
-        if (there == ~0ull && seen_by_all(range.lo + tile * kWideTile)) {
-#pragma unroll
-            for (int i = 0; i < kItems; ++i) put(i, [](auto&&...) {});
+        if constexpr (kItems == 1) {
+            load(0);
         } else {
-            bool unfinite = false;
+            if (k_tile < tiles)
 #pragma unroll
-            for (int i = 0; i < kItems; ++i) {
-                if constexpr (kBits == 16) {
-                    put(i, [&](u32x4& v, uint32_t t) { v = (there >> t) & 1u ? finite_only<E>(v, unfinite) : u32x4{0, 0, 0, 0}; });
-                } else {
-                    put(i, [&](u32x4& v, uint32_t& byte, uint32_t t) {
-                        bool gone = !((there >> t) & 1u);
-                        if (!gone && byte == 255u) gone = unfinite = true;
-                        if (gone) { v = u32x4{0, 0, 0, 0}; byte = 0; }
-                    });
+                for (int i = 0; i < kItems / 2; ++i) load(i);
+            if (v_tile < tiles)
+#pragma unroll
+                for (int i = kItems / 2; i < kItems; ++i) load(i);
+        }
+    };
+    // What was loaded is in LDS when the barrier behind this is passed.  K's rows go as they are: scores of tokens that a line does
+    // not see are replaced.  V's do where every line sees the whole tile.
+    auto store_rows = [&](int32_t k_tile, uint8_t* k_to, int32_t v_tile, uint8_t* v_to, uint64_t there) {
+        const bool whole = there == ~0ull && seen_by_all(range.lo + v_tile * kWideTile);
+        bool unfinite = false;
+        if constexpr (kBits == 16) {
+            loads_to_lds_done();
+            if (!whole && v_tile < tiles) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kItems / 2; ++i) {
+                    const uint32_t t = (i * 256 + threadIdx.x) / kPerRow;
+                    u32x4* const v = (u32x4*)(v_to + (i * 256 + threadIdx.x) * 16);
+                    *v = (there >> t) & 1u ? finite_only<E>(*v, unfinite) : u32x4{0, 0, 0, 0};
                 }
             }
-            if (unfinite) unfinite_lds = 1;
+        } else {
+            uint32_t thread = threadIdx.x;
+            __asm__ volatile("" : "+v"(thread));                         // places are computed in every step, not kept in registers
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+                const uint32_t item = i * 256 + thread, t = item / kPerRow % kWideTile, part = item % kPerRow;
+                const bool is_v = item >= (uint32_t)(kWideTile * kPerRow);
+                const int32_t tile = is_v ? v_tile : k_tile;
+                if (tile >= tiles) continue;
+                uint8_t* const to = (is_v ? v_to : k_to) + t * (D * 2);
+                const uint32_t x = is_v ? v_swap(t) : k_swap(t);
+                uint32_t byte = byte_of(staged_scale[i]);
+                bool gone = false;
+                if (!whole && is_v) {
+                    gone = !((there >> t) & 1u);
+                    if (!gone && byte == 255u) gone = unfinite = true;
+                    byte = gone ? 0u : byte;
+                }
+                const float scale = scale_of(byte);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) *(u32x4*)(to + ((spread<D>(part * 4 + c) ^ x) << 4)) = decode8<E>(gone ? 0u : staged[i][c], scale);
+            }
         }
+        if (unfinite) unfinite_lds = 1;
     };
 
-    // Two places for addresses and rows: a step reads the next tile's addresses while it works on this tile's rows, then the first
-    // wave writes the addresses of the tile after it and all write the next tile's rows; both places were last read a barrier ago.
+    // S^T of a tile, in s[a][i] the score of token 32 a + 8 (i / 4) + 4 upper + i % 4.  Operands are read two steps ahead; `beside(k)`
+    // is done beside step k, and nothing is moved from step to step.
+    auto scores = [&](const uint8_t* from, f32x16 (&s)[2], auto beside) {
+        const uint32_t x = spread<D>(upper) ^ k_swap(m);                 // the same 32 tokens on
+        const uint8_t* p = from + m * (D * 2);
+        u32x4 kf[kK][2];
+        auto read = [&](int k) {
+#pragma unroll
+            for (int a = 0; a < 2; ++a) kf[k][a] = *(const u32x4*)(p + a * (32 * D * 2) + ((spread<D>(2 * k) ^ x) << 4));
+        };
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[a][i] = 0.f;
+        read(0);
+        read(1);
+#pragma unroll
+        for (int k = 0; k < kK; ++k) {
+            if (k + 2 < kK) read(k + 2);
+#pragma unroll
+            for (int a = 0; a < 2; ++a) s[a] = E::mfma32(kf[k][a], qf[k], s[a]);
+            beside(k);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto largest = [&](const f32x16 (&s)[2]) -> float {
+        float big = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) big = fmaxf(big, s[i >> 4][i & 15]);
+        return big;
+    };
+
+    // A step multiplies a tile's weights by its values, and beside their exponentials the next tile's keys by the queries.  Meanwhile
+    // the keys of the tile behind that and the values of the next are loaded, to the places that the step before has read, and the
+    // first wave writes where the tile after them is.
     uint32_t page = 0;
     uint64_t there = 0;
-    if (tiles > 0) {
-        if (wave == 0) {
-            place_rows(0, load_page(0));
-            page = load_page(1);
-        }
-        __syncthreads();
-        load_rows(0);
-        there = same_in_wave(there_lds[0]);
-        if (wave == 0) {
-            place_rows(1, page);
-            page = load_page(2);
-        }
-        store_rows(0, there);
-        __syncthreads();
-    }
-    for (int32_t tile = 0; tile < tiles; ++tile) {
+    float big_of = 0.f;                                                  // largest of a step's scores, of this lane's
+    // `k_from` has the next tile's keys, `v_from` this tile's values.
+    auto step = [&](int32_t tile, f32x16 (&s)[2], f32x16 (&next)[2], uint8_t* k_from, uint8_t* k_to, uint8_t* v_from, uint8_t* v_to) {
         const int32_t t0 = range.lo + tile * kWideTile;
-        const bool more = tile + 1 < tiles;
-        const uint64_t there_next = same_in_wave(there_lds[(tile + 1) & 1]);
-        if (more) load_rows(tile + 1);
-        uint8_t* const k_lds = lds + (tile & 1) * (2 * kPlane);
-        uint8_t* const v_lds = k_lds + kPlane;
-        // O^T's first operand: step u takes tokens 16 u + {0, 8} + 4 upper + 0 .. 3
-        const uint32_t i16 = lane & 15u, low = 2 * ((lane >> 4) & 1u) + ((i16 >> 1) & 1u);
-        auto v_operand = [&](int u, int d) -> u32x4 {
-            const uint32_t ta = 16 * u + 4 * upper + (i16 >> 2);
-            const uint8_t *row_a = v_lds + ta * (D * 2) + (i16 & 1u) * 8, *row_b = row_a + 8 * (D * 2);
-            const uint32_t at = (spread<D>(4 * d) ^ spread<D>(low) ^ v_swap(ta)) << 4;      // the same eight tokens on
-            const u32x2 a = read_transposed(row_a + at), b = read_transposed(row_b + at);
-            return u32x4{a[0], a[1], b[0], b[1]};
-        };
+        load_rows(tile + 2, k_to, tile + 1, v_to);
+        const uint64_t there_next = same_in_wave(there_lds[(tile + 1) & 3]);
         if (!idle && t0 < last.hi && t0 + kWideTile > first.lo) {
-            f32x16 s[2];
-#pragma unroll
-            for (int a = 0; a < 2; ++a)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[a][i] = 0.f;
-            const uint32_t x = spread<D>(upper) ^ k_swap(m);             // the same 32 tokens on
-            const uint8_t* p0 = k_lds + m * (D * 2);
-#pragma unroll
-            for (int k = 0; k < kK; ++k)
-#pragma unroll
-                for (int a = 0; a < 2; ++a) s[a] = E::mfma32(*(const u32x4*)(p0 + a * (32 * D * 2) + ((spread<D>(2 * k) ^ x) << 4)), qf[k], s[a]);
-            if (!(there == ~0ull && t0 >= last.lo && t0 + kWideTile <= first.hi)) {
-                // the tile's tokens that this line sees; s[a][i] is token 32 a + 8 (i / 4) + 4 upper + i % 4
-                uint64_t seen = there;
+            const bool masked = !(there == ~0ull && t0 >= last.lo && t0 + kWideTile <= first.hi);
+            if (masked) {
+                uint64_t seen = there;                                   // the tile's tokens that this line sees
                 if (see.hi < t0 + kWideTile) seen = see.hi > t0 ? seen & ~(~0ull << (see.hi - t0)) : 0;
                 if (see.lo > t0) seen = see.lo < t0 + kWideTile ? seen & ~0ull << (see.lo - t0) : 0;
                 seen >>= 4 * upper;
@@ -721,10 +747,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
                     for (int i = 0; i < 16; ++i) s[a][i] = half & (1u << (8 * (i >> 2) + (i & 3))) ? s[a][i] : -INFINITY;
                 }
             }
-            float big = s[0][0];
-#pragma unroll
-            for (int i = 1; i < 32; ++i) big = fmaxf(big, s[i >> 4][i & 15]);
-            big = max_over32(big) * g.to_log2;
+            const float big = max_over32(masked ? largest(s) : big_of) * g.to_log2;
             if (__any(big > top + kLag)) {
                 const float now = fmaxf(top, big), f = rescale(top, now);
                 top = now;
@@ -735,31 +758,83 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             const float against = E::kWeightShift - (top == -INFINITY ? 0.f : top);
             u32x4 p[4];
             float add[2] = {0.f, 0.f};
+            auto weights = [&](int from, int to) {                       // pairs of them
 #pragma unroll
-            for (int a = 0; a < 2; ++a) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float x0 = __builtin_amdgcn_exp2f(fmaf(s[a][2 * j], g.to_log2, against)), x1 = __builtin_amdgcn_exp2f(fmaf(s[a][2 * j + 1], g.to_log2, against));
+                for (int j = from; j < to; ++j) {
+                    const float x0 = __builtin_amdgcn_exp2f(fmaf(s[j >> 3][2 * (j & 7)], g.to_log2, against)),
+                                x1 = __builtin_amdgcn_exp2f(fmaf(s[j >> 3][2 * (j & 7) + 1], g.to_log2, against));
                     add[0] += x0;
                     add[1] += x1;
-                    p[a * 2 + (j >> 2)][j & 3] = E::pack2(x0, x1);
+                    p[j >> 2][j & 3] = E::pack2(x0, x1);
                 }
+            };
+            // O^T's first operand: step u takes tokens 16 u + {0, 8} + 4 upper + 0 .. 3
+            const uint32_t i16 = lane & 15u, low = 2 * ((lane >> 4) & 1u) + ((i16 >> 1) & 1u);
+            constexpr int kSteps = 4 * kDims;
+            u32x4 vf[kSteps];
+            auto read = [&](int i) {
+                const uint32_t ta = 16 * (i / kDims) + 4 * upper + (i16 >> 2);
+                const uint8_t *row_a = v_from + ta * (D * 2) + (i16 & 1u) * 8, *row_b = row_a + 8 * (D * 2);
+                const uint32_t at = (spread<D>(4 * (i % kDims)) ^ spread<D>(low) ^ v_swap(ta)) << 4;     // the same eight tokens on
+                const u32x2 a = read_transposed(row_a + at), b = read_transposed(row_b + at);
+                vf[i] = u32x4{a[0], a[1], b[0], b[1]};
+            };
+            __builtin_amdgcn_sched_barrier(0);
+            scores(k_from, next, [&](int k) {
+                weights(12 * k / kK, 12 * (k + 1) / kK);
+                if (k == kK - 1) { read(0); read(1); }
+            });
+            big_of = next[0][0];
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                if (i + 2 < kSteps) read(i + 2);
+                o[i % kDims] = E::mfma32(vf[i], p[i / kDims], o[i % kDims]);
+                if (i < kSteps / 2) {
+                    weights(12 + 4 * i / (kSteps / 2), 12 + 4 * (i + 1) / (kSteps / 2));
+                } else {
+#pragma unroll
+                    for (int j = 32 * (i - kSteps / 2) / (kSteps / 2); j < 32 * (i + 1 - kSteps / 2) / (kSteps / 2); ++j) big_of = fmaxf(big_of, next[j >> 4][j & 15]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             sum += add[0] + add[1];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int d = 0; d < kDims; ++d) o[d] = E::mfma32(v_operand(u, d), p[u], o[d]);
+        } else if (!idle) {
+            scores(k_from, next, [](int) {});
+            big_of = largest(next);
         }
-        if (more) {
-            if (wave == 0 && tile + 2 < tiles) {
-                place_rows(tile + 2, page);
-                page = load_page(tile + 3);
-            }
-            store_rows(tile + 1, there_next);
+        if (wave == 0) {
+            place_rows(tile + 3, page);
+            page = load_page(tile + 4);
         }
+        store_rows(tile + 2, k_to, tile + 1, v_to, there_next);
         there = there_next;
         __syncthreads();
+    };
+
+    if (tiles > 0) {
+        if (wave == 0) {
+            const uint32_t page0 = load_page(0), page1 = load_page(1), page2 = load_page(2);
+            page = load_page(3);
+            place_rows(0, page0);
+            place_rows(1, page1);
+            place_rows(2, page2);
+        }
+        __syncthreads();
+        there = same_in_wave(there_lds[0]);
+        load_rows(0, k_even, 0, v_even);
+        if constexpr (kBits == 4) store_rows(0, k_even, 0, v_even, there);
+        load_rows(1, k_odd, tiles, v_odd);
+        if constexpr (kBits == 4) store_rows(1, k_odd, tiles, v_odd, 0);
+        else store_rows(0, k_even, 0, v_even, there);
+        __syncthreads();
+        f32x16 s0[2], s1[2];
+        scores(k_even, s0, [](int) {});
+        big_of = largest(s0);
+        __syncthreads();
+        for (int32_t tile = 0; tile < tiles; tile += 2) {
+            step(tile, s0, s1, k_odd, k_even, v_even, v_odd);
+            if (tile + 1 < tiles) step(tile + 1, s1, s0, k_even, k_odd, v_odd, v_even);
+        }
     }
 
     if (bad_page) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
