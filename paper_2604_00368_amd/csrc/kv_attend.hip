@@ -881,16 +881,19 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
 }
 
 // ---- the splits' parts ---------------------------------------------------------------------------
-// A workgroup for each row and query head, its waves take parts in turn: o = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).
-template <class E, int D>
+// o = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).  A workgroup for each row and query head, whose waves take parts in turn, or,
+// where a wave has few parts to go through anyway, a wave for each: kLines of them to a workgroup.
+template <class E, int D, int kLines>
 __global__ void __launch_bounds__(256) join_kernel(const AttendArgs g)
 {
     constexpr int kPer = D / 64, kAhead = 4;                             // values of a lane; parts that a wave has in flight
-    __shared__ float o_lds[kWaves][D], sum_lds[kWaves];
+    constexpr uint32_t kTurn = kWaves / kLines;                          // waves that share a line
+    __shared__ float o_lds[kLines == 1 ? kWaves : 1][D], sum_lds[kWaves];
     const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const uint32_t row = blockIdx.x / g.q_heads, q_head = blockIdx.x - row * g.q_heads;
+    const uint32_t line = blockIdx.x * kLines + wave / kTurn, turn = wave % kTurn;
+    const uint32_t row = line / g.q_heads, q_head = line - row * g.q_heads;
     const KvSeq q = kv_sequence(g.b, blockIdx.y);
-    if ((int32_t)row >= q.rows) return;
+    if ((int32_t)row >= q.rows) return;                                  // with kLines 1 the whole workgroup
     const uint64_t out_row = (uint64_t)q.row0 + row, first = (out_row * g.q_heads + q_head) * g.n_splits;
     const uint32_t n = splits_of(g, q);
     float top = -INFINITY, sum = 0.f, y[kPer];
@@ -899,40 +902,52 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs g)
     for (uint32_t i = lane; i < n; i += 64) top = fmaxf(top, dev_load<f32x2>(g.part_ml + (first + i) * 2)[0]);
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
-    for (uint32_t i = wave; i < n; i += kWaves * kAhead) {
+    for (uint32_t i = turn; i < n; i += kTurn * kAhead) {
         f32x2 ml[kAhead];
         float part[kAhead][kPer];
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
-            const uint64_t at = first + min(i + a * kWaves, n - 1);
+            const uint64_t at = first + min(i + a * kTurn, n - 1);
             ml[a] = dev_load<f32x2>(g.part_ml + at * 2);
 #pragma unroll
             for (int k = 0; k < kPer; ++k) part[a][k] = dev_load<float>(g.part_o + at * D + lane * kPer + k);
         }
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
-            if (i + a * kWaves >= n || ml[a][1] == 0.f) continue;        // an empty part has a sum of 0 and no output
+            if (i + a * kTurn >= n || ml[a][1] == 0.f) continue;         // an empty part has a sum of 0 and no output
             const float f = rescale(ml[a][0], top);
             sum += ml[a][1] * f * f;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) y[k] += part[a][k] * f * f;
         }
     }
+    uint8_t* const to = g.out + out_row * g.out_stride + (uint64_t)q_head * D * 2;
+    if constexpr (kLines > 1) {
+        const float scale = sum == 0.f ? 0.f : 1.f / sum;
+        if constexpr (kPer == 1) {
+            dev_store(to + lane * 2, (uint16_t)E::pack2(y[0] * scale, 0.f));
+        } else {
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) o_lds[wave][lane * kPer + k] = y[k];
-    if (lane == 0) sum_lds[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x >= D / 2) return;                                    // two values a thread
-    float total = 0.f, a = 0.f, b = 0.f;
+            for (int k = 0; k < kPer; k += 2) dev_store(to + (lane * kPer + k) * 2, E::pack2(y[k] * scale, y[k + 1] * scale));
+        }
+        if (g.lse && lane == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, sum, E::kWeightShift);
+    } else {
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        total += sum_lds[w];
-        a += o_lds[w][threadIdx.x * 2];
-        b += o_lds[w][threadIdx.x * 2 + 1];
+        for (int k = 0; k < kPer; ++k) o_lds[wave][lane * kPer + k] = y[k];
+        if (lane == 0) sum_lds[wave] = sum;
+        __syncthreads();
+        if (threadIdx.x >= D / 2) return;                                // two values a thread
+        float total = 0.f, a = 0.f, b = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            total += sum_lds[w];
+            a += o_lds[w][threadIdx.x * 2];
+            b += o_lds[w][threadIdx.x * 2 + 1];
+        }
+        const float scale = total == 0.f ? 0.f : 1.f / total;
+        dev_store(to + threadIdx.x * 4, E::pack2(a * scale, b * scale));
+        if (g.lse && threadIdx.x == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, total, E::kWeightShift);
     }
-    const float scale = total == 0.f ? 0.f : 1.f / total;
-    dev_store(g.out + out_row * g.out_stride + ((uint64_t)q_head * D + threadIdx.x * 2) * 2, E::pack2(a * scale, b * scale));
-    if (g.lse && threadIdx.x == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, total, E::kWeightShift);
 }
 
 // ---- host ----------------------------------------------------------------------------------------
@@ -957,10 +972,11 @@ Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_att
     if (a.window && (a.flags & TENT_KV_ATTEND_ALL) && a.window < span) span = a.window;
     span += kStep;                                                       // the first token is rounded down
     const uint64_t units = (uint64_t)b.n_seqs * c.kv_heads * (s.wide ? s.line_tiles : 1);
-    const uint64_t wanted = s.wide ? 512 : 1536, least = s.wide ? 512 : 256;
-    uint64_t n = (wanted + units - 1) / units, most = (span + least - 1) / least;
+    const bool filled = s.wide && units >= 256;
+    const uint64_t wanted = filled ? 1024 : s.wide ? 512 : 1536, least = filled ? 4096 : s.wide ? 512 : 256;
+    uint64_t n = (wanted + units - 1) / units, most = filled ? span / least : (span + least - 1) / least;
     n = n > most ? most : n;
-    if (s.wide && units >= 256) n = 1;
+    n = n < 1 ? 1 : n;
     const uint64_t tokens = ((span + n - 1) / n + 127) / 128 * 128;
     s.split_tokens = (uint32_t)tokens;
     s.n_splits = (uint32_t)((span + tokens - 1) / tokens);
@@ -1002,7 +1018,9 @@ int launch(const Shape& s, const AttendArgs& g, hipStream_t stream)
     }
     if (hipGetLastError() != hipSuccess) return TENT_ERR_HIP;
     if (g.part_o) {
-        hipLaunchKernelGGL((join_kernel<E, D>), dim3((uint32_t)join, g.b.n_seqs), threads, 0, stream, g);
+        // A wave to a line: up to four parts are all in flight at once.
+        if (s.n_splits <= 4) hipLaunchKernelGGL((join_kernel<E, D, kWaves>), dim3((uint32_t)((join + kWaves - 1) / kWaves), g.b.n_seqs), threads, 0, stream, g);
+        else hipLaunchKernelGGL((join_kernel<E, D, 1>), dim3((uint32_t)join, g.b.n_seqs), threads, 0, stream, g);
         if (hipGetLastError() != hipSuccess) return TENT_ERR_HIP;
     }
     return TENT_OK;

@@ -105,62 +105,69 @@ __device__ __forceinline__ float in_32(double x)
     return y;
 }
 
+// A 32-bit value of another lane of the same head.
+__device__ __forceinline__ uint32_t of_lane(uint32_t x, uint32_t lane) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(lane * 4), (int)x); }
+
 struct AppendArgs {
     tent_kv_append_args a;
     KvCache c;
     tent_kv_batch b;
-    uint32_t row_tile;
+    uint32_t per_row;          // lanes that a row needs: one for every eight values of its heads
+    uint32_t side;             // rows that a workgroup takes side by side
 };
 
-// Eight values of a head, normalised and turned.  F: float for queries; double for keys, so that a value next to the border of
-// two codes falls on its own side.  `w`, `cs`: this lane's weights and, for its dimensions, cosines and sines.
+// Eight values of a head, normalised and turned; the lanes of the head come here together.  F: float for queries; double for keys,
+// so that a value next to the border of two codes falls on its own side.  `w`: the weights of this lane's dimensions, `cs`: their
+// cosines and sines.  What a dimension turns with is in another lane of the head.
 template <class E, int D, class F>
-__device__ __forceinline__ u32x4 norm_rotate(const tent_kv_append_args& a, const uint8_t* head, uint32_t chunk, const void* weight,
-                                             const float* cs)
+__device__ __forceinline__ u32x4 norm_rotate(const tent_kv_append_args& a, u32x4 raw, uint32_t chunk, bool weighted, u32x4 w, const float* cs)
 {
     constexpr uint32_t kChunks = D / 8;
+    if (!weighted && !a.rope) return raw;
     const uint32_t half = a.rope_dim / 16;                               // chunks of one half
     const bool turned = a.rope && chunk < 2 * half;
     const bool pairs = a.flags & TENT_KV_ROPE_PAIRS;
-    const uint32_t partner = turned && !pairs ? (chunk < half ? chunk + half : chunk - half) : chunk;
-    const u32x4 raw = dev_load<u32x4>(head + chunk * 16);
-    const u32x4 raw2 = turned && !pairs ? dev_load<u32x4>(head + partner * 16) : raw;
-    if (!weight && !turned) return raw;
-    F x[8], y[8];
+    F x[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[2 * i] = (F)E::to_float(raw[i] & 0xFFFFu);
         x[2 * i + 1] = (F)E::to_float(raw[i] >> 16);
-        y[2 * i] = (F)E::to_float(raw2[i] & 0xFFFFu);
-        y[2 * i + 1] = (F)E::to_float(raw2[i] >> 16);
     }
-    if (weight) {
+    F r = 1;
+    if (weighted) {
         F sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
         sum = sum_lanes<kChunks>(sum);
-        const F r = (F)1 / sqrt(sum * ((F)1 / D) + (F)a.eps);
-        const u32x4 w = dev_load<u32x4>((const uint8_t*)weight + chunk * 16), w2 = dev_load<u32x4>((const uint8_t*)weight + partner * 16);
+        r = (F)1 / sqrt(sum * ((F)1 / D) + (F)a.eps);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i] *= r * (F)E::to_float(w[i] & 0xFFFFu);
             x[2 * i + 1] *= r * (F)E::to_float(w[i] >> 16);
-            y[2 * i] *= r * (F)E::to_float(w2[i] & 0xFFFFu);
-            y[2 * i + 1] *= r * (F)E::to_float(w2[i] >> 16);
         }
     }
-    if (turned) {
-        if (pairs) {
+    if (a.rope && !pairs) {
+        const uint32_t partner = (threadIdx.x & 63u) - chunk + (!turned ? chunk : chunk < half ? chunk + half : chunk - half);
+        const F sign = chunk < half ? (F)-1 : (F)1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const F c = (F)cs[i], s = (F)cs[4 + i], p = x[2 * i], q = x[2 * i + 1];
-                x[2 * i] = p * c - q * s;
-                x[2 * i + 1] = q * c + p * s;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t other = of_lane(raw[i], partner), other_w = weighted ? of_lane(w[i], partner) : 0u;
+            F lo = (F)E::to_float(other & 0xFFFFu), hi = (F)E::to_float(other >> 16);
+            if (weighted) {
+                lo *= r * (F)E::to_float(other_w & 0xFFFFu);
+                hi *= r * (F)E::to_float(other_w >> 16);
             }
-        } else {
-            const F sign = chunk < half ? (F)-1 : (F)1;
+            if (turned) {
+                x[2 * i] = x[2 * i] * (F)cs[2 * i] + sign * lo * (F)cs[8 + 2 * i];
+                x[2 * i + 1] = x[2 * i + 1] * (F)cs[2 * i + 1] + sign * hi * (F)cs[9 + 2 * i];
+            }
+        }
+    } else if (turned) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * (F)cs[i] + sign * y[i] * (F)cs[8 + i];
+        for (int i = 0; i < 4; ++i) {
+            const F c = (F)cs[i], t = (F)cs[4 + i], p = x[2 * i], q = x[2 * i + 1];
+            x[2 * i] = p * c - q * t;
+            x[2 * i + 1] = q * c + p * t;
         }
     }
     u32x4 out;
@@ -169,59 +176,85 @@ __device__ __forceinline__ u32x4 norm_rotate(const tent_kv_append_args& a, const
     return out;
 }
 
-// A workgroup takes `row_tile` rows: their places first, then all heads of a row (queries, keys, values), a chunk of eight a
-// lane.  A lane keeps its chunk number over the heads, as the workgroup is a multiple of a head's lanes, and so its cosines.
+// A workgroup takes one row, or `side` short ones side by side, all heads of it (queries, keys, values), a chunk of eight a lane and
+// kBatch chunks at a time.  The chunks are on their way while the first wave finds where the row belongs, a chain of four loads.
+// A lane keeps its chunk number over the heads, as the workgroup is a multiple of a head's lanes, and so its cosines and weights.
+constexpr uint32_t kBatch = 4;
 template <class E, int D, int kBits>
 __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
 {
     __shared__ RowPlace place[kMaxRowTile];
     constexpr uint32_t kChunks = D / 8;
     const tent_kv_append_args& a = g.a;
-    const uint32_t row0 = blockIdx.x * g.row_tile;
-    const uint32_t n = g.b.n_rows - row0 < g.row_tile ? g.b.n_rows - row0 : g.row_tile;
-    find_rows(place, g.c, g.b, row0, n);
-    const uint32_t chunk = threadIdx.x % kChunks, heads = a.q_heads + 2 * g.c.heads;
-    for (uint32_t r = 0; r < n; ++r) {
-        const RowPlace p = place[r];
-        if (!p.live) continue;
-        const uint64_t row = row0 + r;
-        float cs[16];
-        if (a.rope) {
-            const uint32_t at = a.positions ? (uint32_t)a.positions[row] : p.position;
-            if (at >= a.rope_rows) {
-                if (threadIdx.x == 0) kv_note(g.b.errors, TENT_KV_BAD_POSITION);
-                continue;
-            }
-            const uint32_t half = a.rope_dim / 16;
-            if (chunk < 2 * half) {
-                const bool pairs = a.flags & TENT_KV_ROPE_PAIRS;
-                const float* t = a.rope + (uint64_t)at * a.rope_dim + (pairs ? chunk * 4 : (chunk < half ? chunk : chunk - half) * 8);
-                const f32x4 c0 = dev_load<f32x4>(t), s0 = dev_load<f32x4>(t + a.rope_dim / 2);
-                const f32x4 c1 = pairs ? s0 : dev_load<f32x4>(t + 4), s1 = pairs ? s0 : dev_load<f32x4>(t + a.rope_dim / 2 + 4);
+    const uint32_t row0 = blockIdx.x * g.side, n = g.b.n_rows - row0 < g.side ? g.b.n_rows - row0 : g.side;
+    const uint32_t r = g.side == 1 ? 0u : threadIdx.x / g.per_row, x0 = threadIdx.x - r * g.per_row, chunk = x0 % kChunks;
+    const uint64_t row = row0 + r;
+    const bool mine = r < n;
+    auto load = [&](uint32_t x) -> u32x4 {                               // lanes past the last have nothing
+        const uint32_t h = x / kChunks;
+        const uint8_t* p;
+        if (h < a.q_heads) p = (const uint8_t*)a.q + (row * a.q_stride + (uint64_t)h * D) * 2;
+        else if (h < a.q_heads + g.c.heads) p = (const uint8_t*)a.k + (row * a.k_stride + (uint64_t)(h - a.q_heads) * D) * 2;
+        else p = (const uint8_t*)a.v + (row * a.v_stride + (uint64_t)(h - a.q_heads - g.c.heads) * D) * 2;
+        return dev_load<u32x4>(p + chunk * 16);
+    };
+    u32x4 raw[kBatch];
+    auto load_batch = [&](uint32_t x) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    cs[i] = c0[i];
-                    cs[4 + i] = c1[i];
-                    cs[8 + i] = s0[i];
-                    cs[12 + i] = s1[i];
-                }
+        for (uint32_t i = 0; i < kBatch; ++i)
+            if (mine && x + i * blockDim.x < g.per_row) raw[i] = load(x + i * blockDim.x);
+    };
+    load_batch(x0);
+    u32x4 wq = {0, 0, 0, 0}, wk = {0, 0, 0, 0};
+    if (a.q_weight) wq = dev_load<u32x4>((const uint8_t*)a.q_weight + chunk * 16);
+    if (a.k_weight) wk = dev_load<u32x4>((const uint8_t*)a.k_weight + chunk * 16);
+    find_rows(place, g.c, g.b, row0, n);
+    if (!mine) return;
+    const RowPlace p = place[r];
+    if (!p.live) return;
+    float cs[16] = {};
+    if (a.rope) {
+        const uint32_t at = a.positions ? (uint32_t)a.positions[row] : p.position;
+        if (at >= a.rope_rows) {
+            if (x0 == 0) kv_note(g.b.errors, TENT_KV_BAD_POSITION);
+            return;
+        }
+        const uint32_t half = a.rope_dim / 16;
+        if (chunk < 2 * half) {
+            const bool pairs = a.flags & TENT_KV_ROPE_PAIRS;
+            const float* t = a.rope + (uint64_t)at * a.rope_dim + (pairs ? chunk * 4 : (chunk < half ? chunk : chunk - half) * 8);
+            const f32x4 c0 = dev_load<f32x4>(t), s0 = dev_load<f32x4>(t + a.rope_dim / 2);
+            const f32x4 c1 = pairs ? s0 : dev_load<f32x4>(t + 4), s1 = pairs ? s0 : dev_load<f32x4>(t + a.rope_dim / 2 + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                cs[i] = c0[i];
+                cs[4 + i] = c1[i];
+                cs[8 + i] = s0[i];
+                cs[12 + i] = s1[i];
             }
         }
-        for (uint32_t h = threadIdx.x / kChunks; h < heads; h += blockDim.x / kChunks) {
-            if (h < a.q_heads) {
-                const u32x4 y = norm_rotate<E, D, float>(a, (const uint8_t*)a.q + (row * a.q_stride + (uint64_t)h * D) * 2, chunk, a.q_weight, cs);
-                dev_store((uint8_t*)a.q_out + (row * a.q_out_stride + (uint64_t)h * D + chunk * 8) * 2, y);
-            } else if (p.page >= 0) {
-                uint32_t kh = h - a.q_heads;
-                if (kh < g.c.heads) {
-                    const u32x4 y = norm_rotate<E, D, double>(a, (const uint8_t*)a.k + (row * a.k_stride + (uint64_t)kh * D) * 2, chunk, a.k_weight, cs);
-                    put8<E, D, kBits>(g.c.k + p.page, g.c.page_shift, p.slot, g.c.heads, kh, chunk, y);
-                } else {
-                    kh -= g.c.heads;
-                    const u32x4 y = dev_load<u32x4>((const uint8_t*)a.v + (row * a.v_stride + (uint64_t)kh * D + chunk * 8) * 2);
-                    put8<E, D, kBits>(g.c.v + p.page, g.c.page_shift, p.slot, g.c.heads, kh, chunk, y);
-                }
-            }
+    }
+    for (uint32_t x = x0, left = kBatch; x < g.per_row; x += blockDim.x, --left) {
+        if (left == 0) {
+            load_batch(x);
+            left = kBatch;
+        }
+        const u32x4 now = raw[0];
+#pragma unroll
+        for (uint32_t i = 0; i + 1 < kBatch; ++i) raw[i] = raw[i + 1];
+        // cosines and weights are kept as they are: the compiler would keep them in 64 bits, and twice the registers
+#pragma unroll
+        for (int i = 0; i < 16; ++i) __asm__ volatile("" : "+v"(cs[i]));
+        __asm__ volatile("" : "+v"(wq), "+v"(wk));
+        const uint32_t h = x / kChunks;
+        if (h < a.q_heads) {
+            const u32x4 y = norm_rotate<E, D, float>(a, now, chunk, a.q_weight, wq, cs);
+            dev_store((uint8_t*)a.q_out + (row * a.q_out_stride + (uint64_t)h * D + chunk * 8) * 2, y);
+        } else if (p.page >= 0) {
+            const bool is_v = h >= a.q_heads + g.c.heads;
+            const uint32_t kh = h - a.q_heads - (is_v ? g.c.heads : 0u);
+            const u32x4 y = is_v ? now : norm_rotate<E, D, double>(a, now, chunk, a.k_weight, wk, cs);
+            put8<E, D, kBits>((is_v ? g.c.v : g.c.k) + p.page, g.c.page_shift, p.slot, g.c.heads, kh, chunk, y);
         }
     }
 }
@@ -234,6 +267,7 @@ struct ReadArgs {
     uint32_t row_tile;
 };
 
+// A workgroup takes `row_tile` rows, their keys first, then their values, kBatch chunks a lane in flight.
 template <class E, int D, int kBits>
 __global__ void __launch_bounds__(256) read_kernel(const ReadArgs g)
 {
@@ -242,25 +276,39 @@ __global__ void __launch_bounds__(256) read_kernel(const ReadArgs g)
     const uint32_t row0 = blockIdx.x * g.row_tile;
     const uint32_t n = g.b.n_rows - row0 < g.row_tile ? g.b.n_rows - row0 : g.row_tile;
     find_rows(place, g.c, g.b, row0, n);
-    const uint32_t one = g.c.heads * kChunks;                            // chunks of K of a row
-    for (uint32_t i = threadIdx.x; i < n * 2 * one; i += blockDim.x) {
-        const uint32_t r = i / (2 * one), x = i - r * 2 * one;
-        const bool is_v = x >= one;
-        const uint32_t y = is_v ? x - one : x, head = y / kChunks, chunk = y % kChunks;
-        const RowPlace p = place[r];
-        if (!p.live) continue;
-        u32x4 value = {0, 0, 0, 0};
-        if (p.page >= 0) {
-            const uint8_t* page = (is_v ? g.c.v : g.c.k) + p.page;
+    const uint32_t one = g.c.heads * kChunks, all = 2 * n * one;         // chunks of K of a row, and of all there is
+    for (uint32_t first = threadIdx.x; first < all; first += kBatch * 256) {
+        u32x4 value[kBatch];                                             // 4 bits: the codes, the word that holds the scale, and where in it
+        uint32_t where[kBatch];
+#pragma unroll
+        for (uint32_t j = 0; j < kBatch; ++j) {
+            const uint32_t i = first + j * 256 < all ? first + j * 256 : first;
+            const bool is_v = i >= n * one;
+            const uint32_t x = is_v ? i - n * one : i, r = x / one, y = x - r * one, head = y / kChunks, chunk = y % kChunks;
+            const RowPlace p = place[r];
+            where[j] = p.page >= 0 ? 2u : p.live ? 1u : 0u;
+            const uint8_t* page = (is_v ? g.c.v : g.c.k) + (p.page >= 0 ? p.page : 0);
+            const uint32_t slot = p.page >= 0 ? p.slot : 0u;             // of the first page, where there is none
             if constexpr (kBits == 16) {
-                value = dev_load<u32x4>(page + at16<D>(p.slot, g.c.heads, head, chunk));
+                value[j] = dev_load<u32x4>(page + at16<D>(slot, g.c.heads, head, chunk));
             } else {
-                const uint32_t codes = dev_load<uint32_t>(page + at_codes<D>(p.slot, g.c.heads, head, chunk));
-                const uint32_t byte = dev_load<uint8_t>(page + at_scale<D>(p.slot, g.c.heads, head, chunk, g.c.page_shift));
-                value = decode8<E>(codes, scale_of(byte));
+                value[j][0] = dev_load<uint32_t>(page + at_codes<D>(slot, g.c.heads, head, chunk));
+                const uint32_t at = at_scale<D>(slot, g.c.heads, head, chunk, g.c.page_shift);
+                value[j][1] = dev_load<uint32_t>(page + (at & ~3u));     // a byte's load would be waited for here, to extend it
+                value[j][2] = 8 * (at & 3u);
             }
         }
-        dev_stream((is_v ? g.v : g.k) + (row0 + r) * g.stride + (uint64_t)y * 16, value);
+#pragma unroll
+        for (uint32_t j = 0; j < kBatch; ++j) {
+            const uint32_t i = first + j * 256;
+            if (i >= all || where[j] == 0u) continue;
+            const bool is_v = i >= n * one;
+            const uint32_t x = is_v ? i - n * one : i, r = x / one, y = x - r * one;
+            u32x4 out = value[j];
+            if constexpr (kBits == 4) out = decode8<E>(value[j][0], scale_of(value[j][1] >> value[j][2] & 0xFFu));
+            if (where[j] == 1u) out = u32x4{0, 0, 0, 0};
+            dev_stream((is_v ? g.v : g.k) + (row0 + r) * g.stride + (uint64_t)y * 16, out);
+        }
     }
 }
 
@@ -271,7 +319,7 @@ struct PackArgs {
     uint32_t n_pages, parts;   // workgroups for one page of one pool
 };
 
-// A workgroup takes kPackChunks chunks a lane of one page of K or V.
+// A workgroup takes four chunks a lane of one page of K or V.
 constexpr uint32_t kPackChunks = 4;
 template <class E, int D>
 __global__ void __launch_bounds__(256) pack_kernel(const PackArgs g)
@@ -294,39 +342,62 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackArgs g)
 #pragma unroll
     for (uint32_t k = 0; k < kPackChunks; ++k) {
         const uint32_t x = first + k * blockDim.x;
-        if (x < n) v[k] = dev_load<u32x4>(src + (uint64_t)x * 16);
+        v[k] = x < n ? dev_load<u32x4>(src + (uint64_t)x * 16) : u32x4{0, 0, 0, 0};
     }
+    // Four lanes share a block and have it for each k.  They exchange their codes so that lane j of them stores the 16 bytes of k = j.
+    const uint32_t lane = threadIdx.x & 63u, j = lane & 3u;
+    u32x4 codes;
+    uint32_t scale = 0;
 #pragma unroll
     for (uint32_t k = 0; k < kPackChunks; ++k) {
-        const uint32_t x = first + k * blockDim.x;
-        if (x >= n) continue;
         uint32_t byte;
-        const uint32_t codes = encode8<E>(v[k], byte);
-        dev_store(dst + (uint64_t)x * 4, codes);
-        if ((x & 3u) == 0) dev_store(dst + scales + x / 4, (uint8_t)byte);
+        codes[k] = encode8<E>(v[k], byte);
+        scale = j == k ? byte : scale;
     }
-}
-
-// Rows of a workgroup: as many as leave about four workgroups for each of the 256 compute units.
-uint32_t row_tile(uint32_t n_rows)
-{
-    const uint32_t n = n_rows / 1024;
-    return n < 1 ? 1 : n > kMaxRowTile ? kMaxRowTile : n;
+    u32x4 mine;                                                          // mine[i]: codes of lane i of the four for k = j
+#pragma unroll
+    for (uint32_t d = 0; d < 4; ++d) {                                   // from lane j ^ d, which gives what it has for k = j
+        const uint32_t k = j ^ d, give = k == 0 ? codes[0] : k == 1 ? codes[1] : k == 2 ? codes[2] : codes[3];
+        const uint32_t got = d == 0   ? give
+                             : d == 1 ? (uint32_t)__builtin_amdgcn_mov_dpp((int)give, 0xB1, 0xF, 0xF, true)
+                             : d == 2 ? (uint32_t)__builtin_amdgcn_mov_dpp((int)give, 0x4E, 0xF, 0xF, true)
+                                      : (uint32_t)__builtin_amdgcn_mov_dpp((int)give, 0x1B, 0xF, 0xF, true);
+        mine[0] = k == 0 ? got : mine[0];
+        mine[1] = k == 1 ? got : mine[1];
+        mine[2] = k == 2 ? got : mine[2];
+        mine[3] = k == 3 ? got : mine[3];
+    }
+    // and of 16 lanes, which have four blocks in a row for each k, lanes 0..3 store the scales of k = 0..3
+    scale <<= 8 * (lane >> 2 & 3u);
+    scale |= (uint32_t)__builtin_amdgcn_mov_dpp((int)scale, 0x124, 0xF, 0xF, true);      // lanes rotated by 4 within 16
+    scale |= (uint32_t)__builtin_amdgcn_mov_dpp((int)scale, 0x128, 0xF, 0xF, true);      // by 8
+    const uint32_t x = first - j + j * blockDim.x;                       // of the four lanes' first chunk for k = j
+    if (x < n) dev_store(dst + (uint64_t)x * 4, mine);
+    if ((lane & 12u) == 0) {
+        if (x + 16 <= n) dev_store(dst + scales + x / 4, scale);         // a head of 64 values ends inside, a page may
+        else
+            for (uint32_t i = 0; x + 4 * i < n; ++i) dev_store(dst + scales + x / 4 + i, (uint8_t)(scale >> (8 * i)));
+    }
 }
 
 int launched() { return hipGetLastError() == hipSuccess ? TENT_OK : TENT_ERR_HIP; }
 
 template <class E, int D, int kBits>
-int launch_append(const AppendArgs& g, hipStream_t s)
+int launch_append(AppendArgs g, hipStream_t s)
 {
-    const uint32_t lanes = (g.a.q_heads + 2 * g.c.heads) * (D / 8);
-    const uint32_t threads = lanes >= 256 ? 256 : (lanes + 63) / 64 * 64;
-    hipLaunchKernelGGL((append_kernel<E, D, kBits>), dim3((g.b.n_rows + g.row_tile - 1) / g.row_tile), dim3(threads), 0, s, g);
+    g.per_row = (g.a.q_heads + 2 * g.c.heads) * (D / 8);
+    g.side = g.per_row >= 256 ? 1 : 256 / g.per_row;                     // at most 16: a row has a key and a value of 64 at least
+    const uint32_t turns = (g.per_row + 255) / 256, threads = g.side > 1 ? 256 : (g.per_row + turns * 64 - 1) / (turns * 64) * 64;
+    hipLaunchKernelGGL((append_kernel<E, D, kBits>), dim3((g.b.n_rows + g.side - 1) / g.side), dim3(threads), 0, s, g);
     return launched();
 }
+// Rows of a workgroup: as many as its lanes take in one batch, fewer where that leaves compute units without one.
 template <class E, int D, int kBits>
-int launch_read(const ReadArgs& g, hipStream_t s)
+int launch_read(ReadArgs g, hipStream_t s)
 {
+    const uint32_t batch = kBatch * 256 / (2 * g.c.heads * (D / 8)), spread = g.b.n_rows / 1024;
+    const uint32_t n = batch < spread ? batch : spread;
+    g.row_tile = n < 1 ? 1 : n > kMaxRowTile ? kMaxRowTile : n;
     hipLaunchKernelGGL((read_kernel<E, D, kBits>), dim3((g.b.n_rows + g.row_tile - 1) / g.row_tile), dim3(256), 0, s, g);
     return launched();
 }
@@ -374,7 +445,7 @@ extern "C" int tent_kv_append(const tent_kv_cache* cache, const tent_kv_batch* b
     if (!(args->eps >= 0.f) || args->eps > 3.4e38f) return TENT_ERR_RANGE;
     if (args->rope && (args->rope_rows < 1 || args->rope_dim < 16 || args->rope_dim > D || args->rope_dim % 16)) return TENT_ERR_RANGE;
     if ((uintptr_t)args->positions & 3u) return TENT_ERR_INVALID;
-    const AppendArgs g{*args, kv_cache_dev(*cache), *batch, row_tile(n)};
+    const AppendArgs g{*args, kv_cache_dev(*cache), *batch, 0, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define TENT_APPEND(dim)                                                                                   \
     (cache->type == TENT_BF16 ? (cache->bits == 16 ? launch_append<Bf16, dim, 16>(g, s) : launch_append<Bf16, dim, 4>(g, s)) \
@@ -391,7 +462,7 @@ extern "C" int tent_kv_read(const tent_kv_cache* cache, const tent_kv_batch* bat
     if (batch->n_seqs == 0 || batch->n_rows == 0) return TENT_OK;
     if ((rc = kv_check_rows(k_out, out_stride, cache->kv_heads, cache->head_dim, batch->n_rows)) != TENT_OK) return rc;
     if ((rc = kv_check_rows(v_out, out_stride, cache->kv_heads, cache->head_dim, batch->n_rows)) != TENT_OK) return rc;
-    const ReadArgs g{kv_cache_dev(*cache), *batch, static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out), out_stride * 2, row_tile(batch->n_rows)};
+    const ReadArgs g{kv_cache_dev(*cache), *batch, static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out), out_stride * 2, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define TENT_READ(dim)                                                                                     \
     (cache->type == TENT_BF16 ? (cache->bits == 16 ? launch_read<Bf16, dim, 16>(g, s) : launch_read<Bf16, dim, 4>(g, s)) \
