@@ -260,6 +260,10 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
 #pragma unroll
         for (int k = 0; k < kK; ++k) qf[rt][k] = dev_load<u32x4>(p + k * (kBits == 16 ? 64 : 16));
     }
+#pragma unroll
+    for (int rt = 0; rt < kLineTiles; ++rt)
+#pragma unroll
+        for (int k = 0; k < kK; ++k) arrived(qf[rt][k]);
     // tokens that every line sees
     const int32_t all_lo = kv_span(q.rows - 1, q.rows, q.len, g.window, g.all).lo, all_hi = kv_span(0, q.rows, q.len, g.window, g.all).hi;
 
@@ -289,9 +293,11 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
         const int32_t t = range.lo + tile * kTile + (int32_t)(lane & 31u);
         const bool inside = t < range.hi, there = inside && page < g.c.n_pages;
         bad_page |= inside && !there;
-        if (lane < 32) rows_at[wave][lane] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
+        uint32_t to = lane;
+        __asm__ volatile("" : "+v"(to));                                 // its address is computed here, not kept in a register
+        if (lane < 32) rows_at[wave][to] = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
         same_wave_order();
-        return (uint32_t)__ballot(there);
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)__ballot(there));
     };
     T now;
     auto load_rows = [&](u32x4* to, const uint8_t* pool) {
@@ -411,20 +417,20 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
             const u32x2 a = read_transposed(row_a + ((spread<D>(2 * d) ^ x) << 4)), b = read_transposed(row_b + ((spread<D>(2 * d) ^ x) << 4));
             return u32x4{a[0], a[1], b[0], b[1]};
         };
-        // this lane has tokens t0 + 8 quad + 0 .. 7 of its lines
-        auto sees = [&](int rt, int j) -> bool {
-            const int32_t t = t0 + (int32_t)(8 * quad) + j;
-            return t >= see[rt].lo && t < see[rt].hi && ((there >> (8 * quad + j)) & 1u);
-        };
         u32x4 p[kLineTiles];
 #pragma unroll
         for (int rt = 0; rt < kLineTiles; ++rt) {
             float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = s[rt][j >> 2][j & 3];
-            if (!whole)
+            if (!whole) {                                                // this lane has tokens t0 + 8 quad + 0 .. 7 of its line
+                uint32_t seen = there;
+                if (see[rt].hi < t0 + kTile) seen = see[rt].hi > t0 ? seen & ~(~0u << (see[rt].hi - t0)) : 0u;
+                if (see[rt].lo > t0) seen = see[rt].lo < t0 + kTile ? seen & ~0u << (see[rt].lo - t0) : 0u;
+                seen >>= 8 * quad;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = sees(rt, j) ? x[j] : -INFINITY;
+                for (int j = 0; j < 8; ++j) x[j] = seen & (1u << j) ? x[j] : -INFINITY;
+            }
             float big = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
             big = max_over32(max_over16(big)) * g.to_log2;
             if (__any(big > top[rt] + kLag)) {
@@ -958,8 +964,11 @@ struct Shape {
     uint64_t workspace;
 };
 
-// Which kernel, and how many splits: enough workgroups to fill the 256 compute units several times over, while a split keeps
-// enough tokens for its waves to have a tile in flight beside the one they work on.
+// Which kernel, and how many splits.  Few lines: enough workgroups to fill the 256 compute units several times over, while a split
+// keeps enough tokens for its waves to have a tile in flight beside the one they work on; a context of up to 768 tokens stays
+// whole, as a split of it saves less than its join takes (one row over 501 tokens: 7.4 us and 3.7 for the join, whole 9.2).
+// Many lines: enough workgroups to fill the compute units, or, if they are filled already and contexts so long that joins cost
+// little, to leave none with much more to do than others (chunks behind 6k-16k tokens: 406 us in one split, 340 + 17 in three).
 Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_attend_args& a)
 {
     Shape s{};
@@ -976,7 +985,7 @@ Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_att
     const uint64_t wanted = filled ? 1024 : s.wide ? 512 : 1536, least = filled ? 4096 : s.wide ? 512 : 256;
     uint64_t n = (wanted + units - 1) / units, most = filled ? span / least : (span + least - 1) / least;
     n = n > most ? most : n;
-    n = n < 1 ? 1 : n;
+    n = n < 1 || (!s.wide && span <= 768) ? 1 : n;
     const uint64_t tokens = ((span + n - 1) / n + 127) / 128 * 128;
     s.split_tokens = (uint32_t)tokens;
     s.n_splits = (uint32_t)((span + tokens - 1) / tokens);
