@@ -111,6 +111,7 @@ class Cache:
         self.page_tokens, self.kv_heads, self.head_dim = int(page_tokens), int(kv_heads), int(head_dim)
         self.c = T.tent_kv_cache(k.data_ptr(), v.data_ptr(), k.shape[0], stride, self.page_tokens, self.kv_heads, self.head_dim,
                                  _TYPES[dtype], bits, 0)
+        self.ref = C.byref(self.c)                                       # made once: calls take it as it is
 
     @property
     def page_bytes(self) -> int:
@@ -147,6 +148,7 @@ class Batch:
         self.errors = torch.zeros(1, dtype=torch.int32, device=page_table.device)
         self.c = T.tent_kv_batch(page_table.data_ptr(), kv_len.data_ptr(), row_start.data_ptr(), self.errors.data_ptr(), n_seqs, width,
                                  n_rows, max_rows, max_kv, 0)
+        self.ref = C.byref(self.c)
 
 
 def _together(cache, batch):
@@ -166,22 +168,24 @@ def append(cache: Cache, batch: Batch, k, v, q=None, q_weight=None, k_weight=Non
     neighbouring dimensions instead of halves.  q_out may be q."""
     _together(cache, batch)
     n, H, D, dtype, device = batch.n_rows, cache.kv_heads, cache.head_dim, cache.dtype, cache.device
-    a = T.tent_kv_append_args()
-    a.k_stride, a.v_stride = _rows(k, "k", dtype, n, H, D, device), _rows(v, "v", dtype, n, H, D, device)
-    a.k, a.v, a.eps = k.data_ptr(), v.data_ptr(), eps
+    k_stride, v_stride = _rows(k, "k", dtype, n, H, D, device), _rows(v, "v", dtype, n, H, D, device)
+    heads = q_stride = q_out_stride = 0
     if q is not None:
         heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
-        a.q_stride, a.q, a.q_heads = _rows(q, "q", dtype, n, heads, D, device), q.data_ptr(), heads
+        q_stride = _rows(q, "q", dtype, n, heads, D, device)
         if q_out is None:
-            q_out = torch.empty((n, heads, D), dtype=dtype, device=device)
-        a.q_out_stride, a.q_out = _rows(q_out, "q_out", dtype, n, heads, D, device), q_out.data_ptr()
+            q_out, q_out_stride = torch.empty((n, heads, D), dtype=dtype, device=device), heads * D
+        else:
+            q_out_stride = _rows(q_out, "q_out", dtype, n, heads, D, device)
     elif q_out is not None or q_weight is not None:
         raise ValueError("q_out and q_weight go with q")
     for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            if not _on_gpu(w, name, dtype, (D,)).is_contiguous() or w.device != device:
-                raise ValueError(f"{name} must be contiguous, on the cache's device")
-            setattr(a, name, w.data_ptr())
+        if w is not None and (not _on_gpu(w, name, dtype, (D,)).is_contiguous() or w.device != device):
+            raise ValueError(f"{name} must be contiguous, on the cache's device")
+    a = T.tent_kv_append_args(q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(), q_out.data_ptr() if q is not None else None,
+                              q_stride, k_stride, v_stride, q_out_stride, q_weight.data_ptr() if q_weight is not None else None,
+                              k_weight.data_ptr() if k_weight is not None else None)
+    a.q_heads, a.eps = heads, eps
     if rope is not None:
         if not _on_gpu(rope, "rope", torch.float32).is_contiguous() or rope.dim() != 2 or rope.device != device:
             raise ValueError("rope must be contiguous [positions, rope_dim] on the cache's device")
@@ -190,7 +194,7 @@ def append(cache: Cache, batch: Batch, k, v, q=None, q_weight=None, k_weight=Non
         if not _on_gpu(positions, "positions", torch.int32, (n,)).is_contiguous() or positions.device != device:
             raise ValueError("positions must be contiguous, on the cache's device")
         a.positions = positions.data_ptr()
-    _check(T.lib().tent_kv_append(cache.c, batch.c, a, _stream(k, stream)), "tent_kv_append")
+    _check(T.lib().tent_kv_append(cache.ref, batch.ref, C.byref(a), _stream(k, stream)), "tent_kv_append")
     return q_out
 
 
@@ -204,7 +208,7 @@ def pack(src: Cache, dst: Cache, src_pages, dst_pages, errors=None, stream=None)
         raise ValueError("as many pages on one side as on the other, on one device")
     if errors is not None:
         _on_gpu(errors, "errors", torch.int32, (1,))
-    _check(T.lib().tent_kv_pack(src.c, dst.c, src_pages.data_ptr(), dst_pages.data_ptr(), src_pages.shape[0],
+    _check(T.lib().tent_kv_pack(src.ref, dst.ref, src_pages.data_ptr(), dst_pages.data_ptr(), src_pages.shape[0],
                                 errors.data_ptr() if errors is not None else None, _stream(src_pages, stream)), "tent_kv_pack")
 
 
@@ -219,7 +223,7 @@ def read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None):
     stride = _rows(k_out, "k_out", cache.dtype, *shape, cache.device)
     if _rows(v_out, "v_out", cache.dtype, *shape, cache.device) != stride:
         raise ValueError("k_out and v_out must have the same strides")
-    _check(T.lib().tent_kv_read(cache.c, batch.c, k_out.data_ptr(), v_out.data_ptr(), stride, _stream(k_out, stream)), "tent_kv_read")
+    _check(T.lib().tent_kv_read(cache.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), stride, _stream(k_out, stream)), "tent_kv_read")
     return k_out, v_out
 
 
@@ -232,25 +236,23 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
     _together(cache, batch)
     n, D, dtype, device = batch.n_rows, cache.head_dim, cache.dtype, cache.device
     heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
-    a = T.tent_kv_attend_args()
-    a.q_stride, a.q, a.q_heads = _rows(q, "q", dtype, n, heads, D, device), q.data_ptr(), heads
+    q_stride = _rows(q, "q", dtype, n, heads, D, device)
     if out is None:
-        out = torch.empty((n, heads, D), dtype=dtype, device=device)
-    a.out_stride, a.out = _rows(out, "out", dtype, n, heads, D, device), out.data_ptr()
+        out, out_stride = torch.empty((n, heads, D), dtype=dtype, device=device), heads * D
+    else:
+        out_stride = _rows(out, "out", dtype, n, heads, D, device)
     if not 0 <= window < 1 << 31:
         raise ValueError("window must be 0 or more and below 2^31")
-    a.window, a.flags, a.scale = window, 0 if causal else T.TENT_KV_ATTEND_ALL, 1.0 / math.sqrt(D) if scale is None else scale
-    lse = None
-    if want_lse:
-        lse = torch.empty((n, heads), dtype=torch.float32, device=device)
-        a.lse = lse.data_ptr()
-    L, need = T.lib(), C.c_uint64()
-    _check(L.tent_kv_attend_workspace(cache.c, batch.c, a, need), "tent_kv_attend_workspace")
+    lse = torch.empty((n, heads), dtype=torch.float32, device=device) if want_lse else None
+    a = T.tent_kv_attend_args(q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else None, q_stride, out_stride, None, 0, heads, window,
+                              0 if causal else T.TENT_KV_ATTEND_ALL, 1.0 / math.sqrt(D) if scale is None else scale)
+    L, need, ref = T.lib(), C.c_uint64(), C.byref(a)
+    _check(L.tent_kv_attend_workspace(cache.ref, batch.ref, ref, C.byref(need)), "tent_kv_attend_workspace")
     if need.value:
         if workspace is None:
             workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
         a.workspace, a.workspace_bytes = _on_gpu(workspace, "workspace", torch.uint8).data_ptr(), workspace.numel()
-    _check(L.tent_kv_attend(cache.c, batch.c, a, _stream(q, stream)), "tent_kv_attend")
+    _check(L.tent_kv_attend(cache.ref, batch.ref, ref, _stream(q, stream)), "tent_kv_attend")
     return (out, lse) if want_lse else out
 
 
