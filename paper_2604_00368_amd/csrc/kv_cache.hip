@@ -10,9 +10,7 @@ namespace {
 // Where the rows of a workgroup lie: found by its first lanes, used by all of it.
 constexpr uint32_t kMaxRowTile = 16;
 struct RowPlace {
-    int64_t page;              // byte offset of the page; negative: the row is left out
-    uint32_t slot;             // token in the page
-    uint32_t position;
+    uint32_t seq, position;
     bool live;                 // the row belongs to a sequence that is not left out, at a position >= 0
 };
 
@@ -32,28 +30,48 @@ __device__ __forceinline__ uint32_t find_sequence(const tent_kv_batch& b, int32_
     return lo;
 }
 
+// Up to 64 sequences are loaded at once, a lane each, so that a row's place is one load away; more of them are searched.
 __device__ __forceinline__ void find_rows(RowPlace* to, const KvCache& c, const tent_kv_batch& b, uint32_t row0, uint32_t n)
 {
     if (threadIdx.x < 64) {
-        uint32_t s = find_sequence(b, (int32_t)row0, threadIdx.x);
-        if (threadIdx.x < n) {
-            const int32_t row = (int32_t)(row0 + threadIdx.x);
-            while (s + 1 < b.n_seqs && b.row_start[s + 1] <= row) ++s;
-            const KvSeq q = kv_sequence(b, s);
-            RowPlace p{-1, 0, 0, false};
+        const uint32_t lane = threadIdx.x;
+        const int32_t row = (int32_t)(row0 + lane);
+        uint32_t s = 0;
+        KvSeq q{0, 0, 0, false};
+        if (b.n_seqs <= 64) {
+            const uint32_t at = lane < b.n_seqs ? lane : b.n_seqs - 1;
+            const int32_t lo = b.row_start[at], hi = b.row_start[at + 1], len = b.kv_len[at];
+            for (uint32_t i = 0; i < n; ++i) {
+                const uint32_t before = (uint32_t)__popcll(__ballot(lane < b.n_seqs && lo <= (int32_t)(row0 + i)));
+                if (lane == i) s = before ? before - 1 : 0;
+            }
+            q = kv_sequence(b, __shfl(lo, (int)s, 64), __shfl(hi, (int)s, 64), __shfl(len, (int)s, 64));
+        } else {
+            s = find_sequence(b, (int32_t)row0, lane);
+            if (lane < n) {
+                while (s + 1 < b.n_seqs && b.row_start[s + 1] <= row) ++s;
+                q = kv_sequence(b, s);
+            }
+        }
+        if (lane < n) {
+            RowPlace p{0, 0, false};
             if (q.bad) kv_note(b.errors, TENT_KV_BAD_SEQUENCE);
             else if (row >= q.row0 && row < q.row0 + q.rows) {
                 const int32_t position = q.len - q.rows + (row - q.row0);
                 if (position < 0) kv_note(b.errors, TENT_KV_BAD_POSITION);
-                else {
-                    p = RowPlace{kv_page_of(c, b, s, (uint32_t)position), (uint32_t)position & ((1u << c.page_shift) - 1u), (uint32_t)position, true};
-                    if (p.page < 0) kv_note(b.errors, TENT_KV_BAD_PAGE);
-                }
+                else p = RowPlace{s, (uint32_t)position, true};
             }
-            to[threadIdx.x] = p;
+            to[lane] = p;
         }
     }
     __syncthreads();
+}
+
+// A row's page as a byte offset, negative if there is none, and its token in it.
+struct PagePlace { int64_t page; uint32_t slot; };
+__device__ __forceinline__ PagePlace page_place(const KvCache& c, const tent_kv_batch& b, const RowPlace& p)
+{
+    return PagePlace{p.live ? kv_page_of(c, b, p.seq, p.position) : -1, p.position & ((1u << c.page_shift) - 1u)};
 }
 
 // Byte offsets inside a page of the eight values of chunk `chunk` of a head.
@@ -176,8 +194,8 @@ __device__ __forceinline__ u32x4 norm_rotate(const tent_kv_append_args& a, u32x4
     return out;
 }
 
-// A workgroup takes one row, or `side` short ones side by side, all heads of it (queries, keys, values), a chunk of eight a lane and
-// kBatch chunks at a time.  The chunks are on their way while the first wave finds where the row belongs, a chain of four loads.
+// A workgroup takes one row, or `side` short ones side by side, or a part of one where there are few; all heads of it (queries, keys, values), a chunk of eight a lane and
+// kBatch chunks at a time.  The chunks are on their way while the first wave finds where the row belongs, a chain of two or more loads.
 // A lane keeps its chunk number over the heads, as the workgroup is a multiple of a head's lanes, and so its cosines and weights.
 constexpr uint32_t kBatch = 4;
 template <class E, int D, int kBits>
@@ -187,7 +205,8 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
     constexpr uint32_t kChunks = D / 8;
     const tent_kv_append_args& a = g.a;
     const uint32_t row0 = blockIdx.x * g.side, n = g.b.n_rows - row0 < g.side ? g.b.n_rows - row0 : g.side;
-    const uint32_t r = g.side == 1 ? 0u : threadIdx.x / g.per_row, x0 = threadIdx.x - r * g.per_row, chunk = x0 % kChunks;
+    const uint32_t r = g.side == 1 ? 0u : threadIdx.x / g.per_row, x0 = threadIdx.x - r * g.per_row + blockIdx.y * blockDim.x, chunk = x0 % kChunks;
+    const uint32_t stride = blockDim.x * gridDim.y;
     const uint64_t row = row0 + r;
     const bool mine = r < n;
     auto load = [&](uint32_t x) -> u32x4 {                               // lanes past the last have nothing
@@ -202,7 +221,7 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
     auto load_batch = [&](uint32_t x) {
 #pragma unroll
         for (uint32_t i = 0; i < kBatch; ++i)
-            if (mine && x + i * blockDim.x < g.per_row) raw[i] = load(x + i * blockDim.x);
+            if (mine && x + i * stride < g.per_row) raw[i] = load(x + i * stride);
     };
     load_batch(x0);
     u32x4 wq = {0, 0, 0, 0}, wk = {0, 0, 0, 0};
@@ -212,6 +231,7 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
     if (!mine) return;
     const RowPlace p = place[r];
     if (!p.live) return;
+    const PagePlace to = page_place(g.c, g.b, p);                        // beside the cosines
     float cs[16] = {};
     if (a.rope) {
         const uint32_t at = a.positions ? (uint32_t)a.positions[row] : p.position;
@@ -234,7 +254,8 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
             }
         }
     }
-    for (uint32_t x = x0, left = kBatch; x < g.per_row; x += blockDim.x, --left) {
+    if (to.page < 0 && x0 == 0) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
+    for (uint32_t x = x0, left = kBatch; x < g.per_row; x += stride, --left) {
         if (left == 0) {
             load_batch(x);
             left = kBatch;
@@ -250,11 +271,11 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
         if (h < a.q_heads) {
             const u32x4 y = norm_rotate<E, D, float>(a, now, chunk, a.q_weight, wq, cs);
             dev_store((uint8_t*)a.q_out + (row * a.q_out_stride + (uint64_t)h * D + chunk * 8) * 2, y);
-        } else if (p.page >= 0) {
+        } else if (to.page >= 0) {
             const bool is_v = h >= a.q_heads + g.c.heads;
             const uint32_t kh = h - a.q_heads - (is_v ? g.c.heads : 0u);
             const u32x4 y = is_v ? now : norm_rotate<E, D, double>(a, now, chunk, a.k_weight, wk, cs);
-            put8<E, D, kBits>((is_v ? g.c.v : g.c.k) + p.page, g.c.page_shift, p.slot, g.c.heads, kh, chunk, y);
+            put8<E, D, kBits>((is_v ? g.c.v : g.c.k) + to.page, g.c.page_shift, to.slot, g.c.heads, kh, chunk, y);
         }
     }
 }
@@ -276,6 +297,13 @@ __global__ void __launch_bounds__(256) read_kernel(const ReadArgs g)
     const uint32_t row0 = blockIdx.x * g.row_tile;
     const uint32_t n = g.b.n_rows - row0 < g.row_tile ? g.b.n_rows - row0 : g.row_tile;
     find_rows(place, g.c, g.b, row0, n);
+    __shared__ PagePlace pages[kMaxRowTile];
+    if (threadIdx.x < n) {
+        const PagePlace at = page_place(g.c, g.b, place[threadIdx.x]);
+        if (at.page < 0 && place[threadIdx.x].live) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
+        pages[threadIdx.x] = at;
+    }
+    __syncthreads();
     const uint32_t one = g.c.heads * kChunks, all = 2 * n * one;         // chunks of K of a row, and of all there is
     for (uint32_t first = threadIdx.x; first < all; first += kBatch * 256) {
         u32x4 value[kBatch];                                             // 4 bits: the codes, the word that holds the scale, and where in it
@@ -285,8 +313,8 @@ __global__ void __launch_bounds__(256) read_kernel(const ReadArgs g)
             const uint32_t i = first + j * 256 < all ? first + j * 256 : first;
             const bool is_v = i >= n * one;
             const uint32_t x = is_v ? i - n * one : i, r = x / one, y = x - r * one, head = y / kChunks, chunk = y % kChunks;
-            const RowPlace p = place[r];
-            where[j] = p.page >= 0 ? 2u : p.live ? 1u : 0u;
+            const PagePlace p = pages[r];
+            where[j] = p.page >= 0 ? 2u : place[r].live ? 1u : 0u;
             const uint8_t* page = (is_v ? g.c.v : g.c.k) + (p.page >= 0 ? p.page : 0);
             const uint32_t slot = p.page >= 0 ? p.slot : 0u;             // of the first page, where there is none
             if constexpr (kBits == 16) {
@@ -388,7 +416,7 @@ int launch_append(AppendArgs g, hipStream_t s)
     g.per_row = (g.a.q_heads + 2 * g.c.heads) * (D / 8);
     g.side = g.per_row >= 256 ? 1 : 256 / g.per_row;                     // at most 16: a row has a key and a value of 64 at least
     const uint32_t turns = (g.per_row + 255) / 256, threads = g.side > 1 ? 256 : (g.per_row + turns * 64 - 1) / (turns * 64) * 64;
-    hipLaunchKernelGGL((append_kernel<E, D, kBits>), dim3((g.b.n_rows + g.side - 1) / g.side), dim3(threads), 0, s, g);
+    hipLaunchKernelGGL((append_kernel<E, D, kBits>), dim3((g.b.n_rows + g.side - 1) / g.side, (uint64_t)g.b.n_rows * turns <= 512 ? turns : 1), dim3(threads), 0, s, g);
     return launched();
 }
 // Rows of a workgroup: as many as its lanes take in one batch, fewer where that leaves compute units without one.

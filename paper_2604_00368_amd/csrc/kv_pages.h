@@ -81,13 +81,13 @@ struct KvSeq {
     bool bad;
 };
 
-TENT_KV_BOTH KvSeq kv_sequence(const tent_kv_batch& b, uint32_t s)
+TENT_KV_BOTH KvSeq kv_sequence(const tent_kv_batch& b, int32_t lo, int32_t hi, int32_t len)
 {
-    const int32_t lo = b.row_start[s], hi = b.row_start[s + 1], len = b.kv_len[s];
     const bool fits = lo >= 0 && hi >= lo && (uint32_t)hi <= b.n_rows && (uint32_t)(hi - lo) <= b.max_rows && len >= 0 &&
                       (uint32_t)len <= b.max_kv;
     return fits ? KvSeq{lo, hi - lo, len, false} : KvSeq{0, 0, 0, true};
 }
+TENT_KV_BOTH KvSeq kv_sequence(const tent_kv_batch& b, uint32_t s) { return kv_sequence(b, b.row_start[s], b.row_start[s + 1], b.kv_len[s]); }
 
 // Byte offset of the page that holds token t (0 <= t < max_kv) of sequence s; negative where the table names none of the pool.
 TENT_KV_BOTH int64_t kv_page_of(const KvCache& c, const tent_kv_batch& b, uint32_t s, uint32_t t)
