@@ -644,7 +644,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             }
         };
         if constexpr (kItems == 1) {
-            load(0);
+            if ((threadIdx.x >= 128u ? v_tile : k_tile) < tiles) load(0);
         } else {
             if (k_tile < tiles)
 #pragma unroll

@@ -261,6 +261,18 @@ def test_attend(kv, shape, dtype, bits):
         assert int(s.batch.errors) == 0
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [3, 40])
+def test_attend_every_count_of_tiles(kv, dim, bits, rows):
+    # one tile of 32 or 64 tokens to nine, the last one not whole: rows of tiles that are not there are not asked for
+    for tokens in ([64 * i - 5 for i in range(1, 10)], [64 * i for i in range(3, 8)], [129, 192, 191, 130]):
+        s = Setup(kv, [min(rows, n) for n in tokens], tokens, BF16, bits, 4, 1, dim, 16, seed=rows)
+        out, lse = kv.attend(s.cache, s.batch, s.q.cuda(), want_lse=True)
+        s.check_attend(out, lse)
+        assert int(s.batch.errors) == 0
+
+
 @pytest.mark.parametrize("dtype,bits,rows,q_heads,heads,dim", [
     (BF16, 4, [1, 1], 8, 2, 128), (FP16, 16, [1, 1], 4, 1, 64), (BF16, 16, [4, 2], 8, 2, 128), (FP16, 4, [60, 3], 4, 1, 128),
     (BF16, 4, [6, 1], 8, 1, 256), (FP16, 4, [8, 8], 8, 1, 64)])
