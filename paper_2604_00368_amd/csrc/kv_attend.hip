@@ -605,8 +605,6 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         const uint8_t* p = g.q + (uint64_t)(q.row0 + row) * g.q_stride + ((uint64_t)q_head * D + upper * 8) * 2;
 #pragma unroll
         for (int k = 0; k < kK; ++k) qf[k] = dev_load<u32x4>(p + k * 32);
-#pragma unroll
-        for (int k = 0; k < kK; ++k) arrived(qf[k]);
     }
     f32x16 o[kDims];
 #pragma unroll
@@ -843,6 +841,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         if constexpr (kBits == 4) store_rows(1, k_odd, tiles, v_odd, 0);
         else store_rows(0, k_even, 0, v_even, there);
         __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kK; ++k) arrived(qf[k]);
         f32x16 s0[2], s1[2];
         scores(k_even, s0, [](int) {});
         big_of = largest(s0);
