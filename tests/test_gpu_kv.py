@@ -157,6 +157,30 @@ def test_append_and_read(kv, bits, dtype, dim, heads, q_heads, page_tokens, norm
     assert int(s.batch.errors) == 0
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+def test_append_and_read_many_sequences_and_many_heads(kv, bits):
+    # more sequences than are looked up in one load, and rows of more heads than a workgroup has in flight at once
+    rows = [i % 4 for i in range(97)]
+    before = [i % 6 for i in range(97)]
+    s = Setup(kv, rows, [r + b for r, b in zip(rows, before)], BF16, bits, 64, 8, 128, 4, seed=8)
+    k, v = (torch.randn(s.n_rows, 8, 128, generator=s.g).to(BF16) for _ in "kv")
+    table = kv.rope_table(16, 128, device="cpu")
+    got = kv.append(s.cache, s.batch, k.cuda(), v.cuda(), q=s.q.cuda(), rope=table.cuda())
+    back_k, back_v = kv.read(s.cache, s.batch)
+    position = np.concatenate([np.arange(b, b + r) for b, r in zip(before, rows)])
+    turn = table.double().numpy()[position]
+    want_k, want_v = R.to_type(R.norm_rotate(k.double().numpy(), None, 0, turn, 128, False), BF16), v.double().numpy()
+    if bits == 4:
+        want_k, want_v = (R.decode4(*R.encode4(y, BF16)) for y in (want_k, want_v))
+    same(back_k, want_k)
+    same(back_v, want_v)
+    want = R.norm_rotate(s.q.double().numpy(), None, 0, turn, 128, False)
+    # two products and a sum in 32 bits, then the type; the terms of a turn do not exceed the pair's size
+    size = np.abs(s.q.double().numpy()).max(-1, keepdims=True) * 2
+    assert (np.abs(got.cpu().double().numpy() - want) <= R.half_step(BF16) * np.abs(want) * 1.01 + 4 * 2.0 ** -24 * size).all()
+    assert int(s.batch.errors) == 0
+
+
 def test_append_in_place_positions_and_rows_outside_the_table(kv):
     s = Setup(kv, [3, 2], [7, 2], dim=64, heads=1, q_heads=2)
     q = torch.randn(5, 2, 64, generator=s.g).to(BF16).cuda()
