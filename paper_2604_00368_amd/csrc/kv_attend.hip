@@ -856,21 +856,29 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
     if (bad_page) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
     if (tiles > 0 && unfinite_lds && !idle) {                            // behind the loop's last barrier
 #pragma unroll 1
-        for (int32_t t = range.lo; t < range.hi; ++t) {
-            const int32_t t0 = range.lo + (t - range.lo) / kWideTile * kWideTile;
-            if (seen_by_all(t0)) continue;
-            const uint32_t in = (uint32_t)g.b.page_table[(uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift)];
-            if (in >= g.c.n_pages || t < see.lo || t >= see.hi) continue;
-            const RowAt<kBits> at = row_at<D, kBits>(g.c, in, (uint32_t)t, head);
+        for (int32_t tile = 0; tile < tiles; ++tile) {
+            // the tiles that store_rows took values from: those that are not whole
+            const int32_t t0 = range.lo + tile * kWideTile;
+            const uint32_t page_no = load_page(tile);
+            const uint64_t held = __ballot(t0 + (int32_t)lane < range.hi && page_no < g.c.n_pages);
+            if (held == ~0ull && seen_by_all(t0)) continue;
+#pragma unroll 1
+            for (int32_t i = 0; i < kWideTile; ++i) {
+                if (!((held >> i) & 1u)) continue;
+                const int32_t t = t0 + i;
+                const uint32_t in = (uint32_t)__builtin_amdgcn_readlane((int)page_no, i);
+                if (t < see.lo || t >= see.hi) continue;
+                const RowAt<kBits> at = row_at<D, kBits>(g.c, in, (uint32_t)t, head);
 #pragma unroll
-            for (int d = 0; d < kDims; ++d)
+                for (int d = 0; d < kDims; ++d)
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    float x[4] = {o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
-                    add_unfinite<E, D, kBits>(x, g.c.v, at, d * 32 + b * 8 + upper * 4);
+                    for (int b = 0; b < 4; ++b) {
+                        float x[4] = {o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+                        add_unfinite<E, D, kBits>(x, g.c.v, at, d * 32 + b * 8 + upper * 4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[d][4 * b + i] = x[i];
-                }
+                        for (int k = 0; k < 4; ++k) o[d][4 * b + k] = x[k];
+                    }
+            }
         }
     }
     sum = sum_over32(sum);

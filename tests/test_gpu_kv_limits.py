@@ -1,0 +1,100 @@
+"""Paged cache operators at the ends of what their types hold: infinities, NaN, the largest and the least values, and what is noted of
+wrong input, on a GPU against their definitions in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import kv_reference as R  # noqa: E402
+from test_gpu_kv import Setup, kv  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+BF16, FP16 = torch.bfloat16, torch.float16
+
+
+# ---- values that are not finite ------------------------------------------------------------------
+class Marks:
+    """Attention of a setup with values that are not finite put into V of some tokens, against the finite setup's outputs."""
+
+    def __init__(self, s, window=0, causal=True, gone=()):
+        self.s, self.window, self.causal = s, window, causal
+        self.clean = s.kv.attend(s.cache, s.batch, s.q.cuda(), window=window, causal=causal)
+        self.want, self.bound = (np.zeros((s.n_rows, s.q_heads, s.dim)) for _ in range(2))
+        for i, n in enumerate(s.rows):
+            at = slice(s.starts[i], s.starts[i] + n)
+            k, v = (np.delete(s.held(p, i), list(gone) if i == 0 else [], 0) for p in (s.k_pool, s.v_pool))
+            assert causal or not window                                  # tokens that are gone shift no window then
+            want, _, mass, size = R.attend(s.q[at].double().numpy(), k, v, 1 / math.sqrt(s.dim), window, causal)
+            self.want[at] = want
+            self.bound[at] = R.attend_bounds(want, mass, size, s.tokens[i], s.dim, s.dtype)[0]
+
+    def sees(self, row, token):
+        """Whether a row of the first sequence sees a token of it."""
+        n, total = self.s.rows[0], self.s.tokens[0]
+        hi = total - n + row + 1 if self.causal else total
+        return token < hi and (not self.window or token >= hi - self.window)
+
+    def check(self, token, head):
+        """Marks one token of the first sequence, for one head, runs, checks every output, and takes the marks back."""
+        s = self.s
+        page, slot = int(s.table[0, token // s.page_tokens]), token % s.page_tokens
+        group = s.q_heads // s.heads
+        heads = slice(head * group, (head + 1) * group)
+        expect = {3: math.inf, 40: -math.inf, 61: math.nan}
+        if s.bits == 16:
+            row = s.v_pool[page, slot, head]
+            old = row.clone()
+            for d, x in expect.items():
+                row[d] = x
+        else:
+            at = s.page_tokens * s.heads * s.dim // 2 + (slot * s.heads + head) * (s.dim // 32)
+            row = s.v_pool[page, at + 1:at + 2]                          # the scale of dims 32 .. 63
+            old = row.clone()
+            row.fill_(255)
+            expect = dict.fromkeys(range(32, 64), math.nan)
+        out = s.kv.attend(s.cache, s.batch, s.q.cuda(), window=self.window, causal=self.causal)
+        row.copy_(old)
+        see = np.zeros(s.n_rows, bool)
+        see[:s.rows[0]] = [self.sees(r, token) for r in range(s.rows[0])]
+        assert see.any()
+        hit = np.zeros(out.shape, bool)
+        for d in expect:
+            hit[see, heads, d] = True
+        got = out.double().cpu().numpy()
+        for d, x in expect.items():
+            part = got[see, heads, d]
+            assert (np.isnan(part) if math.isnan(x) else part == x).all(), (token, head, d, part.ravel()[:4])
+        assert torch.equal(out[torch.from_numpy(~see).cuda()], self.clean[torch.from_numpy(~see).cuda()]), token
+        assert (np.abs(got - self.want) <= self.bound)[~hit].all(), token
+        return int(see.sum())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("rows,heads,dim", [([60, 3], 1, 128), ([140, 3], 2, 64), ([60, 3], 1, 256), ([5, 3], 1, 128)])
+def test_values_that_are_not_finite_in_split_and_windowed_contexts(kv, rows, heads, dim, dtype, bits):
+    # A window makes lines begin at tokens of their own, so that a tile at the end of a split may be half of one that every line sees;
+    # and around the first and the last tokens that lines see.
+    tokens, window = [9001, 4447], 2500
+    s = Setup(kv, rows, tokens, dtype, bits, 4 * heads, heads, dim, 16, seed=dim + heads)
+    assert kv.attend_workspace(s.cache, s.batch, s.q_heads, window=window) > 0
+    m = Marks(s, window)
+    lo = tokens[0] - rows[0] + 1 - window
+    some = 0
+    for token in [lo, lo + 31, lo + rows[0] - 1, *range(lo + 40, lo + 700, 24), 8000, tokens[0] - rows[0], tokens[0] - 1]:
+        some += m.check(token, heads - 1) < rows[0]
+    assert some >= 2                                                     # tokens that some rows see and others do not, too
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("rows,dim", [(70, 128), (3, 128), (40, 256), (100, 64)])
+def test_values_that_are_not_finite_beside_a_bad_page(kv, rows, dim, dtype, bits):
+    s = Setup(kv, [rows, 2], [200, 9], dtype, bits, 2, 1, dim, 16, seed=dim)
+    s.batch.page_table[0, 2] = -5                                        # tokens 32 .. 47 are not seen
+    m = Marks(s, causal=False, gone=range(32, 48))
+    for token in (0, 31, 48, 50, 63, 64, 130, 191, 199):
+        m.check(token, 0)
+    assert int(s.batch.errors) == 2
