@@ -231,8 +231,8 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
            workspace=None, stream=None):
     """Attention of the batch's rows over their sequences: [rows, q_heads, head_dim], and with `want_lse` the logsumexp of the
     scores [rows, q_heads] in float32.  scale: 1 / sqrt(head_dim) unless given; window: a row sees its last `window` tokens;
-    causal=False: every row sees its whole sequence.  workspace: a uint8 tensor of at least attend_workspace bytes to use
-    instead of a new one."""
+    causal=False: every row sees its whole sequence.  workspace: a contiguous uint8 tensor of at least attend_workspace
+    bytes to use instead of a new one."""
     _together(cache, batch)
     n, D, dtype, device = batch.n_rows, cache.head_dim, cache.dtype, cache.device
     heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
@@ -251,7 +251,9 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
     if need.value:
         if workspace is None:
             workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
-        a.workspace, a.workspace_bytes = _on_gpu(workspace, "workspace", torch.uint8).data_ptr(), workspace.numel()
+        elif not _on_gpu(workspace, "workspace", torch.uint8).is_contiguous() or workspace.device != device:
+            raise ValueError("workspace must be contiguous, on the cache's device")
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
     _check(L.tent_kv_attend(cache.ref, batch.ref, ref, _stream(q, stream)), "tent_kv_attend")
     return (out, lse) if want_lse else out
 
