@@ -206,8 +206,8 @@ def pack(src: Cache, dst: Cache, src_pages, dst_pages, errors=None, stream=None)
             raise ValueError(f"{name} must be contiguous int32 [pages] on the caches' device")
     if src_pages.shape != dst_pages.shape or src.device != dst.device:
         raise ValueError("as many pages on one side as on the other, on one device")
-    if errors is not None:
-        _on_gpu(errors, "errors", torch.int32, (1,))
+    if errors is not None and _on_gpu(errors, "errors", torch.int32, (1,)).device != src.device:
+        raise ValueError("errors must be on the caches' device")
     _check(T.lib().tent_kv_pack(src.ref, dst.ref, src_pages.data_ptr(), dst_pages.data_ptr(), src_pages.shape[0],
                                 errors.data_ptr() if errors is not None else None, _stream(src_pages, stream)), "tent_kv_pack")
 

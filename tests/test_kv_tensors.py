@@ -169,3 +169,9 @@ def test_a_workspace_that_is_not_whole_or_elsewhere_is_refused(gpus):
             s.attend(workspace=bad)
         assert not any(e[0] == "attend" for e in gpus.log[n:])
 
+
+def test_errors_of_pack_on_another_gpu_are_refused(gpus):
+    s = Step(gpus)
+    with pytest.raises(ValueError, match="errors"):
+        s.pack(errors=OnGpu(torch.zeros(1, dtype=torch.int32), 1, gpus.log))
+    assert not any(e[0] == "pack" for e in gpus.log)
