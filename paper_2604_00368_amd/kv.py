@@ -2,8 +2,12 @@
 
 The operators behind ``tent_kv_*`` (include/tent.h) with torch tensors for their device memory: ``Cache`` describes the
 pools, ``Batch`` the sequences of a step, and the functions check their tensors, allocate what they return and enqueue on
-the current stream (or `stream`).  Nothing is kept between calls; a ``Cache`` and a ``Batch`` hold their tensors alive and
-can be used for every layer and step that has the same ones.
+the current stream.  Nothing is kept between calls; a ``Cache`` and a ``Batch`` hold their tensors alive and can be used
+for every layer and step that has the same ones.
+
+With `stream` (a torch.cuda.Stream, or a HIP stream's handle) a call allocates and enqueues there instead.  What it takes
+and what it returns is kept from being allocated again before both streams are done with it; that its inputs are ready
+when `stream` gets to it, and its outputs before they are used elsewhere, is for the caller to order.
 
 A cache of 16 bits is two tensors [pages, page_tokens, kv_heads, head_dim] of bfloat16 or float16; one of 4 bits is two
 uint8 tensors [pages, bytes] (``packed_pool``), whose pages hold 32 values to a shared power of two.  Pages are contiguous
@@ -22,11 +26,29 @@ _TYPES = {torch.bfloat16: T.TENT_BF16, torch.float16: T.TENT_FP16}
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
-def _stream(tensor, stream):
-    if stream is not None:
-        return C.c_void_p(int(getattr(stream, "cuda_stream", stream)))
-    index = tensor.device.index
-    return C.c_void_p(_raw_stream(index) if _raw_stream else torch.cuda.current_stream(index).cuda_stream)
+def _stream(device):
+    return C.c_void_p(_raw_stream(device.index) if _raw_stream else torch.cuda.current_stream(device.index).cuda_stream)
+
+
+def _on(device, stream, used, call):
+    """`call()` with `stream` as the current one, so that what it allocates belongs to the stream that uses it.  The allocator is
+    told that `stream` uses the caller's tensors `used`, and that the caller's stream uses what the call has made."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
+    if stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
+    caller = torch.cuda.current_stream(device)
+    if stream == caller:
+        return call()
+    with torch.cuda.stream(stream):
+        for x in used:                                                   # what is no tensor of this device the call refuses
+            if isinstance(x, torch.Tensor) and x.device == device:
+                x.record_stream(stream)
+        result = call()
+    for x in result if isinstance(result, tuple) else (result,):
+        if x is not None and not any(x is y for y in used):
+            x.record_stream(caller)
+    return result
 
 
 def _on_gpu(tensor, name, dtype, shape=None):
@@ -112,6 +134,7 @@ class Cache:
         self.c = T.tent_kv_cache(k.data_ptr(), v.data_ptr(), k.shape[0], stride, self.page_tokens, self.kv_heads, self.head_dim,
                                  _TYPES[dtype], bits, 0)
         self.ref = C.byref(self.c)                                       # made once: calls take it as it is
+        self.tensors = (k, v)
 
     @property
     def page_bytes(self) -> int:
@@ -149,6 +172,7 @@ class Batch:
         self.c = T.tent_kv_batch(page_table.data_ptr(), kv_len.data_ptr(), row_start.data_ptr(), self.errors.data_ptr(), n_seqs, width,
                                  n_rows, max_rows, max_kv, 0)
         self.ref = C.byref(self.c)
+        self.tensors = (page_table, kv_len, row_start, self.errors)
 
 
 def _together(cache, batch):
@@ -166,6 +190,9 @@ def append(cache: Cache, batch: Batch, k, v, q=None, q_weight=None, k_weight=Non
     multiple of 8 values.  q_weight, k_weight: [head_dim], RMS norm over a head.  rope: float32 [positions, rope_dim] as
     rope_table makes it, indexed by `positions` (int32 [rows]) or the row's position in its sequence; rope_pairs turns
     neighbouring dimensions instead of halves.  q_out may be q."""
+    if stream is not None:
+        return _on(cache.device, stream, (*cache.tensors, *batch.tensors, k, v, q, q_weight, k_weight, rope, positions, q_out),
+                   lambda: append(cache, batch, k, v, q, q_weight, k_weight, eps, rope, rope_pairs, positions, q_out))
     _together(cache, batch)
     n, H, D, dtype, device = batch.n_rows, cache.kv_heads, cache.head_dim, cache.dtype, cache.device
     k_stride, v_stride = _rows(k, "k", dtype, n, H, D, device), _rows(v, "v", dtype, n, H, D, device)
@@ -194,13 +221,15 @@ def append(cache: Cache, batch: Batch, k, v, q=None, q_weight=None, k_weight=Non
         if not _on_gpu(positions, "positions", torch.int32, (n,)).is_contiguous() or positions.device != device:
             raise ValueError("positions must be contiguous, on the cache's device")
         a.positions = positions.data_ptr()
-    _check(T.lib().tent_kv_append(cache.ref, batch.ref, C.byref(a), _stream(k, stream)), "tent_kv_append")
+    _check(T.lib().tent_kv_append(cache.ref, batch.ref, C.byref(a), _stream(cache.device)), "tent_kv_append")
     return q_out
 
 
 def pack(src: Cache, dst: Cache, src_pages, dst_pages, errors=None, stream=None):
     """Pack pages src_pages[i] of the 16-bit cache `src` into pages dst_pages[i] of the 4-bit cache `dst` (int32 [pages]).
     `errors`: int32 [1] that page numbers outside the pools are noted in."""
+    if stream is not None:
+        return _on(src.device, stream, (*src.tensors, *dst.tensors, src_pages, dst_pages, errors), lambda: pack(src, dst, src_pages, dst_pages, errors))
     for x, name in ((src_pages, "src_pages"), (dst_pages, "dst_pages")):
         if not _on_gpu(x, name, torch.int32).is_contiguous() or x.dim() != 1 or x.device != src.device:
             raise ValueError(f"{name} must be contiguous int32 [pages] on the caches' device")
@@ -209,11 +238,13 @@ def pack(src: Cache, dst: Cache, src_pages, dst_pages, errors=None, stream=None)
     if errors is not None and _on_gpu(errors, "errors", torch.int32, (1,)).device != src.device:
         raise ValueError("errors must be on the caches' device")
     _check(T.lib().tent_kv_pack(src.ref, dst.ref, src_pages.data_ptr(), dst_pages.data_ptr(), src_pages.shape[0],
-                                errors.data_ptr() if errors is not None else None, _stream(src_pages, stream)), "tent_kv_pack")
+                                errors.data_ptr() if errors is not None else None, _stream(src.device)), "tent_kv_pack")
 
 
 def read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None):
     """The keys and values of the batch's rows as dense tensors [rows, kv_heads, head_dim] of the cache's type."""
+    if stream is not None:
+        return _on(cache.device, stream, (*cache.tensors, *batch.tensors, k_out, v_out), lambda: read(cache, batch, k_out, v_out))
     _together(cache, batch)
     shape = (batch.n_rows, cache.kv_heads, cache.head_dim)
     if k_out is None:
@@ -223,7 +254,7 @@ def read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None):
     stride = _rows(k_out, "k_out", cache.dtype, *shape, cache.device)
     if _rows(v_out, "v_out", cache.dtype, *shape, cache.device) != stride:
         raise ValueError("k_out and v_out must have the same strides")
-    _check(T.lib().tent_kv_read(cache.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), stride, _stream(k_out, stream)), "tent_kv_read")
+    _check(T.lib().tent_kv_read(cache.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), stride, _stream(cache.device)), "tent_kv_read")
     return k_out, v_out
 
 
@@ -233,6 +264,9 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
     scores [rows, q_heads] in float32.  scale: 1 / sqrt(head_dim) unless given; window: a row sees its last `window` tokens;
     causal=False: every row sees its whole sequence.  workspace: a contiguous uint8 tensor of at least attend_workspace
     bytes to use instead of a new one."""
+    if stream is not None:
+        return _on(cache.device, stream, (*cache.tensors, *batch.tensors, q, out, workspace),
+                   lambda: attend(cache, batch, q, scale, window, causal, out, want_lse, workspace))
     _together(cache, batch)
     n, D, dtype, device = batch.n_rows, cache.head_dim, cache.dtype, cache.device
     heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
@@ -254,7 +288,7 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
         elif not _on_gpu(workspace, "workspace", torch.uint8).is_contiguous() or workspace.device != device:
             raise ValueError("workspace must be contiguous, on the cache's device")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(L.tent_kv_attend(cache.ref, batch.ref, ref, _stream(q, stream)), "tent_kv_attend")
+    _check(L.tent_kv_attend(cache.ref, batch.ref, ref, _stream(cache.device)), "tent_kv_attend")
     return (out, lse) if want_lse else out
 
 

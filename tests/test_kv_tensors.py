@@ -175,3 +175,53 @@ def test_errors_of_pack_on_another_gpu_are_refused(gpus):
     with pytest.raises(ValueError, match="errors"):
         s.pack(errors=OnGpu(torch.zeros(1, dtype=torch.int32), 1, gpus.log))
     assert not any(e[0] == "pack" for e in gpus.log)
+
+
+def test_what_a_call_allocates_belongs_to_the_stream_it_is_given(gpus):
+    s = Step(gpus)
+    extra = {"append": (s.k, s.v, s.q, s.weight, s.rope), "pack": (s.pages, s.errors), "read": (), "attend": (s.q,)}
+    made_by = {"append": 1, "pack": 0, "read": 2, "attend": 3}           # attend: the output, the logsumexps and the workspace
+    for given in (Stream(0, 0x55), 0x55):
+        for name, call in s.calls().items():
+            gpus.log.clear()
+            result = call(stream=given)
+            assert (name, 0, 0x55) in gpus.log and gpus.streams[0].cuda_stream == 0
+            made = [e for e in gpus.log if e[0] == "new"]
+            assert len(made) == made_by[name] and all(e[3] == 0x55 for e in made)
+            # the allocator is told of both streams, for what was passed in before the work is enqueued
+            at = gpus.log.index((name, 0, 0x55))
+            before, behind = ({e[1:] for e in part if e[0] == "record"} for part in (gpus.log[:at], gpus.log[at:]))
+            outs = [] if result is None else [result] if isinstance(result, torch.Tensor) else list(result)
+            tensors = (*s.cache.tensors, *(s.packed.tensors if name == "pack" else s.batch.tensors), *extra[name])
+            assert before == {(t.data_ptr(), 0x55) for t in tensors} and behind == {(t.data_ptr(), 0) for t in outs}
+
+
+def test_tensors_that_are_passed_in_are_not_made_anew(gpus):
+    s = Step(gpus)
+    out = s.on(torch.zeros(3, 4, 64, dtype=torch.bfloat16))
+    room = s.on(torch.zeros(4096, dtype=torch.uint8))
+    gpus.log.clear()
+    assert s.append(q_out=out, stream=0x55) is out and s.attend(out=out, workspace=room, stream=0x55)[0] is out
+    k, v = (s.on(torch.zeros(3, 2, 64, dtype=torch.bfloat16)) for _ in "kv")
+    assert s.read(k_out=k, v_out=v, stream=0x55) == (k, v)
+    assert len([e for e in gpus.log if e[0] == "new"]) == 1              # the logsumexps
+    for t in (out, room, k, v):
+        assert ("record", t.data_ptr(), 0x55) in gpus.log and ("record", t.data_ptr(), 0) not in gpus.log
+
+
+def test_the_current_stream_may_be_given(gpus):
+    s = Step(gpus)
+    gpus.log.clear()
+    with gpus.cuda.stream(Stream(0, 0x77)):
+        for call in s.calls().values():
+            call()
+            call(stream=Stream(0, 0x77))
+    assert not [e for e in gpus.log if e[0] == "record"]
+    assert all(e[-1] == 0x77 for e in gpus.log)
+
+
+def test_a_stream_of_another_gpu_is_refused(gpus):
+    for name, call in Step(gpus).calls().items():
+        with pytest.raises(ValueError, match="stream"):
+            call(stream=Stream(1, 0x55))
+        assert not any(e[0] == name for e in gpus.log)
