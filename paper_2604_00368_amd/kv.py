@@ -24,6 +24,7 @@ from . import binding as T
 
 _TYPES = {torch.bfloat16: T.TENT_BF16, torch.float16: T.TENT_FP16}
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
 def _stream(device):
@@ -31,14 +32,18 @@ def _stream(device):
 
 
 def _on(device, stream, used, call):
-    """`call()` with `stream` as the current one, so that what it allocates belongs to the stream that uses it.  The allocator is
-    told that `stream` uses the caller's tensors `used`, and that the caller's stream uses what the call has made."""
+    """`call()` with the tensors' device current, as the library launches on that, and with `stream`, if one is given, as the
+    current stream, so that what it allocates belongs to the stream that uses it.  The allocator is told that `stream` uses the
+    caller's tensors `used`, and that the caller's stream uses what the call has made."""
+    if stream is None:
+        with torch.cuda.device(device):
+            return call()
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
     if stream.device != device:
         raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
     caller = torch.cuda.current_stream(device)
-    if stream == caller:
+    if stream == caller and _current_device() == device.index:
         return call()
     with torch.cuda.stream(stream):
         for x in used:                                                   # what is no tensor of this device the call refuses
@@ -190,7 +195,7 @@ def append(cache: Cache, batch: Batch, k, v, q=None, q_weight=None, k_weight=Non
     multiple of 8 values.  q_weight, k_weight: [head_dim], RMS norm over a head.  rope: float32 [positions, rope_dim] as
     rope_table makes it, indexed by `positions` (int32 [rows]) or the row's position in its sequence; rope_pairs turns
     neighbouring dimensions instead of halves.  q_out may be q."""
-    if stream is not None:
+    if stream is not None or cache.device.index != _current_device():
         return _on(cache.device, stream, (*cache.tensors, *batch.tensors, k, v, q, q_weight, k_weight, rope, positions, q_out),
                    lambda: append(cache, batch, k, v, q, q_weight, k_weight, eps, rope, rope_pairs, positions, q_out))
     _together(cache, batch)
@@ -228,7 +233,7 @@ def append(cache: Cache, batch: Batch, k, v, q=None, q_weight=None, k_weight=Non
 def pack(src: Cache, dst: Cache, src_pages, dst_pages, errors=None, stream=None):
     """Pack pages src_pages[i] of the 16-bit cache `src` into pages dst_pages[i] of the 4-bit cache `dst` (int32 [pages]).
     `errors`: int32 [1] that page numbers outside the pools are noted in."""
-    if stream is not None:
+    if stream is not None or src.device.index != _current_device():
         return _on(src.device, stream, (*src.tensors, *dst.tensors, src_pages, dst_pages, errors), lambda: pack(src, dst, src_pages, dst_pages, errors))
     for x, name in ((src_pages, "src_pages"), (dst_pages, "dst_pages")):
         if not _on_gpu(x, name, torch.int32).is_contiguous() or x.dim() != 1 or x.device != src.device:
@@ -243,7 +248,7 @@ def pack(src: Cache, dst: Cache, src_pages, dst_pages, errors=None, stream=None)
 
 def read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None):
     """The keys and values of the batch's rows as dense tensors [rows, kv_heads, head_dim] of the cache's type."""
-    if stream is not None:
+    if stream is not None or cache.device.index != _current_device():
         return _on(cache.device, stream, (*cache.tensors, *batch.tensors, k_out, v_out), lambda: read(cache, batch, k_out, v_out))
     _together(cache, batch)
     shape = (batch.n_rows, cache.kv_heads, cache.head_dim)
@@ -264,7 +269,7 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
     scores [rows, q_heads] in float32.  scale: 1 / sqrt(head_dim) unless given; window: a row sees its last `window` tokens;
     causal=False: every row sees its whole sequence.  workspace: a contiguous uint8 tensor of at least attend_workspace
     bytes to use instead of a new one."""
-    if stream is not None:
+    if stream is not None or cache.device.index != _current_device():
         return _on(cache.device, stream, (*cache.tensors, *batch.tensors, q, out, workspace),
                    lambda: attend(cache, batch, q, scale, window, causal, out, want_lse, workspace))
     _together(cache, batch)

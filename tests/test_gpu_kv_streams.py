@@ -47,3 +47,17 @@ def test_a_step_on_a_stream_of_the_callers(kv):
         stream.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert int(s.batch.errors) == 0
+
+
+def test_the_default_stream_by_its_handle(kv):
+    s = Setup(kv, [2, 1], [5000, 7], BF16, 16, 4, 2, 64, 16, seed=5)
+    q = s.q.cuda()
+    want = kv.attend(s.cache, s.batch, q)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for given in (0, torch.cuda.default_stream()):
+            out = kv.attend(s.cache, s.batch, q, stream=given)
+            torch.cuda.default_stream().synchronize()
+            assert torch.equal(out, want)
+        assert torch.cuda.current_stream() == side

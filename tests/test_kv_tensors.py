@@ -148,6 +148,7 @@ def gpus(monkeypatch):
     g = Gpus()
     monkeypatch.setattr(kv, "torch", g)
     monkeypatch.setattr(kv, "_raw_stream", lambda index: g.streams[index].cuda_stream)
+    monkeypatch.setattr(kv, "_current_device", lambda: g.at, raising=False)
     monkeypatch.setattr(T, "lib", lambda: g)
     return g
 
@@ -225,3 +226,17 @@ def test_a_stream_of_another_gpu_is_refused(gpus):
         with pytest.raises(ValueError, match="stream"):
             call(stream=Stream(1, 0x55))
         assert not any(e[0] == name for e in gpus.log)
+
+
+@pytest.mark.parametrize("index", [0, 1])
+def test_calls_go_to_the_device_of_their_tensors(gpus, index):
+    s = Step(gpus, index)
+    gpus.streams = {0: Stream(0, 0x10), 1: Stream(1, 0x20)}
+    for at in (0, 1):
+        gpus.at = at
+        for name, call in s.calls().items():
+            for given, handle in ((None, (0x10, 0x20)[index]), (Stream(index, 0x55), 0x55), (gpus.streams[index], (0x10, 0x20)[index]), (0x66, 0x66)):
+                gpus.log.clear()
+                call(stream=given)
+                assert (name, index, handle) in gpus.log
+                assert gpus.at == at and [gpus.streams[i].cuda_stream for i in (0, 1)] == [0x10, 0x20]
