@@ -630,8 +630,9 @@ int tent_kv_attend_workspace(const tent_kv_cache *cache, const tent_kv_batch *ba
 /* Attention of every row over its sequence: out = sum_t softmax_t(scale q . k_t) v_t over the tokens t that the row sees,
  * its own and those before it (TENT_KV_ATTEND_ALL: all kv_len), within the window; query head h reads head
  * h / (q_heads / kv_heads).  lse is the natural logarithm of the softmax's sum with its maximum (the logsumexp of the
- * scores).  A row that sees no token, or only scores of minus infinity, gives zeros and lse minus infinity.  Tokens that a
- * row does not see have no influence on it, whatever their values.  Scores and sums are 32 bits, weights are rounded to the
+ * scores).  A row that sees no token, or only scores of minus infinity, gives zeros and lse minus infinity; one with a score of
+ * plus infinity gives NaN and lse plus infinity, and one with a score that is NaN gives NaN for both.  Tokens that a row does
+ * not see have no influence on it, whatever their values.  Scores and sums are 32 bits, weights are rounded to the
  * 16-bit type (to nearest) before they multiply the values. */
 int tent_kv_attend(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_attend_args *args, void *stream);
 

@@ -29,6 +29,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The maximum that weights are taken against may lag behind the true one by a factor of 2^8: sums and products are in 32 bits
 // and lose nothing by it, and most tiles then need no rescaling.
 constexpr float kLag = 8.f;
+// The most that weights are taken against.  Scores of plus infinity stay infinite weights against it, and so the sum and the
+// logsumexp are infinite and the outputs NaN; against infinity they would be NaN, and not told from a score that is.
+constexpr float kMost = 3.402823466e38f;
 constexpr int32_t kStep = 32;          // splits and the tokens that a workgroup begins with are multiples of it
 
 struct AttendArgs {
@@ -441,7 +444,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
             float big = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
             big = max_over32(max_over16(big)) * g.to_log2;
             if (__any(big > top[rt] + kLag)) {
-                const float now = fmaxf(top[rt], big), f = rescale(top[rt], now);
+                const float now = fminf(fmaxf(top[rt], big), kMost), f = rescale(top[rt], now);
                 top[rt] = now;
                 sum[rt] = sum[rt] * f * f;
 #pragma unroll
@@ -763,7 +766,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             }
             const float big = max_over32(masked ? largest(s) : big_of) * g.to_log2;
             if (__any(big > top + kLag)) {
-                const float now = fmaxf(top, big), f = rescale(top, now);
+                const float now = fminf(fmaxf(top, big), kMost), f = rescale(top, now);
                 top = now;
                 sum = sum * f * f;
 #pragma unroll

@@ -98,3 +98,25 @@ def test_values_that_are_not_finite_beside_a_bad_page(kv, rows, dim, dtype, bits
     for token in (0, 31, 48, 50, 63, 64, 130, 191, 199):
         m.check(token, 0)
     assert int(s.batch.errors) == 2
+
+
+# ---- scores that are not finite ------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("rows,tokens", [([4, 1], [70, 40]), ([100, 30], [150, 40]), ([4, 1], [9001, 4447]), ([100, 2], [9001, 4447])])
+def test_logsumexp_of_scores_that_are_not_finite(kv, rows, tokens, dtype):
+    s = Setup(kv, rows, tokens, dtype, 16, 2, 1, 128, 16, seed=7)
+    first = s.starts[1]
+    q = s.q.cuda()
+    q[:, :, 0] = 0.5
+    q[first - 1, 0, 0], q[first - 1, 1, 0] = -0.5, math.nan
+    page, slot = int(s.table[0, 20 // 16]), 20 % 16
+    s.k_pool[page, slot, 0, 0] = math.inf                                # token 20 of the first sequence: a score of infinity
+    out, lse = kv.attend(s.cache, s.batch, q, want_lse=True)
+    assert bool((lse[:first - 1] == math.inf).all()) and bool(out[:first - 1].isnan().all())
+    assert bool(lse[first - 1, 0].isfinite()) and bool(out[first - 1, 0].isfinite().all())     # minus infinity: not seen
+    assert bool(lse[first - 1, 1].isnan()) and bool(out[first - 1, 1].isnan().all())
+    s.q = q.cpu()
+    s.check_attend(out, lse, skip=(0,))
+    s.k_pool[page, slot, 0, 1] = math.nan                                # and now none
+    _, lse = kv.attend(s.cache, s.batch, q, want_lse=True)
+    assert bool(lse[:first].isnan().all())
