@@ -542,6 +542,8 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
             if (seg == 0) dev_store(g.part_ml + at * 2, f32x2{best, total});
         } else {
             const float scale = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+            for (uint32_t i = 0; i < kSeg; ++i) y[i] = total == 0.f ? 0.f : y[i];    // no weight: zeros, whatever the values
             uint8_t* to = g.out + out_row * g.out_stride + ((uint64_t)q_head * D + seg * kSeg) * 2;
 #pragma unroll
             for (uint32_t i = 0; i < kSeg / 4; ++i) dev_store(to + i * 8, u32x2{E::pack2(y[4 * i] * scale, y[4 * i + 1] * scale), E::pack2(y[4 * i + 2] * scale, y[4 * i + 3] * scale)});
@@ -897,6 +899,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             for (int b = 0; b < 4; ++b) dev_store(g.part_o + at * D + d * 32 + b * 8 + upper * 4, f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]});
     } else {
         const float scale = sum == 0.f ? 0.f : 1.f / sum;
+        if (sum == 0.f) {                                                // no weight: zeros, whatever the values
+#pragma unroll
+            for (int d = 0; d < kDims; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        }
         uint8_t* to = g.out + out_row * g.out_stride + ((uint64_t)q_head * D + upper * 4) * 2;
 #pragma unroll
         for (int d = 0; d < kDims; ++d)

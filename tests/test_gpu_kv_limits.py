@@ -120,3 +120,18 @@ def test_logsumexp_of_scores_that_are_not_finite(kv, rows, tokens, dtype):
     s.k_pool[page, slot, 0, 1] = math.nan                                # and now none
     _, lse = kv.attend(s.cache, s.batch, q, want_lse=True)
     assert bool(lse[:first].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("rows,tokens", [([4, 1], [70, 40]), ([100, 30], [150, 40]), ([4, 1], [9001, 4447]), ([100, 2], [9001, 4447])])
+def test_rows_of_scores_of_minus_infinity_are_zeros_whatever_the_values(kv, rows, tokens, causal, dtype):
+    s = Setup(kv, rows, tokens, dtype, 16, 2, 1, 64, 16, seed=7)
+    q = s.q.cuda()
+    q[:s.starts[1], :, 0] = 1.0
+    pages = s.table[0, :-(-tokens[0] // 16)].long().cuda()
+    s.k_pool[pages, :, :, 0] = -math.inf
+    s.v_pool[pages, :, :, 5], s.v_pool[pages, :, :, 6] = math.inf, math.nan
+    out, lse = kv.attend(s.cache, s.batch, q, causal=causal, want_lse=True)
+    assert not out[:s.starts[1]].any() and bool((lse[:s.starts[1]] == -math.inf).all())
+    s.check_attend(out, lse, causal=causal, skip=(0,))
