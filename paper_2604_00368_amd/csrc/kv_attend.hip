@@ -32,6 +32,8 @@ constexpr float kLag = 8.f;
 // The most that weights are taken against.  Scores of plus infinity stay infinite weights against it, and so the sum and the
 // logsumexp are infinite and the outputs NaN; against infinity they would be NaN, and not told from a score that is.
 constexpr float kMost = 3.402823466e38f;
+// Joined parts are added up as 2^-11 each, and there are at most 1536: sums of finite parts are finite.
+constexpr float kPart = 0x1p-11f;
 constexpr int32_t kStep = 32;          // splits and the tokens that a workgroup begins with are multiples of it
 
 struct AttendArgs {
@@ -48,6 +50,15 @@ struct AttendArgs {
     uint32_t n_splits, split_tokens;   // tokens of a split: a multiple of 128
     uint32_t line_tiles;               // workgroups over the lines of a sequence and head
 };
+
+// A kernel's arguments, read anew: what hardly any call comes to should not keep them in registers all along.
+__device__ __forceinline__ const AttendArgs& args_again()
+{
+    typedef const __attribute__((address_space(4))) AttendArgs* ArgsAt;
+    ArgsAt at = (ArgsAt)__builtin_amdgcn_kernarg_segment_ptr();
+    __asm__ volatile("" : "+s"(at));
+    return *(const AttendArgs*)at;
+}
 
 // ---- what both kernels share ---------------------------------------------------------------------
 // A sequence's splits begin at the first token that its first row sees, rounded down to a whole step.
@@ -188,6 +199,113 @@ __device__ __forceinline__ void add_unfinite(float* o, const uint8_t* pool, cons
 __device__ __forceinline__ float lse_of(float top, float sum, float shift)
 {
     return sum > 0.f ? kLn2 * (top - shift + __builtin_amdgcn_logf(sum)) : sum == 0.f ? -INFINITY : sum;
+}
+
+// One line by one wave, in plain steps: for the lines whose sums pass what 32 bits hold, which outputs of bfloat16 values do not (up
+// to 2^128 both, and a sum takes weights of 2^16 and more).  Here a weight is divided by the sum of all weights before it multiplies a
+// value.  A lane takes one of 64 tokens for its score, then D / 64 dimensions of all 64.  Scores are finite or minus infinity here;
+// values that are not finite are added as they are, whatever their weight.  `line_top`, `line_sum`: what the loops below have
+// found, which stand for the logsumexp and for a part.
+template <class E, int D, int kBits>
+__device__ __forceinline__ void plain_line(const AttendArgs& g, const KvSeq& seq_of, uint32_t seq, uint32_t head, uint32_t split, int32_t line, const Range& range,
+                                           float line_top, float line_sum)
+{
+    const int32_t row = line / (int32_t)g.group, h = line - row * (int32_t)g.group;
+    const uint32_t q_head = head * g.group + (uint32_t)h;
+    const uint64_t out_row = (uint64_t)(seq_of.row0 + row);
+    const KvSpan see = kv_span(row, seq_of.rows, seq_of.len, g.window, g.all);
+    const int32_t lo = see.lo > range.lo ? see.lo : range.lo, hi = see.hi < range.hi ? see.hi : range.hi;
+    const uint8_t* const q = g.q + out_row * g.q_stride + (uint64_t)q_head * D * 2;
+    float top = -INFINITY, sum = 0.f, y[D / 64];
+    constexpr int kPer = D / 64;
+    const uint32_t lane = threadIdx.x & 63u;
+    const int32_t* const table = g.b.page_table + (uint64_t)seq * g.b.table_stride;
+    RowAt<kBits> at;                                                     // of this lane's token
+    bool there;
+    auto score = [&](int32_t t0) -> float {                              // times log2(e)
+        const int32_t t = t0 + (int32_t)lane < hi ? t0 + (int32_t)lane : hi - 1;
+        const uint32_t page = dev_load<uint32_t>(table + ((uint32_t)t >> g.c.page_shift));
+        there = t0 + (int32_t)lane < hi && page < g.c.n_pages;
+        at = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
+        float s = 0.f;
+#pragma unroll 1
+        for (uint32_t c = 0; c < D / 8; ++c) {
+            const u32x4 a = dev_load<u32x4>(q + c * 16);
+            u32x4 k;
+            if constexpr (kBits == 16) k = dev_load<u32x4>(g.c.k + at.row + c * 16);
+            else k = decode8<E>(dev_load<uint32_t>(g.c.k + at.row + c * 4), scale_of(dev_load<uint8_t>(g.c.k + at.scale + c / 4)));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s = fmaf(E::to_float(a[i] & 0xFFFFu), E::to_float(k[i] & 0xFFFFu), s);
+                s = fmaf(E::to_float(a[i] >> 16), E::to_float(k[i] >> 16), s);
+            }
+        }
+        return there ? s * g.to_log2 : -INFINITY;
+    };
+#pragma unroll 1
+    for (int32_t t0 = lo; t0 < hi; t0 += 64) {
+        const float x = score(t0);
+        float now = x;
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) now = fmaxf(now, __shfl_xor(now, k, 64));
+        now = fmaxf(now, top);
+        float add = __builtin_amdgcn_exp2f(x - (now == -INFINITY ? 0.f : now));
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) add += __shfl_xor(add, k, 64);
+        const float f = rescale(top, now);
+        sum = sum * f * f + add;
+        top = now;
+    }
+    const float share = 1.f / sum;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) y[k] = 0.f;
+#pragma unroll 1
+    for (int32_t t0 = lo; t0 < hi; t0 += 64) {
+        const float w = __builtin_amdgcn_exp2f(score(t0) - top) * share;
+        const uint64_t held = __ballot(there);
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i) {
+            if (!((held >> i) & 1u)) continue;
+            const float wi = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), i));
+            const uint64_t row = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at.row >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at.row, i);
+            const uint8_t* p = g.c.v + row;
+            uint32_t v[(kPer + 1) / 2];                                  // dims kPer * lane ..
+            if constexpr (kBits == 16) {
+                if constexpr (kPer == 1) v[0] = dev_load<uint16_t>(p + lane * 2);
+                else
+#pragma unroll
+                    for (int k = 0; k < kPer / 2; ++k) v[k] = dev_load<uint32_t>(p + (lane * kPer + 2 * k) * 2);
+            } else {
+                const uint64_t scales = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at.scale >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at.scale, i);
+                const float scale = scale_of(dev_load<uint8_t>(g.c.v + scales + lane * kPer / 32));
+                if constexpr (kPer == 1) v[0] = E::template decode2<0>(dev_load<uint8_t>(p + lane / 2), scale) >> (16 * (lane & 1u)) & 0xFFFFu;
+                else
+#pragma unroll
+                    for (int k = 0; k < kPer / 2; ++k) v[k] = E::template decode2<0>(dev_load<uint8_t>(p + lane * (kPer / 2) + k), scale);
+            }
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                const float x = E::to_float(v[k / 2] >> (16 * (k & 1)) & 0xFFFFu);
+                y[k] = fabsf(x) < INFINITY ? fmaf(wi, x, y[k]) : y[k] + x;
+            }
+        }
+    }
+    if (g.part_o) {                                                      // the sum brought to 1 at most, by a power of two whose root is one
+        const uint64_t at = (out_row * g.q_heads + q_head) * g.n_splits + split;
+        const int power = ((int)(__float_as_uint(line_sum) >> 23) - 127 + 2) & ~1;
+        line_sum = ldexpf(line_sum, -power);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) dev_store(g.part_o + at * D + lane * kPer + k, y[k] * line_sum);
+        if (lane == 0) dev_store(g.part_ml + at * 2, f32x2{line_top + (float)power, line_sum});
+        return;
+    }
+    uint8_t* const to = g.out + out_row * g.out_stride + (uint64_t)q_head * D * 2;
+    if constexpr (kPer == 1) {
+        dev_store(to + lane * 2, (uint16_t)E::pack2(y[0], 0.f));
+    } else {
+#pragma unroll
+        for (int k = 0; k < kPer; k += 2) dev_store(to + (lane * kPer + k) * 2, E::pack2(y[k], y[k + 1]));
+    }
 }
 
 // ---- few lines -----------------------------------------------------------------------------------
@@ -504,6 +622,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
     }
     float* const o_lds = (float*)lds;
     constexpr uint32_t kRow = D + 4, kSeg = D / 16;
+    uint64_t large = 0;                                                  // lines of this wave whose sums passed 32 bits
 #pragma unroll
     for (int rt = 0; rt < kLineTiles; ++rt) {
         __syncthreads();
@@ -516,7 +635,6 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
         __syncthreads();
         const uint32_t in_tile = threadIdx.x >> 4, seg = threadIdx.x & 15u;
         const int32_t line = rt * 16 + (int32_t)in_tile;
-        if (line >= lines) continue;
         float best = line_top[0][line], total = 0.f;
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) best = fmaxf(best, line_top[w][line]);
@@ -532,11 +650,22 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) y[i] += o_lds[(w * 16 + in_tile) * kRow + seg * kSeg + i];
         }
+        if constexpr (E::kLarge) {                                       // a line is in 16 lanes side by side, four of them in a wave
+            float x = 0.f;
+#pragma unroll
+            for (uint32_t i = 0; i < kSeg; ++i) x = fmaf(y[i], 0.f, x);
+            const uint64_t here = __ballot(line < lines && total > 0.f && total < INFINITY && !(x == 0.f));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) large |= (uint64_t)((here >> (16 * i) & 0xFFFFu) != 0) << (rt * 16 + 4 * wave + i);
+        }
+        if (line >= lines) continue;
+        const bool stands = !(large >> line & 1u);                       // else plain_line stores it
         const int32_t row = line / (int32_t)g.group, h = line - row * (int32_t)g.group;
         const uint32_t q_head = head * g.group + (uint32_t)h;
         const uint64_t out_row = (uint64_t)(q.row0 + row);
         if (g.part_o) {
             const uint64_t at = (out_row * g.q_heads + q_head) * g.n_splits + split;
+            if (!stands) continue;
 #pragma unroll
             for (uint32_t i = 0; i < kSeg / 4; ++i) dev_store(g.part_o + at * D + seg * kSeg + i * 4, f32x4{y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]});
             if (seg == 0) dev_store(g.part_ml + at * 2, f32x2{best, total});
@@ -545,9 +674,28 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
 #pragma unroll
             for (uint32_t i = 0; i < kSeg; ++i) y[i] = total == 0.f ? 0.f : y[i];    // no weight: zeros, whatever the values
             uint8_t* to = g.out + out_row * g.out_stride + ((uint64_t)q_head * D + seg * kSeg) * 2;
+            if (stands)
 #pragma unroll
-            for (uint32_t i = 0; i < kSeg / 4; ++i) dev_store(to + i * 8, u32x2{E::pack2(y[4 * i] * scale, y[4 * i + 1] * scale), E::pack2(y[4 * i + 2] * scale, y[4 * i + 3] * scale)});
+                for (uint32_t i = 0; i < kSeg / 4; ++i) dev_store(to + i * 8, u32x2{E::pack2(y[4 * i] * scale, y[4 * i + 1] * scale), E::pack2(y[4 * i + 2] * scale, y[4 * i + 3] * scale)});
             if (g.lse && seg == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(best, total, E::kWeightShift);
+        }
+    }
+    if constexpr (E::kLarge) {
+        if (large) {
+            const AttendArgs& a = args_again();
+#pragma unroll 1
+            for (; large; large &= large - 1) {
+                const int32_t line = __builtin_ctzll(large);
+                float best = line_top[0][line], total = 0.f;
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) best = fmaxf(best, line_top[w][line]);
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const float r = rescale(line_top[w][line], best);
+                    total += line_sum[w][line] * r * r;
+                }
+                plain_line<E, D, kBits>(a, q, seq, head, split, line, range, best, total);
+            }
         }
     }
 }
@@ -555,6 +703,21 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
 // ---- many lines ----------------------------------------------------------------------------------
 constexpr int kWideTile = 64;          // tokens of a step
 constexpr int kWideLines = 128;        // 32 a wave
+
+// What a workgroup is for.  Heads vary fastest, so a head stays on an XCD where there are eight, and its tokens in that XCD's cache;
+// the rows that see the most tokens come first.
+struct WideUnit { uint32_t head, seq, split, line_tile; };
+__device__ __forceinline__ WideUnit wide_unit(const AttendArgs& g, uint32_t block)
+{
+    WideUnit u;
+    u.head = block % g.c.heads;
+    block /= g.c.heads;
+    u.seq = block % g.b.n_seqs;
+    block /= g.b.n_seqs;
+    u.split = block % g.n_splits;
+    u.line_tile = g.line_tiles - 1 - block / g.n_splits;
+    return u;
+}
 
 // 32 lines a wave, so that scores, outputs and queries of two waves fit a SIMD's registers (one wave for 256 dimensions): a wave's
 // vector work can run beside the other's products as well as beside its own.  Four waves share a tile because LDS, read by every wave
@@ -575,14 +738,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
 
     const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t m = lane & 31u, upper = lane >> 5;
-    // Heads vary fastest, so a head stays on an XCD where there are eight, and its tokens in that XCD's cache; the rows that see
-    // the most tokens come first.
-    uint32_t block = blockIdx.x;
-    const uint32_t head = block % g.c.heads;
-    block /= g.c.heads;
-    const uint32_t seq = block % g.b.n_seqs;
-    block /= g.b.n_seqs;
-    const uint32_t split = block % g.n_splits, line_tile = g.line_tiles - 1 - block / g.n_splits;
+    const WideUnit unit = wide_unit(g, blockIdx.x);
+    const uint32_t head = unit.head, seq = unit.seq, split = unit.split, line_tile = unit.line_tile;
     const KvSeq q = kv_sequence(g.b, seq);
     if (q.bad && threadIdx.x == 0 && split == 0 && head == 0 && line_tile == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
     const int32_t lines = q.rows * (int32_t)g.group, line0 = (int32_t)line_tile * kWideLines;
@@ -887,10 +1044,36 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         }
     }
     sum = sum_over32(sum);
-    if (!mine) return;
+    bool large = false;                                                  // this line's sums passed 32 bits
+    if constexpr (E::kLarge) {
+        float x = 0.f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x = fmaf(o[d][i], 0.f, x);
+        x = sum_over32(x);
+        large = mine && sum > 0.f && sum < INFINITY && !(x == 0.f);
+        uint32_t lines_left = (uint32_t)__ballot(large);                 // the lower lanes: a line each
+        if (lines_left) {
+            const AttendArgs& a = args_again();
+            const WideUnit u = wide_unit(a, blockIdx.x);
+            const KvSeq q = kv_sequence(a.b, u.seq);
+            const int32_t line0 = (int32_t)u.line_tile * kWideLines, lines = q.rows * (int32_t)a.group;
+            const Range range = token_range(a, q, line0, line0 + kWideLines < lines ? line0 + kWideLines - 1 : lines - 1, u.split);
+#pragma unroll 1
+            for (; lines_left; lines_left &= lines_left - 1) {
+                const int i = __builtin_ctz(lines_left);
+                plain_line<E, D, kBits>(a, q, u.seq, u.head, u.split, line0 + (int32_t)wave * 32 + i, range,
+                                        __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), i)),
+                                        __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(sum), i)));
+            }
+        }
+    }
+    if (!mine) return;                                                   // plain_line has stored lines that are large
     const uint64_t out_row = (uint64_t)(q.row0 + row);
     if (g.part_o) {
         const uint64_t at = (out_row * g.q_heads + q_head) * g.n_splits + split;
+        if (large) return;
         if (upper == 0) dev_store(g.part_ml + at * 2, f32x2{top, sum});
         if (sum == 0.f) return;                                          // join_kernel does not read it
 #pragma unroll
@@ -906,11 +1089,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
                 for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         }
         uint8_t* to = g.out + out_row * g.out_stride + ((uint64_t)q_head * D + upper * 4) * 2;
+        if (!large)
 #pragma unroll
-        for (int d = 0; d < kDims; ++d)
+            for (int d = 0; d < kDims; ++d)
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                dev_store(to + (d * 32 + b * 8) * 2, u32x2{E::pack2(o[d][4 * b] * scale, o[d][4 * b + 1] * scale), E::pack2(o[d][4 * b + 2] * scale, o[d][4 * b + 3] * scale)});
+                for (int b = 0; b < 4; ++b)
+                    dev_store(to + (d * 32 + b * 8) * 2, u32x2{E::pack2(o[d][4 * b] * scale, o[d][4 * b + 1] * scale), E::pack2(o[d][4 * b + 2] * scale, o[d][4 * b + 3] * scale)});
         if (g.lse && upper == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, sum, E::kWeightShift);
     }
 }
@@ -951,9 +1135,9 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs g)
         for (int a = 0; a < kAhead; ++a) {
             if (i + a * kTurn >= n || ml[a][1] == 0.f) continue;         // an empty part has a sum of 0 and no output
             const float f = rescale(ml[a][0], top);
-            sum += ml[a][1] * f * f;
+            sum += ml[a][1] * f * (f * kPart);
 #pragma unroll
-            for (int k = 0; k < kPer; ++k) y[k] += part[a][k] * f * f;
+            for (int k = 0; k < kPer; ++k) y[k] += part[a][k] * f * (f * kPart);
         }
     }
     uint8_t* const to = g.out + out_row * g.out_stride + (uint64_t)q_head * D * 2;
@@ -965,7 +1149,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs g)
 #pragma unroll
             for (int k = 0; k < kPer; k += 2) dev_store(to + (lane * kPer + k) * 2, E::pack2(y[k] * scale, y[k + 1] * scale));
         }
-        if (g.lse && lane == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, sum, E::kWeightShift);
+        if (g.lse && lane == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, sum * (1.f / kPart), E::kWeightShift);
     } else {
 #pragma unroll
         for (int k = 0; k < kPer; ++k) o_lds[wave][lane * kPer + k] = y[k];
@@ -981,7 +1165,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs g)
         }
         const float scale = total == 0.f ? 0.f : 1.f / total;
         dev_store(to + threadIdx.x * 4, E::pack2(a * scale, b * scale));
-        if (g.lse && threadIdx.x == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, total, E::kWeightShift);
+        if (g.lse && threadIdx.x == 0) g.lse[out_row * g.q_heads + q_head] = lse_of(top, total * (1.f / kPart), E::kWeightShift);
     }
 }
 

@@ -135,3 +135,36 @@ def test_rows_of_scores_of_minus_infinity_are_zeros_whatever_the_values(kv, rows
     out, lse = kv.attend(s.cache, s.batch, q, causal=causal, want_lse=True)
     assert not out[:s.starts[1]].any() and bool((lse[:s.starts[1]] == -math.inf).all())
     s.check_attend(out, lse, causal=causal, skip=(0,))
+
+
+# ---- the ends of the type's range ----------------------------------------------------------------
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("power", [125, -128])
+@pytest.mark.parametrize("rows,tokens,q_heads,heads,dim", [
+    ([1], [1], 2, 1, 128), ([1, 5], [300, 40], 8, 2, 64), ([3, 2], [65, 700], 8, 1, 256), ([100, 33], [700, 33], 4, 2, 128), ([50, 40], [300, 40], 4, 1, 256),
+    ([1, 1], [9001, 4447], 8, 2, 128), ([60, 3], [9001, 4447], 4, 1, 64), ([60, 3], [9001, 4447], 4, 1, 128)])
+def test_attend_values_near_the_ends_of_bfloat16(kv, rows, tokens, q_heads, heads, dim, power, bits):
+    # weights times values, and their sums, pass what 32 bits hold long before the outputs do
+    s = Setup(kv, rows, tokens, BF16, bits, q_heads, heads, dim, 16, seed=dim)
+    s.v16 = (s.v16.double().clamp(-4, 4) * 2.0 ** power).to(BF16)
+    s.v16[..., ::7] = (s.v16[..., ::7].double() * 2.0 ** (-power)).to(BF16)      # ordinary values beside them
+    s.v_pool = s.pool(s.v16)
+    s.cache = s.make_cache(s.k_pool, s.v_pool)
+    out, lse = kv.attend(s.cache, s.batch, s.q.cuda(), want_lse=True)
+    assert bool(out.isfinite().all())
+    s.check_attend(out, lse)
+
+
+@pytest.mark.parametrize("rows,tokens", [([4, 2], [300, 40]), ([100, 30], [300, 40]), ([60, 2], [9001, 4447]), ([4, 2], [9001, 4447])])
+def test_rows_that_do_not_see_large_values_do_not_change(kv, rows, tokens):
+    s = Setup(kv, rows, tokens, BF16, 16, 4, 2, 128, 16, seed=2)
+    q = s.q.cuda()
+    clean, lse = kv.attend(s.cache, s.batch, q, want_lse=True)
+    seen_from = rows[0] // 2                                             # of the first sequence, by this row and those behind it
+    token = tokens[0] - rows[0] + seen_from
+    s.v_pool[int(s.table[0, token // 16]), token % 16] = 2.0 ** 127
+    out, again = kv.attend(s.cache, s.batch, q, want_lse=True)
+    see = torch.zeros(s.n_rows, dtype=torch.bool, device="cuda")
+    see[seen_from:rows[0]] = True
+    assert torch.equal(out[~see], clean[~see]) and torch.equal(lse[~see], again[~see])
+    s.check_attend(out, again)
