@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
     if (a.rope) {
         const uint32_t at = a.positions ? (uint32_t)a.positions[row] : p.position;
         if (at >= a.rope_rows) {
-            if (x0 == 0) kv_note(g.b.errors, TENT_KV_BAD_POSITION);
+            if (x0 == 0) kv_note(g.b.errors, TENT_KV_BAD_POSITION | (to.page < 0 ? TENT_KV_BAD_PAGE : 0));
             return;
         }
         const uint32_t half = a.rope_dim / 16;

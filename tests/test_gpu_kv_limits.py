@@ -168,3 +168,16 @@ def test_rows_that_do_not_see_large_values_do_not_change(kv, rows, tokens):
     see[seen_from:rows[0]] = True
     assert torch.equal(out[~see], clean[~see]) and torch.equal(lse[~see], again[~see])
     s.check_attend(out, again)
+
+
+# ---- what is noted -------------------------------------------------------------------------------
+def test_a_row_outside_the_rotations_without_a_page_notes_both(kv):
+    s = Setup(kv, [1, 2], [30, 2], BF16, 16, 2, 1, 64, 16)
+    x = torch.zeros(3, 1, 64, dtype=BF16, device="cuda")
+    s.batch.page_table[0, 1] = 1 << 20
+    for at, page, noted in ((0, 1 << 20, 2), (40, int(s.table[0, 1]), 4), (40, 1 << 20, 2 | 4)):
+        s.batch.errors.zero_()
+        s.batch.page_table[0, 1] = page
+        positions = torch.tensor([at, 0, 1], dtype=torch.int32, device="cuda")
+        kv.append(s.cache, s.batch, x, x, rope=kv.rope_table(40, 64), positions=positions)
+        assert int(s.batch.errors) == noted
