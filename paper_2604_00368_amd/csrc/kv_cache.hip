@@ -34,7 +34,8 @@ __device__ __forceinline__ uint32_t find_sequence(const tent_kv_batch& b, int32_
     return lo;
 }
 
-// Up to 64 sequences are loaded at once, a lane each, so that a row's place is one load away; more of them are searched.
+// Up to 64 sequences are loaded at once, a lane each, so that a row's place is one load away; more of them are searched.  Wrong
+// sequences are noted whether or not rows belong to them: by the first workgroup, or, of more than 64, by as many as it takes.
 __device__ __forceinline__ void find_rows(RowPlace* to, const KvCache& c, const tent_kv_batch& b, uint32_t row0, uint32_t n)
 {
     if (threadIdx.x < 64) {
@@ -50,6 +51,7 @@ __device__ __forceinline__ void find_rows(RowPlace* to, const KvCache& c, const 
                 if (lane == i) s = before ? before - 1 : 0;
             }
             q = kv_sequence(b, __shfl(lo, (int)s, 64), __shfl(hi, (int)s, 64), __shfl(len, (int)s, 64));
+            if (blockIdx.x == 0 && kv_sequence(b, lo, hi, len).bad) kv_note(b.errors, TENT_KV_BAD_SEQUENCE);
         } else {
             s = find_sequence(b, (int32_t)row0, lane);
             if (lane < n) {
@@ -59,8 +61,7 @@ __device__ __forceinline__ void find_rows(RowPlace* to, const KvCache& c, const 
         }
         if (lane < n) {
             RowPlace p{0, 0, false};
-            if (q.bad) kv_note(b.errors, TENT_KV_BAD_SEQUENCE);
-            else if (row >= q.row0 && row < q.row0 + q.rows) {
+            if (row >= q.row0 && row < q.row0 + q.rows) {                // a bad sequence has no rows
                 const int32_t position = q.len - q.rows + (row - q.row0);
                 if (position < 0) kv_note(b.errors, TENT_KV_BAD_POSITION);
                 else p = RowPlace{s, (uint32_t)position, true};
@@ -69,6 +70,9 @@ __device__ __forceinline__ void find_rows(RowPlace* to, const KvCache& c, const 
         }
     }
     __syncthreads();
+    if (b.n_seqs > 64 && threadIdx.x < 64)                               // behind the barrier, which the others wait at
+        for (uint32_t s = blockIdx.x * 64 + threadIdx.x; s < b.n_seqs; s += gridDim.x * 64)
+            if (kv_sequence(b, s).bad) kv_note(b.errors, TENT_KV_BAD_SEQUENCE);
 }
 
 // A row's page as a byte offset, negative if there is none, and its token in it.

@@ -181,3 +181,26 @@ def test_a_row_outside_the_rotations_without_a_page_notes_both(kv):
         positions = torch.tensor([at, 0, 1], dtype=torch.int32, device="cuda")
         kv.append(s.cache, s.batch, x, x, rope=kv.rope_table(40, 64), positions=positions)
         assert int(s.batch.errors) == noted
+
+
+@pytest.mark.parametrize("n_seqs", [3, 64, 65, 300])
+@pytest.mark.parametrize("wrong", ["length", "rows", "beyond"])
+def test_wrong_sequences_without_rows_of_their_own_are_noted(kv, n_seqs, wrong):
+    # sequence s - 1 has no rows, or rows that are no rows of the call
+    rows = [2] + [0] * (n_seqs - 3) + [0, 1]
+    s = Setup(kv, rows, [r + 3 for r in rows], BF16, 16, 2, 1, 64, 16)
+    x = torch.zeros(3, 1, 64, dtype=BF16, device="cuda")
+    calls = (lambda: kv.append(s.cache, s.batch, x, x), lambda: kv.read(s.cache, s.batch), lambda: kv.attend(s.cache, s.batch, s.q.cuda()))
+    for call in calls:
+        call()
+        assert int(s.batch.errors) == 0
+    if wrong == "length":
+        s.batch.kv_len[n_seqs - 2] = 1 << 20
+    elif wrong == "rows":
+        s.batch.row_start[n_seqs - 1] = 1                                # it would end before it starts
+    else:
+        s.batch.row_start[n_seqs] = 4                                    # the last one's rows go past the call's
+    for call in calls:
+        s.batch.errors.zero_()
+        call()
+        assert int(s.batch.errors) & 1
