@@ -49,6 +49,7 @@ struct AttendArgs {
     float to_log2;                     // scale * log2(e)
     uint32_t n_splits, split_tokens;   // tokens of a split: a multiple of 128
     uint32_t line_tiles;               // workgroups over the lines of a sequence and head
+    uint32_t first;                    // of the launch's workgroups
 };
 
 // A kernel's arguments, read anew: what hardly any call comes to should not keep them in registers all along.
@@ -365,7 +366,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
     // All heads of a (sequence, split) go to one XCD one after the other: the heads of a token share lines of its page.  The later
     // splits, which short sequences do not have, come last, and each of them begins with another sequence: otherwise the XCDs that
     // get them, or get the long sequences, would have more or less to do than the others.
-    const uint32_t eight = blockIdx.x / (8 * g.c.heads), in_eight = blockIdx.x - eight * 8 * g.c.heads;
+    const uint32_t block = g.first + blockIdx.x, eight = block / (8 * g.c.heads), in_eight = block - eight * 8 * g.c.heads;
     const uint32_t unit = eight * 8 + in_eight % 8, head = in_eight / 8;
     if (unit >= g.b.n_seqs * g.n_splits) return;
     const uint32_t split = unit / g.b.n_seqs, seq = (unit + split) % g.b.n_seqs;
@@ -738,7 +739,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
 
     const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t m = lane & 31u, upper = lane >> 5;
-    const WideUnit unit = wide_unit(g, blockIdx.x);
+    const WideUnit unit = wide_unit(g, g.first + blockIdx.x);
     const uint32_t head = unit.head, seq = unit.seq, split = unit.split, line_tile = unit.line_tile;
     const KvSeq q = kv_sequence(g.b, seq);
     if (q.bad && threadIdx.x == 0 && split == 0 && head == 0 && line_tile == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
@@ -1056,7 +1057,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         uint32_t lines_left = (uint32_t)__ballot(large);                 // the lower lanes: a line each
         if (lines_left) {
             const AttendArgs& a = args_again();
-            const WideUnit u = wide_unit(a, blockIdx.x);
+            const WideUnit u = wide_unit(a, a.first + blockIdx.x);
             const KvSeq q = kv_sequence(a.b, u.seq);
             const int32_t line0 = (int32_t)u.line_tile * kWideLines, lines = q.rows * (int32_t)a.group;
             const Range range = token_range(a, q, line0, line0 + kWideLines < lines ? line0 + kWideLines - 1 : lines - 1, u.split);
@@ -1224,22 +1225,26 @@ uint64_t blocks_of(const Shape& s, const AttendArgs& g)
 }
 
 template <class E, int D, int kBits>
-int launch(const Shape& s, const AttendArgs& g, hipStream_t stream)
+int launch(const Shape& s, AttendArgs g, hipStream_t stream)
 {
-    const uint64_t blocks = blocks_of(s, g), join = (uint64_t)g.b.max_rows * g.q_heads;
-    if (blocks > 0x7FFFFFFFull || join > 0x7FFFFFFFull) return TENT_ERR_RANGE;
-    const dim3 grid((uint32_t)blocks), threads(256);
-    if (s.wide) {
-        hipLaunchKernelGGL((wide_kernel<E, D, kBits>), grid, threads, 0, stream, g);
-    } else if (s.line_tiles == 1) {
-        hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 1>), grid, threads, 0, stream, g);
-    } else if (s.line_tiles == 2) {
-        hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 2>), grid, threads, 0, stream, g);
-    } else {
-        if constexpr (D != 256) hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 4>), grid, threads, 0, stream, g);
-    }
-    if (hipGetLastError() != hipSuccess) return TENT_ERR_HIP;
+    const dim3 threads(256);
+    const int rc = launch_blocks(blocks_of(s, g), [&](uint32_t first, uint32_t blocks) {
+        const dim3 grid(blocks);
+        g.first = first;
+        if (s.wide) {
+            hipLaunchKernelGGL((wide_kernel<E, D, kBits>), grid, threads, 0, stream, g);
+        } else if (s.line_tiles == 1) {
+            hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 1>), grid, threads, 0, stream, g);
+        } else if (s.line_tiles == 2) {
+            hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 2>), grid, threads, 0, stream, g);
+        } else {
+            if constexpr (D != 256) hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 4>), grid, threads, 0, stream, g);
+        }
+    });
+    if (rc != TENT_OK) return rc;
     if (g.part_o) {
+        // There are splits where fewer workgroups are wanted than the 1536 of shape_of, of 128 lines at most: a launch holds their joins.
+        const uint64_t join = (uint64_t)g.b.max_rows * g.q_heads;
         // A wave to a line: up to four parts are all in flight at once.
         if (s.n_splits <= 4) hipLaunchKernelGGL((join_kernel<E, D, kWaves>), dim3((uint32_t)((join + kWaves - 1) / kWaves), g.b.n_seqs), threads, 0, stream, g);
         else hipLaunchKernelGGL((join_kernel<E, D, 1>), dim3((uint32_t)join, g.b.n_seqs), threads, 0, stream, g);

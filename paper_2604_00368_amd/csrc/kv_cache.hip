@@ -140,6 +140,7 @@ struct AppendArgs {
     tent_kv_batch b;
     uint32_t per_row;          // lanes that a row needs: one for every eight values of its heads
     uint32_t side;             // rows that a workgroup takes side by side
+    uint32_t first;            // of the launch's workgroups
 };
 
 // Eight values of a head, normalised and turned; the lanes of the head come here together.  F: float for queries; double for keys,
@@ -212,7 +213,7 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
     __shared__ RowPlace place[kMaxRowTile];
     constexpr uint32_t kChunks = D / 8;
     const tent_kv_append_args& a = g.a;
-    const uint32_t row0 = blockIdx.x * g.side, n = g.b.n_rows - row0 < g.side ? g.b.n_rows - row0 : g.side;
+    const uint32_t row0 = (g.first + blockIdx.x) * g.side, n = g.b.n_rows - row0 < g.side ? g.b.n_rows - row0 : g.side;
     const uint32_t r = g.side == 1 ? 0u : threadIdx.x / g.per_row, x0 = threadIdx.x - r * g.per_row + blockIdx.y * blockDim.x, chunk = x0 % kChunks;
     const uint32_t stride = blockDim.x * gridDim.y;
     const uint64_t row = row0 + r;
@@ -294,6 +295,7 @@ struct ReadArgs {
     uint8_t *k, *v;
     uint64_t stride;           // bytes
     uint32_t row_tile;
+    uint32_t first;            // of the launch's workgroups
 };
 
 // A workgroup takes `row_tile` rows, their keys first, then their values, kBatch chunks a lane in flight.
@@ -302,7 +304,7 @@ __global__ void __launch_bounds__(256) read_kernel(const ReadArgs g)
 {
     __shared__ RowPlace place[kMaxRowTile];
     constexpr uint32_t kChunks = D / 8;
-    const uint32_t row0 = blockIdx.x * g.row_tile;
+    const uint32_t row0 = (g.first + blockIdx.x) * g.row_tile;
     const uint32_t n = g.b.n_rows - row0 < g.row_tile ? g.b.n_rows - row0 : g.row_tile;
     find_rows(place, g.c, g.b, row0, n);
     __shared__ PagePlace pages[kMaxRowTile];
@@ -353,6 +355,7 @@ struct PackArgs {
     const int32_t *src_pages, *dst_pages;
     int32_t* errors;
     uint32_t n_pages, parts;   // workgroups for one page of one pool
+    uint32_t first;            // of the launch's workgroups
 };
 
 // A workgroup takes four chunks a lane of one page of K or V, all four in flight at once.
@@ -361,7 +364,7 @@ template <class E, int D>
 __global__ void __launch_bounds__(256) pack_kernel(const PackArgs g)
 {
     constexpr uint32_t kChunks = D / 8;
-    const uint32_t part = blockIdx.x % g.parts, at = blockIdx.x / g.parts;
+    const uint32_t block = g.first + blockIdx.x, part = block % g.parts, at = block / g.parts;
     const bool is_v = at >= g.n_pages;
     const uint32_t i = is_v ? at - g.n_pages : at;
     const uint32_t from = (uint32_t)g.src_pages[i], to = (uint32_t)g.dst_pages[i];
@@ -416,16 +419,16 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackArgs g)
     }
 }
 
-int launched() { return hipGetLastError() == hipSuccess ? TENT_OK : TENT_ERR_HIP; }
-
 template <class E, int D, int kBits>
 int launch_append(AppendArgs g, hipStream_t s)
 {
     g.per_row = (g.a.q_heads + 2 * g.c.heads) * (D / 8);
     g.side = g.per_row >= 256 ? 1 : 256 / g.per_row;                     // at most 16: a row has a key and a value of 64 at least
     const uint32_t turns = (g.per_row + 255) / 256, threads = g.side > 1 ? 256 : (g.per_row + turns * 64 - 1) / (turns * 64) * 64;
-    hipLaunchKernelGGL((append_kernel<E, D, kBits>), dim3((g.b.n_rows + g.side - 1) / g.side, (uint64_t)g.b.n_rows * turns <= 512 ? turns : 1), dim3(threads), 0, s, g);
-    return launched();
+    return launch_blocks(((uint64_t)g.b.n_rows + g.side - 1) / g.side, [&](uint32_t first, uint32_t blocks) {
+        g.first = first;
+        hipLaunchKernelGGL((append_kernel<E, D, kBits>), dim3(blocks, (uint64_t)g.b.n_rows * turns <= 512 ? turns : 1), dim3(threads), 0, s, g);
+    });
 }
 // Rows of a workgroup: as many as its lanes take in one batch, fewer where that leaves compute units without one.
 template <class E, int D, int kBits>
@@ -434,18 +437,20 @@ int launch_read(ReadArgs g, hipStream_t s)
     const uint32_t batch = kBatch * 256 / (2 * g.c.heads * (D / 8)), spread = g.b.n_rows / 1024;
     const uint32_t n = batch < spread ? batch : spread;
     g.row_tile = n < 1 ? 1 : n > kMaxRowTile ? kMaxRowTile : n;
-    hipLaunchKernelGGL((read_kernel<E, D, kBits>), dim3((g.b.n_rows + g.row_tile - 1) / g.row_tile), dim3(256), 0, s, g);
-    return launched();
+    return launch_blocks(((uint64_t)g.b.n_rows + g.row_tile - 1) / g.row_tile, [&](uint32_t first, uint32_t blocks) {
+        g.first = first;
+        hipLaunchKernelGGL((read_kernel<E, D, kBits>), dim3(blocks), dim3(256), 0, s, g);
+    });
 }
 template <class E, int D>
 int launch_pack(PackArgs g, hipStream_t s)
 {
     const uint32_t n = (g.src.heads * (D / 8)) << g.src.page_shift;
     g.parts = (n + 256 * kPackChunks - 1) / (256 * kPackChunks);
-    const uint64_t blocks = (uint64_t)2 * g.n_pages * g.parts;
-    if (blocks > 0x7FFFFFFFull) return TENT_ERR_RANGE;
-    hipLaunchKernelGGL((pack_kernel<E, D>), dim3((uint32_t)blocks), dim3(256), 0, s, g);
-    return launched();
+    return launch_blocks((uint64_t)2 * g.n_pages * g.parts, [&](uint32_t first, uint32_t blocks) {
+        g.first = first;
+        hipLaunchKernelGGL((pack_kernel<E, D>), dim3(blocks), dim3(256), 0, s, g);
+    });
 }
 
 }  // namespace
@@ -481,7 +486,7 @@ extern "C" int tent_kv_append(const tent_kv_cache* cache, const tent_kv_batch* b
     if (!(args->eps >= 0.f) || args->eps > 3.4e38f) return TENT_ERR_RANGE;
     if (args->rope && (args->rope_rows < 1 || args->rope_dim < 16 || args->rope_dim > D || args->rope_dim % 16)) return TENT_ERR_RANGE;
     if ((uintptr_t)args->positions & 3u) return TENT_ERR_INVALID;
-    const AppendArgs g{*args, kv_cache_dev(*cache), *batch, 0, 0};
+    const AppendArgs g{*args, kv_cache_dev(*cache), *batch, 0, 0, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define TENT_APPEND(dim)                                                                                   \
     (cache->type == TENT_BF16 ? (cache->bits == 16 ? launch_append<Bf16, dim, 16>(g, s) : launch_append<Bf16, dim, 4>(g, s)) \
@@ -498,7 +503,7 @@ extern "C" int tent_kv_read(const tent_kv_cache* cache, const tent_kv_batch* bat
     if (batch->n_seqs == 0 || batch->n_rows == 0) return TENT_OK;
     if ((rc = kv_check_rows(k_out, out_stride, cache->kv_heads, cache->head_dim, batch->n_rows)) != TENT_OK) return rc;
     if ((rc = kv_check_rows(v_out, out_stride, cache->kv_heads, cache->head_dim, batch->n_rows)) != TENT_OK) return rc;
-    const ReadArgs g{kv_cache_dev(*cache), *batch, static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out), out_stride * 2, 0};
+    const ReadArgs g{kv_cache_dev(*cache), *batch, static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out), out_stride * 2, 0, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define TENT_READ(dim)                                                                                     \
     (cache->type == TENT_BF16 ? (cache->bits == 16 ? launch_read<Bf16, dim, 16>(g, s) : launch_read<Bf16, dim, 4>(g, s)) \
@@ -517,7 +522,7 @@ extern "C" int tent_kv_pack(const tent_kv_cache* src, const tent_kv_cache* dst, 
     if (n_pages == 0) return TENT_OK;
     if (!src_pages || !dst_pages || (((uintptr_t)src_pages | (uintptr_t)dst_pages | (uintptr_t)errors) & 3u)) return TENT_ERR_INVALID;
     if (n_pages > 0x7FFFFFFFu) return TENT_ERR_RANGE;
-    const PackArgs g{kv_cache_dev(*src), kv_cache_dev(*dst), src_pages, dst_pages, errors, n_pages, 0};
+    const PackArgs g{kv_cache_dev(*src), kv_cache_dev(*dst), src_pages, dst_pages, errors, n_pages, 0, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define TENT_PACK(dim) (src->type == TENT_BF16 ? launch_pack<Bf16, dim>(g, s) : launch_pack<Fp16, dim>(g, s))
     return TENT_KV_DIM(src->head_dim, TENT_PACK);

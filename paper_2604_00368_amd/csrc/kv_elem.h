@@ -28,6 +28,20 @@ __device__ __forceinline__ void dev_store(void* p, V v) { *(__attribute__((addre
 template <class V>
 __device__ __forceinline__ void dev_stream(void* p, V v) { __builtin_nontemporal_store(v, (__attribute__((address_space(1))) V*)(uintptr_t)p); }
 
+// A launch takes fewer than 2^32 lanes, so more than this many workgroups of up to 256 go in several launches, each told its first.
+// A multiple of eight: workgroups keep their XCDs.
+constexpr uint32_t kMostBlocks = 1u << 23;
+template <class Launch>
+int launch_blocks(uint64_t blocks, Launch launch)
+{
+    if (blocks > 0x7FFFFFFFull) return TENT_ERR_RANGE;
+    for (uint64_t first = 0; first < blocks; first += kMostBlocks) {
+        launch((uint32_t)first, (uint32_t)(blocks - first < kMostBlocks ? blocks - first : kMostBlocks));
+        if (hipGetLastError() != hipSuccess) return TENT_ERR_HIP;
+    }
+    return TENT_OK;
+}
+
 __device__ __forceinline__ void kv_note(int32_t* errors, int32_t what)
 {
     if (errors) atomicOr(errors, what);

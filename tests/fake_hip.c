@@ -8,7 +8,7 @@
 enum { LAUNCH = 1, RECORD = 2, WAIT = 3, HOST_WAIT = 4, COPY = 5 };
 enum { MOST = 1 << 16, KERNELS = 512 };
 
-static struct { int kind; void *stream, *what; } log_[MOST];
+static struct { int kind; void *stream, *what; dim3 grid, block; } log_[MOST];
 static int n_log, n_kernels, fail_host_waits;
 static struct { const void *fn; const char *name; } kernel[KERNELS];
 static void *capturing_stream, *termed_stream;
@@ -30,6 +30,11 @@ int fake_log_at(int i, void **stream, void **what)
     *stream = log_[i].stream;
     *what = log_[i].what;
     return log_[i].kind;
+}
+void fake_log_grid(int i, unsigned *blocks, unsigned *threads)
+{
+    blocks[0] = log_[i].grid.x; blocks[1] = log_[i].grid.y; blocks[2] = log_[i].grid.z;
+    threads[0] = log_[i].block.x; threads[1] = log_[i].block.y; threads[2] = log_[i].block.z;
 }
 const char *fake_kernel_name(const void *fn)
 {
@@ -158,7 +163,8 @@ hipError_t __hipPopCallConfiguration(dim3 *g, dim3 *b, size_t *sh, hipStream_t *
 }
 hipError_t hipLaunchKernel(const void *fn, dim3 g, dim3 b, void **args, size_t sh, hipStream_t s)
 {
-    (void)g; (void)b; (void)sh;
+    (void)sh;
+    if (n_log < MOST) { log_[n_log].grid = g; log_[n_log].block = b; }
     note(LAUNCH, s, (void *)fn);
     for (size_t r = 0; answer && r < sizeof(reporter) / sizeof(reporter[0]); ++r) {
         if (!strstr(fake_kernel_name(fn), reporter[r].name)) continue;
