@@ -9,6 +9,8 @@ With `stream` (a torch.cuda.Stream, or a HIP stream's handle) a call allocates a
 and what it returns is kept from being allocated again before both streams are done with it; that its inputs are ready
 when `stream` gets to it, and its outputs before they are used elsewhere, is for the caller to order.
 
+There is no backward pass.  A tensor that requires gradients is refused while they are recorded (not under torch.no_grad()).
+
 A cache of 16 bits is two tensors [pages, page_tokens, kv_heads, head_dim] of bfloat16 or float16; one of 4 bits is two
 uint8 tensors [pages, bytes] (``packed_pool``), whose pages hold 32 values to a shared power of two.  Pages are contiguous
 byte ranges either way, so the engine moves them as extents of ``page_bytes``.
@@ -56,9 +58,15 @@ def _on(device, stream, used, call):
     return result
 
 
+def _no_gradients(tensor, name):
+    if tensor.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires gradients, and there is no backward pass: detach it, or call under torch.no_grad()")
+
+
 def _on_gpu(tensor, name, dtype, shape=None):
     if not isinstance(tensor, torch.Tensor) or not tensor.is_cuda:
         raise ValueError(f"{name} must be a tensor on a GPU")
+    _no_gradients(tensor, name)
     if tensor.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, not {tensor.dtype}")
     if shape is not None and tuple(tensor.shape) != tuple(shape):
@@ -74,6 +82,8 @@ def _rows(tensor, name, dtype, rows, heads, dim, device):
         raise ValueError(f"{name} must be {dtype} on {device}, not {tensor.dtype} on {tensor.device}")
     if tensor.shape != (rows, heads, dim):
         raise ValueError(f"{name} must have shape {(rows, heads, dim)}, not {tuple(tensor.shape)}")
+    if tensor.requires_grad:
+        _no_gradients(tensor, name)
     stride = tensor.stride()
     if (stride[2] != 1 and dim > 1) or (stride[1] != dim and heads > 1):
         raise ValueError(f"{name} must have contiguous heads (strides {stride})")
@@ -117,6 +127,8 @@ class Cache:
             raise ValueError("k and v must be tensors on one GPU")
         if k.dtype != v.dtype or k.shape != v.shape or k.stride() != v.stride():
             raise ValueError("k and v must have the same type, shape and strides")
+        _no_gradients(k, "k")
+        _no_gradients(v, "v")
         if k.dtype == torch.uint8:
             if k.dim() != 2 or dtype not in _TYPES or None in (page_tokens, kv_heads, head_dim):
                 raise ValueError("a 4-bit cache is uint8 [pages, bytes], with dtype, page_tokens, kv_heads and head_dim")

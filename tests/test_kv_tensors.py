@@ -240,3 +240,28 @@ def test_calls_go_to_the_device_of_their_tensors(gpus, index):
                 call(stream=given)
                 assert (name, index, handle) in gpus.log
                 assert gpus.at == at and [gpus.streams[i].cuda_stream for i in (0, 1)] == [0x10, 0x20]
+
+
+def test_gradients_are_not_dropped_without_a_word(gpus):
+    s = Step(gpus)
+
+    def learns(t):
+        return s.on(t.as_subclass(torch.Tensor).detach().clone().requires_grad_())
+
+    cases = [(s.append, name, dict([(name, learns(getattr(s, of)))])) for name, of in
+             (("k", "k"), ("v", "v"), ("q", "q"), ("q_weight", "weight"), ("k_weight", "weight"), ("rope", "rope"))]
+    cases += [(s.append, "q_out", dict(q_out=learns(s.q))), (s.attend, "q", dict(q=learns(s.q))), (s.attend, "out", dict(out=learns(s.q))),
+              (s.read, "k_out", dict(k_out=learns(s.k), v_out=s.v))]
+    for call, name, change in cases:
+        gpus.log.clear()
+        with pytest.raises(ValueError, match=f"{name} requires gradients"):
+            call(**change)
+        assert not [e for e in gpus.log if e[0] in ("append", "attend", "read")]
+        with torch.no_grad():                                            # a serving program's weights are parameters, too
+            call(**change)
+        assert gpus.log[-1][0] in ("append", "attend", "read")
+    pool = learns(s.cache.k)
+    with pytest.raises(ValueError, match="k requires gradients"):
+        kv.Cache(pool, pool)
+    with torch.no_grad():
+        kv.Cache(pool, pool)
