@@ -139,8 +139,8 @@ class Cache:
             if k.dtype not in _TYPES or k.dim() != 4 or dtype not in (None, k.dtype):
                 raise ValueError("a 16-bit cache is bfloat16 or float16 [pages, page_tokens, kv_heads, head_dim]")
             dtype, (_, page_tokens, kv_heads, head_dim) = k.dtype, k.shape
-            if k[0].numel() == 0 or not k[0].is_contiguous():
-                raise ValueError("pages must be contiguous and not empty")
+            if k[:1].numel() == 0 or not k[0].is_contiguous():
+                raise ValueError("pages must be contiguous, not empty, and one at least")
             bits, stride = 16, 2 * k.stride(0)
         if k.shape[0] == 0:
             raise ValueError("a cache needs a page")

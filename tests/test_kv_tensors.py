@@ -265,3 +265,14 @@ def test_gradients_are_not_dropped_without_a_word(gpus):
         kv.Cache(pool, pool)
     with torch.no_grad():
         kv.Cache(pool, pool)
+
+
+def test_pools_of_nothing_are_refused(gpus):
+    s = Step(gpus)
+    for shape in ((0, 16, 2, 64), (2, 0, 2, 64), (2, 16, 0, 64), (2, 16, 2, 0)):
+        pool = s.on(torch.zeros(*shape, dtype=torch.bfloat16))
+        with pytest.raises(ValueError, match="page"):
+            kv.Cache(pool, pool)
+    pool = s.on(torch.zeros(0, 16 * 2 * 34, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="page"):
+        kv.Cache(pool, pool, dtype=torch.bfloat16, page_tokens=16, kv_heads=2, head_dim=64)
