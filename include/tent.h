@@ -608,7 +608,8 @@ uint64_t tent_kv_packed_page(uint32_t page_tokens, uint32_t kv_heads, uint32_t h
  * the keys and values to their pages.  Without `rope` nothing is rotated; dimensions from rope_dim on never are.
  * Dimension i < rope_dim / 2 turns with i + rope_dim / 2 (TENT_KV_ROPE_PAIRS: 2i with 2i + 1) by angle i:
  * (a, b) -> (a cos - b sin, b cos + a sin).  Keys are computed in 64 bits and rounded to 32 and from there to 16 bits, for
- * both kinds of page, so a 4-bit cache holds what tent_kv_pack makes of a 16-bit one; queries are computed in 32 bits. */
+ * both kinds of page, so a 4-bit cache holds what tent_kv_pack makes of a 16-bit one; queries are computed in 32 bits, or in 64
+ * where their mean of squares is too large or too small for 32. */
 int tent_kv_append(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_append_args *args, void *stream);
 
 /* Pack `n_pages` whole pages: page src_pages[i] of the 16-bit cache `src` becomes page dst_pages[i] of the 4-bit cache

@@ -145,9 +145,10 @@ struct AppendArgs {
 
 // Eight values of a head, normalised and turned; the lanes of the head come here together.  F: float for queries; double for keys,
 // so that a value next to the border of two codes falls on its own side.  `w`: the weights of this lane's dimensions, `cs`: their
-// cosines and sines.  What a dimension turns with is in another lane of the head.
+// cosines and sines.  What a dimension turns with is in another lane of the head.  `in_64` becomes true, and the result means nothing,
+// where a float's range is too short for a mean of squares: of bfloat16 values from 2^60 on, or where neither they nor eps reach 2^-100.
 template <class E, int D, class F>
-__device__ __forceinline__ u32x4 norm_rotate(const tent_kv_append_args& a, u32x4 raw, uint32_t chunk, bool weighted, u32x4 w, const float* cs)
+__device__ __forceinline__ u32x4 norm_rotate(const tent_kv_append_args& a, u32x4 raw, uint32_t chunk, bool weighted, u32x4 w, const float* cs, bool& in_64)
 {
     constexpr uint32_t kChunks = D / 8;
     if (!weighted && !a.rope) return raw;
@@ -166,7 +167,9 @@ __device__ __forceinline__ u32x4 norm_rotate(const tent_kv_append_args& a, u32x4
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
         sum = sum_lanes<kChunks>(sum);
-        r = (F)1 / sqrt(sum * ((F)1 / D) + (F)a.eps);
+        const F mean = sum * ((F)1 / D) + (F)a.eps;
+        if (E::kLarge && sizeof(F) == 4 && !(mean >= (F)0x1p-100 && mean < (F)0x1p120)) in_64 = true;
+        r = (F)1 / sqrt(mean);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i] *= r * (F)E::to_float(w[i] & 0xFFFFu);
@@ -277,13 +280,15 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs g)
         for (int i = 0; i < 16; ++i) __asm__ volatile("" : "+v"(cs[i]));
         __asm__ volatile("" : "+v"(wq), "+v"(wk));
         const uint32_t h = x / kChunks;
+        bool in_64 = false;
         if (h < a.q_heads) {
-            const u32x4 y = norm_rotate<E, D, float>(a, now, chunk, a.q_weight, wq, cs);
+            u32x4 y = norm_rotate<E, D, float>(a, now, chunk, a.q_weight, wq, cs, in_64);
+            if (in_64) y = norm_rotate<E, D, double>(a, now, chunk, a.q_weight, wq, cs, in_64);
             dev_store((uint8_t*)a.q_out + (row * a.q_out_stride + (uint64_t)h * D + chunk * 8) * 2, y);
         } else if (to.page >= 0) {
             const bool is_v = h >= a.q_heads + g.c.heads;
             const uint32_t kh = h - a.q_heads - (is_v ? g.c.heads : 0u);
-            const u32x4 y = is_v ? now : norm_rotate<E, D, double>(a, now, chunk, a.k_weight, wk, cs);
+            const u32x4 y = is_v ? now : norm_rotate<E, D, double>(a, now, chunk, a.k_weight, wk, cs, in_64);
             put8<E, D, kBits>((is_v ? g.c.v : g.c.k) + to.page, g.c.page_shift, to.slot, g.c.heads, kh, chunk, y);
         }
     }

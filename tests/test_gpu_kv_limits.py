@@ -204,3 +204,32 @@ def test_wrong_sequences_without_rows_of_their_own_are_noted(kv, n_seqs, wrong):
         s.batch.errors.zero_()
         call()
         assert int(s.batch.errors) & 1
+
+
+# ---- norms ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("power,eps", [(62, 1e-6), (120, 1e-6), (-60, 0.0), (-120, 0.0), (-60, 1e-6), (10, 0.0)])
+def test_norms_of_large_and_small_rows(kv, dim, pairs, power, eps, bits):
+    # of queries as of keys; every second head is of ordinary size
+    s = Setup(kv, [3, 2], [30, 2], BF16, bits, 4, 2, dim, 16)
+    q, k, v = (torch.randn(5, h, dim, generator=s.g).to(BF16) for h in (4, 2, 2))
+    for x in (q, k):
+        x[:, ::2] = (x[:, ::2].double() * 2.0 ** power).to(BF16)
+    weights = [(1 + 0.3 * torch.randn(dim, generator=s.g)).to(BF16) for _ in "qk"]
+    table = kv.rope_table(30, dim, device="cpu")
+    got = kv.append(s.cache, s.batch, k.cuda(), v.cuda(), q=q.cuda(), q_weight=weights[0].cuda(), k_weight=weights[1].cuda(), eps=eps,
+                    rope=table.cuda(), rope_pairs=pairs)
+    turn = table.double().numpy()[[27, 28, 29, 0, 1]]
+    e = float(np.float32(eps))
+    want_k = R.to_type(R.norm_rotate(k.double().numpy(), weights[1].double().numpy(), e, turn, dim, pairs), BF16)
+    back, _ = kv.read(s.cache, s.batch)
+    want = R.decode4(*R.encode4(want_k, BF16)) if bits == 4 else want_k
+    assert np.array_equal(back.cpu().double().numpy(), want)
+    want = R.norm_rotate(q.double().numpy(), weights[0].double().numpy(), e, turn, dim, pairs)
+    # 32-bit arithmetic, or better: a sum of squares over `dim`, a root, a quotient, products; terms of a turn do not exceed the pair's size
+    size = 2 * np.abs(want).max(-1, keepdims=True)
+    off = np.abs(got.cpu().double().numpy() - want)
+    assert (off <= R.half_step(BF16) * np.abs(want) * 1.01 + (dim + 32) * 2.0 ** -24 * size + 2.0 ** -133).all()
+    assert int(s.batch.errors) == 0
