@@ -29,8 +29,8 @@ _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_get
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
-def _stream(device):
-    return C.c_void_p(_raw_stream(device.index) if _raw_stream else torch.cuda.current_stream(device.index).cuda_stream)
+def _stream(index):
+    return C.c_void_p(_raw_stream(index) if _raw_stream else torch.cuda.current_stream(index).cuda_stream)
 
 
 def _on(device, stream, used, call):
@@ -151,7 +151,7 @@ class Cache:
         self.c = T.tent_kv_cache(k.data_ptr(), v.data_ptr(), k.shape[0], stride, self.page_tokens, self.kv_heads, self.head_dim,
                                  _TYPES[dtype], bits, 0)
         self.ref = C.byref(self.c)                                       # made once: calls take it as it is
-        self.tensors = (k, v)
+        self.tensors, self.index = (k, v), k.device.index
 
     @property
     def page_bytes(self) -> int:
@@ -207,7 +207,7 @@ def append(cache: Cache, batch: Batch, k, v, q=None, q_weight=None, k_weight=Non
     multiple of 8 values.  q_weight, k_weight: [head_dim], RMS norm over a head.  rope: float32 [positions, rope_dim] as
     rope_table makes it, indexed by `positions` (int32 [rows]) or the row's position in its sequence; rope_pairs turns
     neighbouring dimensions instead of halves.  q_out may be q."""
-    if stream is not None or cache.device.index != _current_device():
+    if stream is not None or cache.index != _current_device():
         return _on(cache.device, stream, (*cache.tensors, *batch.tensors, k, v, q, q_weight, k_weight, rope, positions, q_out),
                    lambda: append(cache, batch, k, v, q, q_weight, k_weight, eps, rope, rope_pairs, positions, q_out))
     _together(cache, batch)
@@ -238,14 +238,14 @@ def append(cache: Cache, batch: Batch, k, v, q=None, q_weight=None, k_weight=Non
         if not _on_gpu(positions, "positions", torch.int32, (n,)).is_contiguous() or positions.device != device:
             raise ValueError("positions must be contiguous, on the cache's device")
         a.positions = positions.data_ptr()
-    _check(T.lib().tent_kv_append(cache.ref, batch.ref, C.byref(a), _stream(cache.device)), "tent_kv_append")
+    _check(T.lib().tent_kv_append(cache.ref, batch.ref, C.byref(a), _stream(cache.index)), "tent_kv_append")
     return q_out
 
 
 def pack(src: Cache, dst: Cache, src_pages, dst_pages, errors=None, stream=None):
     """Pack pages src_pages[i] of the 16-bit cache `src` into pages dst_pages[i] of the 4-bit cache `dst` (int32 [pages]).
     `errors`: int32 [1] that page numbers outside the pools are noted in."""
-    if stream is not None or src.device.index != _current_device():
+    if stream is not None or src.index != _current_device():
         return _on(src.device, stream, (*src.tensors, *dst.tensors, src_pages, dst_pages, errors), lambda: pack(src, dst, src_pages, dst_pages, errors))
     for x, name in ((src_pages, "src_pages"), (dst_pages, "dst_pages")):
         if not _on_gpu(x, name, torch.int32).is_contiguous() or x.dim() != 1 or x.device != src.device:
@@ -255,12 +255,12 @@ def pack(src: Cache, dst: Cache, src_pages, dst_pages, errors=None, stream=None)
     if errors is not None and _on_gpu(errors, "errors", torch.int32, (1,)).device != src.device:
         raise ValueError("errors must be on the caches' device")
     _check(T.lib().tent_kv_pack(src.ref, dst.ref, src_pages.data_ptr(), dst_pages.data_ptr(), src_pages.shape[0],
-                                errors.data_ptr() if errors is not None else None, _stream(src.device)), "tent_kv_pack")
+                                errors.data_ptr() if errors is not None else None, _stream(src.index)), "tent_kv_pack")
 
 
 def read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None):
     """The keys and values of the batch's rows as dense tensors [rows, kv_heads, head_dim] of the cache's type."""
-    if stream is not None or cache.device.index != _current_device():
+    if stream is not None or cache.index != _current_device():
         return _on(cache.device, stream, (*cache.tensors, *batch.tensors, k_out, v_out), lambda: read(cache, batch, k_out, v_out))
     _together(cache, batch)
     shape = (batch.n_rows, cache.kv_heads, cache.head_dim)
@@ -271,7 +271,7 @@ def read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None):
     stride = _rows(k_out, "k_out", cache.dtype, *shape, cache.device)
     if _rows(v_out, "v_out", cache.dtype, *shape, cache.device) != stride:
         raise ValueError("k_out and v_out must have the same strides")
-    _check(T.lib().tent_kv_read(cache.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), stride, _stream(cache.device)), "tent_kv_read")
+    _check(T.lib().tent_kv_read(cache.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), stride, _stream(cache.index)), "tent_kv_read")
     return k_out, v_out
 
 
@@ -281,7 +281,7 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
     scores [rows, q_heads] in float32.  scale: 1 / sqrt(head_dim) unless given; window: a row sees its last `window` tokens;
     causal=False: every row sees its whole sequence.  workspace: a contiguous uint8 tensor of at least attend_workspace
     bytes to use instead of a new one."""
-    if stream is not None or cache.device.index != _current_device():
+    if stream is not None or cache.index != _current_device():
         return _on(cache.device, stream, (*cache.tensors, *batch.tensors, q, out, workspace),
                    lambda: attend(cache, batch, q, scale, window, causal, out, want_lse, workspace))
     _together(cache, batch)
@@ -305,7 +305,7 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
         elif not _on_gpu(workspace, "workspace", torch.uint8).is_contiguous() or workspace.device != device:
             raise ValueError("workspace must be contiguous, on the cache's device")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(L.tent_kv_attend(cache.ref, batch.ref, ref, _stream(cache.device)), "tent_kv_attend")
+    _check(L.tent_kv_attend(cache.ref, batch.ref, ref, _stream(cache.index)), "tent_kv_attend")
     return (out, lse) if want_lse else out
 
 
