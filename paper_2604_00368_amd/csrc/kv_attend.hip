@@ -202,50 +202,133 @@ __device__ __forceinline__ float lse_of(float top, float sum, float shift)
     return sum > 0.f ? kLn2 * (top - shift + __builtin_amdgcn_logf(sum)) : sum == 0.f ? -INFINITY : sum;
 }
 
-// One line by one wave, in plain steps: for the lines whose sums pass what 32 bits hold, which outputs of bfloat16 values do not (up
-// to 2^128 both, and a sum takes weights of 2^16 and more).  Here a weight is divided by the sum of all weights before it multiplies a
-// value.  A lane takes one of 64 tokens for its score, then D / 64 dimensions of all 64.  Scores are finite or minus infinity here;
-// values that are not finite are added as they are, whatever their weight.  `line_top`, `line_sum`: what the loops below have
-// found, which stand for the logsumexp and for a part.
+// ---- sums that pass 32 bits ----------------------------------------------------------------------
+// bfloat16 values go up to 2^128, as sums in 32 bits do, and weights of 2^16 and more times values pass it where outputs do not.  A line
+// whose sum of weights is finite and some of whose sums of values are not, though it sees no value in those dimensions that is not, is
+// gone through once more by one wave in plain steps, with each weight divided by the sum of all weights before it multiplies a value.
+// Both walks take 64 tokens at a time: a lane finds one token's row (and its score), then has D / 64 dimensions of all 64 rows.
+// The lane's number, counted anew rather than kept.
+__device__ __forceinline__ uint32_t lane_again() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
+template <int D, int kBits>
+struct Rows64 {
+    RowAt<kBits> at;                                                     // of this lane's token
+    uint64_t held;                                                       // which tokens are there
+};
+template <int D, int kBits>
+__device__ __forceinline__ Rows64<D, kBits> rows_64(const AttendArgs& g, uint32_t seq, uint32_t head, int32_t t0, int32_t hi)
+{
+    const int32_t mine = t0 + (int32_t)lane_again(), t = mine < hi ? mine : hi - 1;
+    const uint32_t page = dev_load<uint32_t>(g.b.page_table + (uint64_t)seq * g.b.table_stride + ((uint32_t)t >> g.c.page_shift));
+    const bool there = mine < hi && page < g.c.n_pages;
+    return Rows64<D, kBits>{row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head), __ballot(there)};
+}
+
+// This lane's dimensions, D / 64 from D / 64 * lane on, of the row of V that lane i has found, in 16 bits each.
+template <class E, int D, int kBits>
+struct Dims {
+    static constexpr int kPer = D / 64;
+    uint32_t v[(kPer + 1) / 2];
+    __device__ __forceinline__ float value(int k) const { return E::to_float(v[k / 2] >> (16 * (k & 1)) & 0xFFFFu); }
+};
+__device__ __forceinline__ uint64_t of_lane(uint64_t x, int i)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, i);
+}
+template <class E, int D, int kBits>
+__device__ __forceinline__ Dims<E, D, kBits> dims_of(const uint8_t* pool, const Rows64<D, kBits>& rows, int i)
+{
+    constexpr int kPer = D / 64;
+    const uint32_t lane = lane_again();
+    const uint8_t* const p = pool + of_lane(rows.at.row, i);
+    Dims<E, D, kBits> to;
+    if constexpr (kBits == 16) {
+        if constexpr (kPer == 1) to.v[0] = dev_load<uint16_t>(p + lane * 2);
+        else
+#pragma unroll
+            for (int k = 0; k < kPer / 2; ++k) to.v[k] = dev_load<uint32_t>(p + (lane * kPer + 2 * k) * 2);
+    } else {
+        const float scale = scale_of(dev_load<uint8_t>(pool + of_lane(rows.at.scale, i) + lane * kPer / 32));
+        if constexpr (kPer == 1) to.v[0] = E::template decode2<0>(dev_load<uint8_t>(p + lane / 2), scale) >> (16 * (lane & 1u)) & 0xFFFFu;
+        else
+#pragma unroll
+            for (int k = 0; k < kPer / 2; ++k) to.v[k] = E::template decode2<0>(dev_load<uint8_t>(p + lane * (kPer / 2) + k), scale);
+    }
+    return to;
+}
+
+// The first and the last token from lo to hi with a value that is not finite, for each of this lane's dimensions.
+template <int D>
+struct Unfinite {
+    int32_t first[D / 64], last[D / 64];
+    // Whether a line that sees the tokens of `see` is known to see such a value of dimension `dim`, of which `k` is dim % (D / 64).
+    // All lanes come here together.
+    __device__ __forceinline__ bool seen(const KvSpan& see, uint32_t dim, int k) const
+    {
+        const int32_t a = __shfl(first[k], (int)(dim / (D / 64)), 64), z = __shfl(last[k], (int)(dim / (D / 64)), 64);
+        return (a >= see.lo && a < see.hi) || (z >= see.lo && z < see.hi);
+    }
+};
+template <class E, int D, int kBits>
+__device__ __forceinline__ Unfinite<D> find_unfinite(const AttendArgs& g, uint32_t seq, uint32_t head, const Range& range)
+{
+    Unfinite<D> u;
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) u.first[k] = u.last[k] = -1;
+#pragma unroll 1
+    for (int32_t t0 = range.lo; t0 < range.hi; t0 += 64) {
+        const Rows64<D, kBits> rows = rows_64<D, kBits>(g, seq, head, t0, range.hi);
+#pragma unroll 1
+        for (int i = 0; i < 64; i += 16) {
+            Dims<E, D, kBits> v[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = dims_of<E, D, kBits>(g.c.v, rows, i + j);
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+#pragma unroll
+                for (int k = 0; k < D / 64; ++k)
+                    if (!(fabsf(v[j].value(k)) < INFINITY) && (rows.held >> (i + j) & 1u)) {
+                        u.first[k] = u.first[k] < 0 ? t0 + i + j : u.first[k];
+                        u.last[k] = t0 + i + j;
+                    }
+        }
+    }
+    return u;
+}
+
+// `line_top`, `line_sum`: what the loops below have found, which stand for the logsumexp and for a part.  Scores are finite or minus
+// infinity here; values that are not finite are added as they are, whatever their weight.
 template <class E, int D, int kBits>
 __device__ __forceinline__ void plain_line(const AttendArgs& g, const KvSeq& seq_of, uint32_t seq, uint32_t head, uint32_t split, int32_t line, const Range& range,
                                            float line_top, float line_sum)
 {
+    constexpr int kPer = D / 64;
+    const uint32_t lane = lane_again();
     const int32_t row = line / (int32_t)g.group, h = line - row * (int32_t)g.group;
     const uint32_t q_head = head * g.group + (uint32_t)h;
     const uint64_t out_row = (uint64_t)(seq_of.row0 + row);
     const KvSpan see = kv_span(row, seq_of.rows, seq_of.len, g.window, g.all);
     const int32_t lo = see.lo > range.lo ? see.lo : range.lo, hi = see.hi < range.hi ? see.hi : range.hi;
     const uint8_t* const q = g.q + out_row * g.q_stride + (uint64_t)q_head * D * 2;
-    float top = -INFINITY, sum = 0.f, y[D / 64];
-    constexpr int kPer = D / 64;
-    const uint32_t lane = threadIdx.x & 63u;
-    const int32_t* const table = g.b.page_table + (uint64_t)seq * g.b.table_stride;
-    RowAt<kBits> at;                                                     // of this lane's token
-    bool there;
-    auto score = [&](int32_t t0) -> float {                              // times log2(e)
-        const int32_t t = t0 + (int32_t)lane < hi ? t0 + (int32_t)lane : hi - 1;
-        const uint32_t page = dev_load<uint32_t>(table + ((uint32_t)t >> g.c.page_shift));
-        there = t0 + (int32_t)lane < hi && page < g.c.n_pages;
-        at = row_at<D, kBits>(g.c, there ? page : 0u, (uint32_t)t, head);
+    float top = -INFINITY, sum = 0.f, y[kPer];
+    auto score = [&](const Rows64<D, kBits>& rows) -> float {            // of this lane's token, times log2(e)
         float s = 0.f;
-#pragma unroll 1
+#pragma unroll 4
         for (uint32_t c = 0; c < D / 8; ++c) {
             const u32x4 a = dev_load<u32x4>(q + c * 16);
             u32x4 k;
-            if constexpr (kBits == 16) k = dev_load<u32x4>(g.c.k + at.row + c * 16);
-            else k = decode8<E>(dev_load<uint32_t>(g.c.k + at.row + c * 4), scale_of(dev_load<uint8_t>(g.c.k + at.scale + c / 4)));
+            if constexpr (kBits == 16) k = dev_load<u32x4>(g.c.k + rows.at.row + c * 16);
+            else k = decode8<E>(dev_load<uint32_t>(g.c.k + rows.at.row + c * 4), scale_of(dev_load<uint8_t>(g.c.k + rows.at.scale + c / 4)));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s = fmaf(E::to_float(a[i] & 0xFFFFu), E::to_float(k[i] & 0xFFFFu), s);
                 s = fmaf(E::to_float(a[i] >> 16), E::to_float(k[i] >> 16), s);
             }
         }
-        return there ? s * g.to_log2 : -INFINITY;
+        return rows.held >> lane & 1u ? s * g.to_log2 : -INFINITY;
     };
 #pragma unroll 1
     for (int32_t t0 = lo; t0 < hi; t0 += 64) {
-        const float x = score(t0);
+        const float x = score(rows_64<D, kBits>(g, seq, head, t0, hi));
         float now = x;
 #pragma unroll
         for (int k = 1; k < 64; k <<= 1) now = fmaxf(now, __shfl_xor(now, k, 64));
@@ -262,32 +345,21 @@ __device__ __forceinline__ void plain_line(const AttendArgs& g, const KvSeq& seq
     for (int k = 0; k < kPer; ++k) y[k] = 0.f;
 #pragma unroll 1
     for (int32_t t0 = lo; t0 < hi; t0 += 64) {
-        const float w = __builtin_amdgcn_exp2f(score(t0) - top) * share;
-        const uint64_t held = __ballot(there);
+        const Rows64<D, kBits> rows = rows_64<D, kBits>(g, seq, head, t0, hi);
+        const float w = __builtin_amdgcn_exp2f(score(rows) - top) * share;
 #pragma unroll 1
-        for (int i = 0; i < 64; ++i) {
-            if (!((held >> i) & 1u)) continue;
-            const float wi = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), i));
-            const uint64_t row = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at.row >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at.row, i);
-            const uint8_t* p = g.c.v + row;
-            uint32_t v[(kPer + 1) / 2];                                  // dims kPer * lane ..
-            if constexpr (kBits == 16) {
-                if constexpr (kPer == 1) v[0] = dev_load<uint16_t>(p + lane * 2);
-                else
+        for (int i = 0; i < 64; i += 16) {
+            Dims<E, D, kBits> v[16];
 #pragma unroll
-                    for (int k = 0; k < kPer / 2; ++k) v[k] = dev_load<uint32_t>(p + (lane * kPer + 2 * k) * 2);
-            } else {
-                const uint64_t scales = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at.scale >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at.scale, i);
-                const float scale = scale_of(dev_load<uint8_t>(g.c.v + scales + lane * kPer / 32));
-                if constexpr (kPer == 1) v[0] = E::template decode2<0>(dev_load<uint8_t>(p + lane / 2), scale) >> (16 * (lane & 1u)) & 0xFFFFu;
-                else
+            for (int j = 0; j < 16; ++j) v[j] = dims_of<E, D, kBits>(g.c.v, rows, i + j);
 #pragma unroll
-                    for (int k = 0; k < kPer / 2; ++k) v[k] = E::template decode2<0>(dev_load<uint8_t>(p + lane * (kPer / 2) + k), scale);
-            }
+            for (int j = 0; j < 16; ++j) {
+                const float wj = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), i + j));
 #pragma unroll
-            for (int k = 0; k < kPer; ++k) {
-                const float x = E::to_float(v[k / 2] >> (16 * (k & 1)) & 0xFFFFu);
-                y[k] = fabsf(x) < INFINITY ? fmaf(wi, x, y[k]) : y[k] + x;
+                for (int k = 0; k < kPer; ++k) {
+                    const float x = v[j].value(k);
+                    if (rows.held >> (i + j) & 1u) y[k] = fabsf(x) < INFINITY ? fmaf(wj, x, y[k]) : y[k] + x;
+                }
             }
         }
     }
@@ -655,9 +727,18 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
             float x = 0.f;
 #pragma unroll
             for (uint32_t i = 0; i < kSeg; ++i) x = fmaf(y[i], 0.f, x);
-            const uint64_t here = __ballot(line < lines && total > 0.f && total < INFINITY && !(x == 0.f));
+            bool odd = line < lines && total > 0.f && total < INFINITY && !(x == 0.f);
+            if (__any(odd)) {
+                const AttendArgs& a = args_again();
+                const Unfinite<D> u = find_unfinite<E, D, kBits>(a, seq, head, range);
+                const KvSpan see_line = kv_span((line < lines ? line : 0) / (int32_t)a.group, q.rows, q.len, a.window, a.all);
+                bool more = false;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) large |= (uint64_t)((here >> (16 * i) & 0xFFFFu) != 0) << (rt * 16 + 4 * wave + i);
+                for (uint32_t i = 0; i < kSeg; ++i) more |= !u.seen(see_line, seg * kSeg + i, i % (D / 64)) && !(fabsf(y[i]) < INFINITY);
+                const uint64_t here = __ballot(odd && more);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) large |= (uint64_t)((here >> (16 * i) & 0xFFFFu) != 0) << (rt * 16 + 4 * wave + i);
+            }
         }
         if (line >= lines) continue;
         const bool stands = !(large >> line & 1u);                       // else plain_line stores it
@@ -1053,18 +1134,29 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
 #pragma unroll
             for (int i = 0; i < 16; ++i) x = fmaf(o[d][i], 0.f, x);
         x = sum_over32(x);
-        large = mine && sum > 0.f && sum < INFINITY && !(x == 0.f);
-        uint32_t lines_left = (uint32_t)__ballot(large);                 // the lower lanes: a line each
-        if (lines_left) {
+        const bool odd = mine && sum > 0.f && sum < INFINITY && !(x == 0.f);
+        if (__any(odd)) {
             const AttendArgs& a = args_again();
             const WideUnit u = wide_unit(a, a.first + blockIdx.x);
             const KvSeq q = kv_sequence(a.b, u.seq);
             const int32_t line0 = (int32_t)u.line_tile * kWideLines, lines = q.rows * (int32_t)a.group;
             const Range range = token_range(a, q, line0, line0 + kWideLines < lines ? line0 + kWideLines - 1 : lines - 1, u.split);
+            const Unfinite<D> unfinite = find_unfinite<E, D, kBits>(a, u.seq, u.head, range);
+            const int32_t first_line = line0 + (int32_t)wave * 32, my_line = first_line + (int32_t)(lane_again() & 31u);
+            const KvSpan see = kv_span(my_line < lines ? my_line / (int32_t)a.group : 0, q.rows, q.len, a.window, a.all);
+            bool more = false;
+#pragma unroll
+            for (int d = 0; d < kDims; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    more |= !unfinite.seen(see, d * 32 + (i >> 2) * 8 + upper * 4 + (i & 3), i % (D / 64)) && !(fabsf(o[d][i]) < INFINITY);
+            const uint64_t here = __ballot(odd && more);
+            uint32_t lines_left = (uint32_t)here | (uint32_t)(here >> 32);
+            large = lines_left >> m & 1u;
 #pragma unroll 1
             for (; lines_left; lines_left &= lines_left - 1) {
                 const int i = __builtin_ctz(lines_left);
-                plain_line<E, D, kBits>(a, q, u.seq, u.head, u.split, line0 + (int32_t)wave * 32 + i, range,
+                plain_line<E, D, kBits>(a, q, u.seq, u.head, u.split, first_line + i, range,
                                         __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), i)),
                                         __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(sum), i)));
             }
