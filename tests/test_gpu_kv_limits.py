@@ -155,6 +155,40 @@ def test_attend_values_near_the_ends_of_bfloat16(kv, rows, tokens, q_heads, head
     s.check_attend(out, lse)
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("rows,tokens,q_heads,heads,dim", [
+    ([3, 2], [300, 40], 4, 2, 64), ([100, 3], [300, 40], 4, 2, 128), ([40, 3], [300, 40], 4, 1, 256), ([4, 2], [2001, 1100], 4, 2, 128), ([60, 3], [2001, 1100], 4, 1, 128)])
+def test_large_values_beside_values_that_are_not_finite(kv, rows, tokens, q_heads, heads, dim, window, bits):
+    # dimensions whose sums pass 32 bits in rows that see infinities or NaN in others, of a first, a middle and a last token
+    s = Setup(kv, rows, tokens, BF16, bits, q_heads, heads, dim, 16, seed=dim)
+    s.v16 = (s.v16.double().clamp(-4, 4) * 2.0 ** 125).to(BF16)
+    s.v_pool = s.pool(s.v16)
+    s.cache = s.make_cache(s.k_pool, s.v_pool)
+    scale = 1 / math.sqrt(dim)
+    want, bound = (np.zeros((s.n_rows, q_heads, dim)) for _ in range(2))
+    for i, n in enumerate(rows):
+        at = slice(s.starts[i], s.starts[i] + n)
+        want[at], _, mass, size = R.attend(s.q[at].double().numpy(), s.held(s.k_pool, i), s.held(s.v_pool, i), scale, window, True)
+        bound[at] = R.attend_bounds(want[at], mass, size, tokens[i], dim, BF16)[0]
+    marked = [tokens[0] - rows[0] - 39, tokens[0] - rows[0] - 2, tokens[0] - 1]
+    dims = slice(5, 6) if bits == 16 else slice(32, 64)
+    for t in marked:
+        page, slot = int(s.table[0, t // 16]), t % 16
+        if bits == 16:
+            s.v_pool[page, slot, 0, dims] = math.nan
+        else:
+            s.v_pool[page, 16 * heads * dim // 2 + slot * heads * (dim // 32) + 1] = 255
+    out = kv.attend(s.cache, s.batch, s.q.cuda(), window=window).double().cpu().numpy()
+    hit = np.zeros(out.shape, bool)
+    for r in range(rows[0]):
+        hi = tokens[0] - rows[0] + r + 1
+        if any((hi - window if window else 0) <= t < hi for t in marked):
+            hit[r, :q_heads // heads, dims] = True
+    assert hit.any() and np.isnan(out[hit]).all()
+    assert (np.abs(out - want) <= bound)[~hit].all()
+
+
 @pytest.mark.parametrize("rows,tokens", [([4, 2], [300, 40]), ([100, 30], [300, 40]), ([60, 2], [9001, 4447]), ([4, 2], [9001, 4447])])
 def test_rows_that_do_not_see_large_values_do_not_change(kv, rows, tokens):
     s = Setup(kv, rows, tokens, BF16, 16, 4, 2, 128, 16, seed=2)
