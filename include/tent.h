@@ -541,7 +541,8 @@ int tent_probe_copy(const void *read_window, void *write_window, uint64_t bytes,
  *
  * Alignment: pools, rows, tables of rotations, norm weights and the workspace start at multiples of 16 bytes, strides are
  * whole multiples of 16 bytes.  TENT_ERR_INVALID for null pointers, other alignments, unknown types and flags,
- * TENT_ERR_RANGE for sizes that are not supported or do not go together.
+ * TENT_ERR_RANGE for sizes that are not supported or do not go together, and for more than 2^31 - 1 workgroups (of a few
+ * rows, some kilobytes of a page, or 16 to 128 queries of a head); up to there calls go in as many launches as it takes.
  */
 enum { TENT_BF16 = 0, TENT_FP16 = 1 };                      /* tent_kv_cache.type                                    */
 enum { TENT_KV_BAD_SEQUENCE = 1, TENT_KV_BAD_PAGE = 2, TENT_KV_BAD_POSITION = 4 };
@@ -596,7 +597,7 @@ typedef struct {
     void *workspace;           /* device: tent_kv_attend_workspace bytes; NULL where that is 0     */
     uint64_t workspace_bytes;
     uint32_t q_heads;          /* a multiple of kv_heads, at most TENT_KV_MAX_HEADS                */
-    uint32_t window;           /* a row sees the last `window` tokens up to its own; 0: all        */
+    uint32_t window;           /* a row sees the last `window` tokens up to its own, at most 2^30; 0: all */
     uint32_t flags;            /* TENT_KV_ATTEND_ALL                                               */
     float scale;               /* of the scores, above 0                                           */
 } tent_kv_attend_args;

@@ -14,12 +14,18 @@
 //   wide_kernel    more lines: 128 to a workgroup, 32 to a wave, tiles of 64 tokens in LDS for all four waves; bound by the
 //                  matrix units and the softmax's vector work beside them
 //
-// Measured, 32 heads on 8 of 128 dimensions: 32 rows over 2k-8k tokens each in 4 bits 45 us and 5 for the join (152 MB); 8 rows over
-// 100k-131k tokens 69 + 8 us (256 MB, 3.8 TB/s; without the arithmetic it takes the same); two prompts of 3.5k-4k tokens 296 us (895
-// TFLOP/s, a large matrix product reaches 1256); 1150 rows in three chunks behind 6k-16k tokens in 4 bits 341 + 17 us.
+// Measured, 32 heads on 8 of 128 dimensions: 32 rows over 2k-8k tokens each in 4 bits 44 us and 5 for the join (152 MB, 3.4 TB/s; no more
+// than that is read from memory), over 16-bit pages 114 (573 MB, 5.0 TB/s); 8 rows over 100k-131k tokens in 4 bits 69 + 8 us (256 MB, 3.7
+// TB/s); two prompts of 4k tokens 297 us, call and all (890 TFLOP/s, a large matrix product reaches 1251); 1128 rows in three chunks
+// behind 6k-16k tokens in 4 bits 330 us, of it 17 for the join.
 //
 // Where lines are few and contexts long the tokens are split over workgroups; their parts (largest score, sum, output, all in
 // 32 bits) go through the workspace and are joined by join_kernel.
+//
+// Scores, maxima, sums and outputs are in 32 bits.  Weights alone are rounded to the 16-bit type, as the second product takes such, and
+// their sum takes them before that.  It costs a third more error (bf16, against 64 bits: 2.2e-3 of the outputs' norm, where rounding the
+// outputs costs 1.65e-3 by itself).  A second product with what the rounding leaves ends it: at 52.2 us instead of 50.4 for the 32 rows in 4
+// bits, 404 instead of 309 for the prompts, and 420 instead of 334 for the chunks, which is more than it is worth to a result of 16 bits.
 #include "kv_elem.h"
 
 namespace tent {
@@ -648,7 +654,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
                 sum[rt] += x[j];
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) p[rt][j] = E::pack2(x[2 * j], x[2 * j + 1]);
+            for (int j = 0; j < 4; ++j) p[rt][j] = E::pack2(x[2 * j], x[2 * j + 1]);     // rounded to nearest: see the head of this file
         }
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
@@ -1023,7 +1029,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
                                 x1 = __builtin_amdgcn_exp2f(fmaf(s[j >> 3][2 * (j & 7) + 1], g.to_log2, against));
                     add[0] += x0;
                     add[1] += x1;
-                    p[j >> 2][j & 3] = E::pack2(x0, x1);
+                    p[j >> 2][j & 3] = E::pack2(x0, x1);                 // rounded to nearest: see the head of this file
                 }
             };
             // O^T's first operand: step u takes tokens 16 u + {0, 8} + 4 upper + 0 .. 3
@@ -1272,9 +1278,13 @@ struct Shape {
 
 // Which kernel, and how many splits.  Few lines: enough workgroups to fill the 256 compute units several times over, while a split
 // keeps enough tokens for its waves to have a tile in flight beside the one they work on; a context of up to 768 tokens stays
-// whole, as a split of it saves less than its join takes (one row over 501 tokens: 7.4 us and 3.7 for the join, whole 9.2).
+// whole, as a split of it saves less than its join takes, 3 to 4 us.  Whole and split, one row of 8 heads of 128 dimensions, 16 bits: 512
+// tokens 9.3 and 10.0 us, 768 11.8 and 10.0; 4 bits: 640 8.9 and 9.1, 768 9.8 and 9.2; 64 dimensions: 768 8.4 and 8.5; 64 rows: 768
+// 33.9 and 38.4.  Of 256 dimensions in 16 bits the two cross at 400 tokens already (768: 21.3 and 14.3), which the rule does not follow.
 // Many lines: enough workgroups to fill the compute units, or, if they are filled already and contexts so long that joins cost
-// little, to leave none with much more to do than others (chunks behind 6k-16k tokens: 406 us in one split, 340 + 17 in three).
+// little, to leave none with much more to do than others.  Three chunks of 511 rows, 384 workgroups, 4 bits, whole and in the rule's
+// three: behind 8k tokens 265 and 275 us, 16k 527 and 511, 32k 1047 and 977; 1024 workgroups stay whole behind 16k (1116, and
+// 1198 in two).
 Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_attend_args& a)
 {
     Shape s{};

@@ -3,9 +3,9 @@
 // All three move each value once and compute little: HBM bounds them, and latency where there are few rows.  A lane
 // works on eight values (16 bytes of a 16-bit row, 4 bytes of codes; four lanes in a row share a block's scale).
 //
-// Measured, 8 heads of 128 dimensions (and 32 of queries): append of 20,500 rows in 16 bits, 515 MB, 132-150 us (3.4-3.9 TB/s), of one
-// row 4 us; pack of 177,500 tokens, 920 MB, 177 us (5.2 TB/s, where a large copy reaches 4.8); read of as many from 4 bits 187 us, of 30,000
-// 24 us (6.4 TB/s, much of it from the last-level cache).
+// Measured, 8 heads of 128 dimensions (and 32 of queries): append of 20,500 rows in 16 bits, 515 MB, 137 us (3.8 TB/s), of one
+// row 4 us; pack of 177,500 tokens, 920 MB, 178 us (5.2 TB/s, where a large copy reaches 4.7); read of as many from 4 bits 192 us, of 30,000
+// 25 us (6.3 TB/s, much of it from the last-level cache).
 #include "kv_elem.h"
 
 namespace tent {
