@@ -58,7 +58,8 @@ struct AttendArgs {
     uint32_t first;                    // of the launch's workgroups
 };
 
-// A kernel's arguments, read anew: what hardly any call comes to should not keep them in registers all along.
+// The arguments of either kernel (each has this one structure), read anew: what hardly any call comes to should not keep them in
+// registers all along.
 __device__ __forceinline__ const AttendArgs& args_again()
 {
     typedef const __attribute__((address_space(4))) AttendArgs* ArgsAt;
