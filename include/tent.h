@@ -544,8 +544,8 @@ int tent_probe_copy(const void *read_window, void *write_window, uint64_t bytes,
  * TENT_ERR_RANGE for sizes that are not supported or do not go together, and for more than 2^31 - 1 workgroups (of a few
  * rows, some kilobytes of a page, or 16 to 128 queries of a head); up to there calls go in as many launches as it takes.
  */
-enum { TENT_BF16 = 0, TENT_FP16 = 1 };                      /* tent_kv_cache.type                                    */
-enum { TENT_KV_BAD_SEQUENCE = 1, TENT_KV_BAD_PAGE = 2, TENT_KV_BAD_POSITION = 4 };
+enum { TENT_BF16 = 0, TENT_FP16 = 1, TENT_FP32 = 2 };       /* tent_kv_cache.type: the first two; tent_kv_verify_args.type */
+enum { TENT_KV_BAD_SEQUENCE = 1, TENT_KV_BAD_PAGE = 2, TENT_KV_BAD_POSITION = 4, TENT_KV_BAD_TOKEN = 8 };
 enum { TENT_KV_MAX_HEADS = 1024, TENT_KV_MAX_PAGE_TOKENS = 1024 };
 enum { TENT_KV_ROPE_PAIRS = 1u << 0 };                      /* tent_kv_append_args.flags: rotate dims (2i, 2i+1)     */
 enum { TENT_KV_ATTEND_ALL = 1u << 0 };                      /* tent_kv_attend_args.flags: no row is causal           */
@@ -637,6 +637,124 @@ int tent_kv_attend_workspace(const tent_kv_cache *cache, const tent_kv_batch *ba
  * not see have no influence on it, whatever their values.  Scores and sums are 32 bits, weights are rounded to the
  * 16-bit type (to nearest) before they multiply the values. */
 int tent_kv_attend(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_attend_args *args, void *stream);
+
+/*
+ * Drafted tokens, and eviction.
+ *
+ * A step may append more tokens than will stand: the rows of a sequence are then its last decided token and tokens drafted
+ * behind it, in a row or as a tree.  tent_kv_attend_tree lets each row see the context and its own branch,
+ * tent_kv_verify finds which rows stand, given the target's probabilities and random numbers, and tent_kv_keep makes those the
+ * sequence.  A cache that gets too long is cut the same way: tent_kv_weigh adds up the attention that every token has got, tent_kv_choose
+ * says which tokens a sequence keeps, tent_kv_keep moves them together.  Everything said above of rows, errors, alignment, streams
+ * and graphs holds for them; none takes atomics but the error bits, so results repeat bit for bit.
+ */
+enum { TENT_KV_KEEP_ROWS = 1u << 0 };                       /* tent_kv_keep_args.flags: lists name rows, not tokens   */
+enum { TENT_KV_MAX_VOCAB = 1 << 24 };
+
+typedef struct {
+    const uint64_t *masks;     /* device [n_rows][mask_stride]: bit j of a row's words: it sees row j of its sequence */
+    uint32_t mask_stride;      /* words from a row's to the next's, at least max_rows / 64         */
+    uint32_t reserved;         /* 0                                                                */
+} tent_kv_tree;
+
+typedef struct {
+    const void *target;        /* device [n_rows][vocab]: probabilities of the token behind each row */
+    const void *draft;         /* device [n_rows][vocab]: those that the tokens behind each row were drawn from; NULL: they were chosen */
+    uint64_t target_stride, draft_stride;   /* values from a row to the next, at least vocab       */
+    const int32_t *tokens;     /* device [n_rows]: a row's token (the first row's is not read)      */
+    const int32_t *parents;    /* device [n_rows]: the row of its sequence that a row is behind; NULL: the one before */
+    const float *accept, *next;        /* device [n_rows] and [n_seqs]: random numbers, 0 <= u < 1   */
+    int32_t *path;             /* device [n_seqs][path_stride]: the rows that stand, then -1 up to max_rows */
+    int32_t *counts;           /* device [n_seqs]: how many stand, the first row among them         */
+    int32_t *token;            /* device [n_seqs]: the token behind the last of them                */
+    void *workspace;           /* device: tent_kv_verify_workspace bytes; NULL where that is 0      */
+    uint64_t workspace_bytes;
+    uint32_t vocab;            /* 1 .. TENT_KV_MAX_VOCAB                                            */
+    uint32_t path_stride;      /* at least max_rows                                                */
+    uint32_t type;             /* TENT_BF16, TENT_FP16 or TENT_FP32: of the probabilities          */
+    uint32_t reserved;         /* 0                                                                */
+} tent_kv_verify_args;
+
+typedef struct {
+    const void *q;             /* device [n_rows][q_heads][head_dim]                               */
+    const float *lse;          /* device [n_rows][q_heads], as tent_kv_attend has given them        */
+    const float *weights;      /* device [n_seqs][n_lists][weights_stride]: so far, or NULL: 0      */
+    float *weights_out;        /* device, laid out the same; may be `weights`                      */
+    uint64_t q_stride;         /* values from a row to the next                                    */
+    uint64_t weights_stride;   /* values from a list to the next, at least max_kv                  */
+    uint32_t q_heads;          /* a multiple of kv_heads, at most TENT_KV_MAX_HEADS                */
+    uint32_t n_lists;          /* kv_heads: weights by head of the cache; 1: of all of them         */
+    uint32_t window, flags;    /* as tent_kv_attend had them                                       */
+    float scale;               /* likewise                                                         */
+    uint32_t reserved;         /* 0                                                                */
+} tent_kv_weigh_args;
+
+typedef struct {
+    const float *weights;      /* device [n_seqs][n_lists][weights_stride]                         */
+    int32_t *lists;            /* device [n_seqs][n_lists][list_stride]: tokens, ascending, then -1 up to budget */
+    int32_t *counts;           /* device [n_seqs]: how many of them                                 */
+    uint64_t weights_stride, list_stride;   /* values, at least max_kv, and at least budget        */
+    uint32_t n_lists;          /* 1 .. TENT_KV_MAX_HEADS                                           */
+    uint32_t budget;           /* tokens to keep, 1 .. 2^30                                        */
+    uint32_t first, recent;    /* that many first and last tokens are kept whatever their weights: budget at most */
+} tent_kv_choose_args;
+
+typedef struct {
+    const int32_t *lists;      /* device [n_seqs][n_lists][list_stride]                            */
+    const int32_t *counts;     /* device [n_seqs]: entries of a sequence's lists                   */
+    const int32_t *to_table;   /* device [n_seqs][to_stride]: pages that the kept tokens go to; NULL: the batch's, in place */
+    int32_t *kv_len_out;       /* device [n_seqs]: tokens afterwards; not the batch's kv_len       */
+    const float *weights;      /* device [n_seqs][n_weights][weights_stride]: moved with the tokens; or NULL */
+    float *weights_out;        /* device, laid out the same; in place it may be `weights`          */
+    uint64_t list_stride;      /* entries from a list to the next                                  */
+    uint64_t weights_stride;   /* values, at least max_kv                                          */
+    uint32_t n_lists;          /* kv_heads: a list for every head of the cache; 1: one for all      */
+    uint32_t n_weights;        /* kv_heads or 1; 1 with a list for every head is refused            */
+    uint32_t to_stride;        /* entries from a sequence's pages in to_table to the next's        */
+    uint32_t most;             /* most entries of a list, at most list_stride                      */
+    uint32_t flags;            /* TENT_KV_KEEP_ROWS                                                */
+    uint32_t reserved;         /* 0                                                                */
+} tent_kv_keep_args;
+
+/* tent_kv_attend for rows that are a tree (or anything else that masks say): with base = kv_len - its sequence's rows, a row sees the
+ * context, tokens 0 .. base - 1, and token base + j where bit j of its mask is set and row j is one of its sequence.  Of a window (at
+ * least max_rows, else TENT_ERR_RANGE) the rows that its mask names come first, the last tokens of the context have the rest.
+ * TENT_KV_ATTEND_ALL is refused.  The workspace is tent_kv_attend_workspace's. */
+int tent_kv_attend_tree(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_attend_args *args, const tent_kv_tree *tree,
+                        void *stream);
+
+/* Which rows of a sequence stand, and the token behind them.  The first row stands.  From the row c that stands last the rows behind it
+ * are tried in their order: row i with token x stands if accept[i] * draft[c][x] < r[x], and then it is tried from there; r is target[c]
+ * at first, and after each row that does not stand max(r - draft[c], 0) over its sum.  So the tokens are as drawn from `target`,
+ * given that each row was drawn from `draft` by itself.  Without `draft` a row stands if accept[i] * m < r[x], where m is 1 at first; one
+ * that does not takes r[x] off m and its token out of r.  Rows whose parent is none before them are behind none.  When no row is left
+ * the token is the least t with r[0] + .. + r[t] > next * (r[0] + ..); should r be all zeros then target[c] takes its place, and -1 stands
+ * for the token if that is all zeros too.  Sums and r are 64 bits.  Probabilities that are negative, infinite or NaN count as 0, and so do
+ * those of a token outside 0 .. vocab - 1, which is noted (TENT_KV_BAD_TOKEN).  A sequence of no rows, or one that is left out, gets count 0, token -1
+ * and a path of -1. */
+int tent_kv_verify(const tent_kv_batch *batch, const tent_kv_verify_args *args, void *stream);
+int tent_kv_verify_workspace(const tent_kv_batch *batch, const tent_kv_verify_args *args, uint64_t *bytes);
+
+/* Attention weights onto the tokens: weights_out[s][l][t] = weights[s][l][t] + the sum over the rows that see token t, and the query heads
+ * that read head l (with one list all of them), of exp(scale q . k_t - lse).  Written for all t below max_kv: where nothing sees a
+ * token its weight stays.  Rows whose lse is not finite add nothing.  A sequence that is left out, or has no rows, keeps its weights. */
+int tent_kv_weigh(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_weigh_args *args, void *stream);
+
+/* Which tokens every sequence keeps: all where it has no more than `budget`; else its first `first` and last `recent` ones, and
+ * of the others those with the greatest weights, of equal ones the first (NaN counts as minus infinity).  Takes n_seqs, kv_len and max_kv
+ * of the batch, no pages.  A sequence that is left out gets count 0. */
+int tent_kv_choose(const tent_kv_batch *batch, const tent_kv_choose_args *args, void *stream);
+
+/* Token j becomes what token lists[s][l][j] was, for j < counts[s] and head l (with one list every head): K, V, and `weights` if
+ * given, whose places behind the last kept token up to max_kv become 0.  kv_len_out is counts[s].  With TENT_KV_KEEP_ROWS lists name rows:
+ * with base = kv_len - its rows, token base + j becomes what token base + lists[s][l][j] was, and kv_len_out is base + counts[s].
+ * In place an entry must not be below its own number j, so that lists may name a token twice and nothing is read that was written;
+ * with to_table, whose pages must not be ones that are read, entries may be anything below kv_len (below the rows).  An entry that is not
+ * is left out and noted (TENT_KV_BAD_POSITION); wrong pages likewise.  A sequence with a count that is negative, more than
+ * `most`, or more than it has (in place), with
+ * rows of which some are at negative positions, and one that is left out, stay as they are, with their kv_len, noted as
+ * TENT_KV_BAD_SEQUENCE. */
+int tent_kv_keep(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_keep_args *args, void *stream);
 
 /* Static description of a status code. */
 const char *tent_strerror(int status);

@@ -29,7 +29,8 @@ EXPORTS = ["tent_create", "tent_destroy", "tent_register_segment", "tent_declare
            "tent_get_plan", "tent_get_timings", "tent_release", "tent_strerror",
            "tent_sim_fail", "tent_get_retries", "tent_monitor_init", "tent_monitor_update",
            "tent_plan_dispatch", "tent_get_modes", "tent_execute_bounded", "tent_probe_copy", "tent_declare_static",
-           "tent_kv_packed_page", "tent_kv_append", "tent_kv_pack", "tent_kv_read", "tent_kv_attend_workspace", "tent_kv_attend"]
+           "tent_kv_packed_page", "tent_kv_append", "tent_kv_pack", "tent_kv_read", "tent_kv_attend_workspace", "tent_kv_attend",
+           "tent_kv_attend_tree", "tent_kv_verify_workspace", "tent_kv_verify", "tent_kv_weigh", "tent_kv_choose", "tent_kv_keep"]
 
 
 class tent_config(C.Structure):
@@ -58,10 +59,11 @@ SLICE_DTYPE = np.dtype(
 
 
 # Operators on paged key/value caches (kv.py passes tensors to them)
-TENT_BF16, TENT_FP16 = 0, 1
-TENT_KV_BAD_SEQUENCE, TENT_KV_BAD_PAGE, TENT_KV_BAD_POSITION = 1, 2, 4
+TENT_BF16, TENT_FP16, TENT_FP32 = 0, 1, 2
+TENT_KV_BAD_SEQUENCE, TENT_KV_BAD_PAGE, TENT_KV_BAD_POSITION, TENT_KV_BAD_TOKEN = 1, 2, 4, 8
 TENT_KV_MAX_HEADS, TENT_KV_MAX_PAGE_TOKENS = 1024, 1024
-TENT_KV_ROPE_PAIRS, TENT_KV_ATTEND_ALL = 1, 1
+TENT_KV_MAX_VOCAB = 1 << 24
+TENT_KV_ROPE_PAIRS, TENT_KV_ATTEND_ALL, TENT_KV_KEEP_ROWS = 1, 1, 1
 
 
 class tent_kv_cache(C.Structure):
@@ -88,6 +90,34 @@ class tent_kv_attend_args(C.Structure):
     _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("q_stride", C.c_uint64), ("out_stride", C.c_uint64),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("q_heads", C.c_uint32), ("window", C.c_uint32),
                 ("flags", C.c_uint32), ("scale", C.c_float)]
+
+
+class tent_kv_tree(C.Structure):
+    _fields_ = [("masks", C.c_void_p), ("mask_stride", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tent_kv_verify_args(C.Structure):
+    _fields_ = [("target", C.c_void_p), ("draft", C.c_void_p), ("target_stride", C.c_uint64), ("draft_stride", C.c_uint64),
+                ("tokens", C.c_void_p), ("parents", C.c_void_p), ("accept", C.c_void_p), ("next", C.c_void_p),
+                ("path", C.c_void_p), ("counts", C.c_void_p), ("token", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("vocab", C.c_uint32), ("path_stride", C.c_uint32), ("type", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tent_kv_weigh_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("lse", C.c_void_p), ("weights", C.c_void_p), ("weights_out", C.c_void_p), ("q_stride", C.c_uint64),
+                ("weights_stride", C.c_uint64), ("q_heads", C.c_uint32), ("n_lists", C.c_uint32), ("window", C.c_uint32),
+                ("flags", C.c_uint32), ("scale", C.c_float), ("reserved", C.c_uint32)]
+
+
+class tent_kv_choose_args(C.Structure):
+    _fields_ = [("weights", C.c_void_p), ("lists", C.c_void_p), ("counts", C.c_void_p), ("weights_stride", C.c_uint64),
+                ("list_stride", C.c_uint64), ("n_lists", C.c_uint32), ("budget", C.c_uint32), ("first", C.c_uint32), ("recent", C.c_uint32)]
+
+
+class tent_kv_keep_args(C.Structure):
+    _fields_ = [("lists", C.c_void_p), ("counts", C.c_void_p), ("to_table", C.c_void_p), ("kv_len_out", C.c_void_p), ("weights", C.c_void_p),
+                ("weights_out", C.c_void_p), ("list_stride", C.c_uint64), ("weights_stride", C.c_uint64), ("n_lists", C.c_uint32),
+                ("n_weights", C.c_uint32), ("to_stride", C.c_uint32), ("most", C.c_uint32), ("flags", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 class TentError(RuntimeError):
@@ -150,6 +180,12 @@ def lib():
         L.tent_kv_read.argtypes = [cache, batch, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
         L.tent_kv_attend_workspace.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.POINTER(C.c_uint64)]
         L.tent_kv_attend.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.c_void_p]
+        L.tent_kv_attend_tree.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.POINTER(tent_kv_tree), C.c_void_p]
+        L.tent_kv_verify_workspace.argtypes = [batch, C.POINTER(tent_kv_verify_args), C.POINTER(C.c_uint64)]
+        L.tent_kv_verify.argtypes = [batch, C.POINTER(tent_kv_verify_args), C.c_void_p]
+        L.tent_kv_weigh.argtypes = [cache, batch, C.POINTER(tent_kv_weigh_args), C.c_void_p]
+        L.tent_kv_choose.argtypes = [batch, C.POINTER(tent_kv_choose_args), C.c_void_p]
+        L.tent_kv_keep.argtypes = [cache, batch, C.POINTER(tent_kv_keep_args), C.c_void_p]
         _lib = L
     return _lib
 
@@ -387,3 +423,29 @@ def tent_kv_attend_workspace(cache: tent_kv_cache, batch: tent_kv_batch, args: t
 
 def tent_kv_attend(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_attend_args, stream=None):
     _check(lib().tent_kv_attend(cache, batch, args, _stream(stream)), "tent_kv_attend")
+
+
+def tent_kv_attend_tree(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_attend_args, tree: tent_kv_tree, stream=None):
+    _check(lib().tent_kv_attend_tree(cache, batch, args, tree, _stream(stream)), "tent_kv_attend_tree")
+
+
+def tent_kv_verify_workspace(batch: tent_kv_batch, args: tent_kv_verify_args) -> int:
+    n = C.c_uint64()
+    _check(lib().tent_kv_verify_workspace(batch, args, n), "tent_kv_verify_workspace")
+    return n.value
+
+
+def tent_kv_verify(batch: tent_kv_batch, args: tent_kv_verify_args, stream=None):
+    _check(lib().tent_kv_verify(batch, args, _stream(stream)), "tent_kv_verify")
+
+
+def tent_kv_weigh(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_weigh_args, stream=None):
+    _check(lib().tent_kv_weigh(cache, batch, args, _stream(stream)), "tent_kv_weigh")
+
+
+def tent_kv_choose(batch: tent_kv_batch, args: tent_kv_choose_args, stream=None):
+    _check(lib().tent_kv_choose(batch, args, _stream(stream)), "tent_kv_choose")
+
+
+def tent_kv_keep(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_keep_args, stream=None):
+    _check(lib().tent_kv_keep(cache, batch, args, _stream(stream)), "tent_kv_keep")

@@ -32,11 +32,11 @@ __device__ __forceinline__ void dev_stream(void* p, V v) { __builtin_nontemporal
 // A multiple of eight: workgroups keep their XCDs.
 constexpr uint32_t kMostBlocks = 1u << 23;
 template <class Launch>
-int launch_blocks(uint64_t blocks, Launch launch)
+int launch_blocks(uint64_t blocks, Launch launch, uint32_t most = kMostBlocks)
 {
     if (blocks > 0x7FFFFFFFull) return TENT_ERR_RANGE;
-    for (uint64_t first = 0; first < blocks; first += kMostBlocks) {
-        launch((uint32_t)first, (uint32_t)(blocks - first < kMostBlocks ? blocks - first : kMostBlocks));
+    for (uint64_t first = 0; first < blocks; first += most) {
+        launch((uint32_t)first, (uint32_t)(blocks - first < most ? blocks - first : most));
         if (hipGetLastError() != hipSuccess) return TENT_ERR_HIP;
     }
     return TENT_OK;

@@ -52,6 +52,21 @@ inline int kv_check_batch(const tent_kv_cache* c, const tent_kv_batch* b)
     return TENT_OK;
 }
 
+// The sequences of a batch, for calls that take no pages or need no rows.
+inline int kv_check_sequences(const tent_kv_batch* b)
+{
+    if (!b || b->reserved) return TENT_ERR_INVALID;
+    if (b->n_seqs == 0) return TENT_OK;
+    if (!b->kv_len || !b->row_start || (((uintptr_t)b->kv_len | (uintptr_t)b->row_start | (uintptr_t)b->errors) & 3u)) return TENT_ERR_INVALID;
+    if (b->n_seqs > 65535 || b->n_rows > 0x7FFFFFFFu || (b->n_rows && (b->max_rows < 1 || b->max_rows > b->n_rows)) || b->max_kv > (1u << 30)) return TENT_ERR_RANGE;
+    return TENT_OK;
+}
+inline int kv_check_table(const tent_kv_cache* c, const tent_kv_batch* b)
+{
+    if (!b->page_table || ((uintptr_t)b->page_table & 3u)) return TENT_ERR_INVALID;
+    return b->max_kv > (uint64_t)b->table_stride * c->page_tokens ? TENT_ERR_RANGE : TENT_OK;
+}
+
 // Rows of `heads` heads: a base, and a stride that holds them, in whole vectors of 16 bytes.
 inline int kv_check_rows(const void* p, uint64_t stride, uint32_t heads, uint32_t head_dim, uint32_t n_rows)
 {
@@ -104,6 +119,28 @@ TENT_KV_BOTH KvSpan kv_span(int32_t row, int32_t rows, int32_t len, uint32_t win
     if (hi <= 0) return KvSpan{0, 0};
     const int32_t lo = window && window < (uint32_t)hi ? hi - (int32_t)window : 0;
     return KvSpan{lo, hi};
+}
+
+// What a row of a tree sees: the context from lo to base, and of the rows, tokens base to len, those that its mask names (`words` of it).
+// Of a window the context has what the `deep` rows that it sees leave.
+struct KvTreeSpan { int32_t lo, base, len, words; };
+TENT_KV_BOTH KvTreeSpan kv_tree_span(int32_t rows, int32_t len, uint32_t window, int32_t deep)
+{
+    const int32_t base = len - rows, lo = window ? base + deep - (int32_t)window : 0;
+    return KvTreeSpan{lo > 0 ? lo : 0, base, len, (rows + 63) >> 6};
+}
+// The 64 tokens from t0 on as bits; word(i): 64 rows of the mask, 0 for those past the last.
+template <class Word>
+TENT_KV_BOTH uint64_t kv_tree_bits(const KvTreeSpan& s, int32_t t0, Word word)
+{
+    const int32_t at = t0 - s.base;                                      // of the first among the rows
+    uint64_t bits = at <= -64 ? ~0ull : at < 0 ? ~(~0ull << -at) : 0;
+    if (s.lo > t0) bits = s.lo < t0 + 64 ? bits & ~0ull << (s.lo - t0) : 0;
+    if (at > -64) {
+        if (at < 0) bits |= word(0) << -at;
+        else bits |= word(at >> 6) >> (at & 63) | (at & 63 ? word((at >> 6) + 1) << (64 - (at & 63)) : 0);
+    }
+    return bits;
 }
 
 }  // namespace tent

@@ -1,4 +1,4 @@
-"""Paged key/value caches as tensors: append, pack, read and attend.
+"""Paged key/value caches as tensors: append, pack, read and attend; verify, weigh, choose and keep.
 
 The operators behind ``tent_kv_*`` (include/tent.h) with torch tensors for their device memory: ``Cache`` describes the
 pools, ``Batch`` the sequences of a step, and the functions check their tensors, allocate what they return and enqueue on
@@ -10,6 +10,9 @@ and what it returns is kept from being allocated again before both streams are d
 when `stream` gets to it, and its outputs before they are used elsewhere, is for the caller to order.
 
 There is no backward pass.  A tensor that requires gradients is refused while they are recorded (not under torch.no_grad()).
+
+Speculative decoding: append the drafted tokens behind the last decided one, attend with tree= (``tree_masks``), verify, keep
+with rows=True.  Eviction: weigh after attention, choose, keep.
 
 A cache of 16 bits is two tensors [pages, page_tokens, kv_heads, head_dim] of bfloat16 or float16; one of 4 bits is two
 uint8 tensors [pages, bytes] (``packed_pool``), whose pages hold 32 values to a shared power of two.  Pages are contiguous
@@ -114,6 +117,29 @@ def rope_table(n_positions: int, rope_dim: int, base: float = 10000.0, device="c
     rate = float(base) ** (-torch.arange(half, dtype=torch.float64, device=device) / half)
     angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * rate
     return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def tree_masks(parents, row_start, max_rows: int):
+    """What attend's `tree` takes for a tree: bits [rows, words] (int64) of the rows that each row sees, itself and those on the way
+    to it, and how far down each row is [rows] (int32; what to add to the context's length for its position).
+
+    parents: int32 [rows], the row of its sequence that a row is behind (verify's); a row that is behind none before it is a
+    root.  row_start: int32 [sequences + 1]."""
+    n, words, device = parents.shape[0], max(1, -(-max_rows // 64)), parents.device
+    row = torch.arange(n, device=device)
+    first = row_start.long()[torch.bucketize(row, row_start[1:].long(), right=True).clamp(max=max(row_start.shape[0] - 2, 0))]
+    local = row - first
+    up = torch.where((parents >= 0) & (parents < local), first + parents, -1)            # the row above, then the one 2, 4, .. up
+    bit = torch.ones((), dtype=torch.int64, device=device) << (local & 63)
+    masks = torch.where(torch.arange(words, device=device) == (local >> 6)[:, None], bit[:, None], 0)
+    reach = torch.ones(n, dtype=torch.int32, device=device)
+    for _ in range(max(max_rows - 1, 0).bit_length()):
+        there = up >= 0
+        at = up.clamp(min=0)
+        masks = masks | torch.where(there[:, None], masks[at], 0)
+        reach = reach + torch.where(there, reach[at], 0)
+        up = torch.where(there, up[at], -1)
+    return masks, reach - 1
 
 
 class Cache:
@@ -276,14 +302,16 @@ def read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None):
 
 
 def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, causal: bool = True, out=None, want_lse: bool = False,
-           workspace=None, stream=None):
+           workspace=None, stream=None, tree=None):
     """Attention of the batch's rows over their sequences: [rows, q_heads, head_dim], and with `want_lse` the logsumexp of the
     scores [rows, q_heads] in float32.  scale: 1 / sqrt(head_dim) unless given; window: a row sees its last `window` tokens;
     causal=False: every row sees its whole sequence.  workspace: a contiguous uint8 tensor of at least attend_workspace
-    bytes to use instead of a new one."""
+    bytes to use instead of a new one.  tree: int64 [rows, words], a row sees the context in front of its sequence's rows and
+    those of them whose bits are set in its words (``tree_masks``); a window has to be max_rows at least then."""
     if stream is not None or cache.index != _current_device():
-        return _on(cache.device, stream, (*cache.tensors, *batch.tensors, q, out, workspace),
-                   lambda: attend(cache, batch, q, scale, window, causal, out, want_lse, workspace))
+        used = (*cache.tensors, *batch.tensors, q, out, workspace)
+        return _on(cache.device, stream, used if tree is None else (*used, tree),
+                   lambda: attend(cache, batch, q, scale, window, causal, out, want_lse, workspace, tree=tree))
     _together(cache, batch)
     n, D, dtype, device = batch.n_rows, cache.head_dim, cache.dtype, cache.device
     heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
@@ -294,6 +322,12 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
         out_stride = _rows(out, "out", dtype, n, heads, D, device)
     if not 0 <= window < 1 << 31:
         raise ValueError("window must be 0 or more and below 2^31")
+    if tree is not None:
+        _on_gpu(tree, "tree", torch.int64)
+        if tree.device != device or tree.dim() != 2 or tree.shape[0] != n or not tree.is_contiguous():
+            raise ValueError("tree must be contiguous [rows, words] on the cache's device")
+        if not causal:
+            raise ValueError("a tree says what each row sees: causal stays True")
     lse = torch.empty((n, heads), dtype=torch.float32, device=device) if want_lse else None
     a = T.tent_kv_attend_args(q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else None, q_stride, out_stride, None, 0, heads, window,
                               0 if causal else T.TENT_KV_ATTEND_ALL, 1.0 / math.sqrt(D) if scale is None else scale)
@@ -305,7 +339,11 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
         elif not _on_gpu(workspace, "workspace", torch.uint8).is_contiguous() or workspace.device != device:
             raise ValueError("workspace must be contiguous, on the cache's device")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(L.tent_kv_attend(cache.ref, batch.ref, ref, _stream(cache.index)), "tent_kv_attend")
+    if tree is None:
+        _check(L.tent_kv_attend(cache.ref, batch.ref, ref, _stream(cache.index)), "tent_kv_attend")
+    else:
+        masks = T.tent_kv_tree(tree.data_ptr(), tree.shape[1], 0)
+        _check(L.tent_kv_attend_tree(cache.ref, batch.ref, ref, C.byref(masks), _stream(cache.index)), "tent_kv_attend_tree")
     return (out, lse) if want_lse else out
 
 
@@ -314,3 +352,179 @@ def attend_workspace(cache: Cache, batch: Batch, q_heads: int, window: int = 0, 
     _together(cache, batch)
     return T.tent_kv_attend_workspace(cache.c, batch.c, T.tent_kv_attend_args(q_heads=q_heads, window=window, scale=1.0,
                                                                              flags=0 if causal else T.TENT_KV_ATTEND_ALL))
+
+
+_PROBABILITIES = {**_TYPES, torch.float32: T.TENT_FP32}
+
+
+def _vector(tensor, name, dtype, n, device):
+    """A contiguous tensor of `n` values on `device`; its address."""
+    if not _on_gpu(tensor, name, dtype, (n,)).is_contiguous() or tensor.device != device:
+        raise ValueError(f"{name} must be contiguous, on the batch's device")
+    return tensor.data_ptr()
+
+
+def _by_list(tensor, name, dtype, n_seqs, width, device):
+    """A tensor [sequences, values] or [sequences, heads, values] of `width` values at least, lists at one distance; heads, distance."""
+    _on_gpu(tensor, name, dtype)
+    if tensor.device != device or tensor.dim() not in (2, 3) or tensor.shape[0] != n_seqs or tensor.shape[-1] < width:
+        raise ValueError(f"{name} must be [sequences, (heads,) values] with {width} values at least, on the batch's device, not {tuple(tensor.shape)}")
+    lists, stride = tensor.shape[1] if tensor.dim() == 3 else 1, tensor.stride()
+    apart = stride[1] if tensor.dim() == 3 and lists > 1 else stride[0] if n_seqs > 1 else tensor.shape[-1]
+    if (tensor.shape[-1] > 1 and stride[-1] != 1) or (n_seqs > 1 and stride[0] != lists * apart) or apart < tensor.shape[-1]:
+        raise ValueError(f"{name} must have lists of contiguous values, all as far apart (strides {stride})")
+    return lists, apart
+
+
+def _like(tensor, lists, apart, known):
+    """A new tensor laid out as one that _by_list has seen, with its values from place `known` of a list on."""
+    shape = (tensor.shape[0], apart) if tensor.dim() == 2 else (tensor.shape[0], lists, apart)
+    out = torch.empty(shape, dtype=tensor.dtype, device=tensor.device)
+    if apart > tensor.shape[-1]:
+        out = out[..., :tensor.shape[-1]]
+    if tensor.shape[-1] > known:
+        out[..., known:] = tensor[..., known:]
+    return out
+
+
+def verify(batch: Batch, target, tokens, accept, next, parents=None, draft=None, path=None, workspace=None, stream=None):
+    """Which of the batch's rows stand, and what comes behind them: path [sequences, max_rows] (int32, rows of the sequence, the first of
+    them first, then -1), counts [sequences] and token [sequences].
+
+    target: [rows, vocab], probabilities of the token behind each row, float32, bfloat16 or float16.  tokens: int32 [rows], drafted
+    tokens, of which the first of a sequence stands for the one that is decided already.  parents: int32 [rows], the row of its
+    sequence that a row is behind; the one before unless given.  draft: as target, the probabilities that the rows behind a row
+    were drawn from, each by itself; None: they were chosen without drawing.  accept: float32 [rows] and next: float32 [sequences],
+    random numbers, 0 <= u < 1.  workspace: a contiguous uint8 tensor of at least verify_workspace bytes to use instead of a new one."""
+    if stream is not None or batch.device.index != _current_device():
+        used = [x for x in (*batch.tensors, target, tokens, accept, next, parents, draft, path, workspace) if x is not None]
+        return _on(batch.device, stream, used, lambda: verify(batch, target, tokens, accept, next, parents, draft, path, workspace))
+    n, n_seqs, most, device = batch.n_rows, batch.c.n_seqs, batch.c.max_rows, batch.device
+    if not isinstance(target, torch.Tensor) or target.dim() != 2 or target.dtype not in _PROBABILITIES:
+        raise ValueError("target must be float32, bfloat16 or float16 [rows, vocab]")
+    vocab, strides = target.shape[1], []
+    for x, name in ((target, "target"), (draft, "draft")):
+        if x is None:
+            strides.append(0)
+            continue
+        _on_gpu(x, name, target.dtype, (n, vocab))
+        if x.device != device or (vocab > 1 and x.stride(1) != 1) or (n > 1 and x.stride(0) < vocab):
+            raise ValueError(f"{name} must have contiguous rows, on the batch's device")
+        strides.append(x.stride(0) if n > 1 else vocab)
+    a = T.tent_kv_verify_args(target.data_ptr(), draft.data_ptr() if draft is not None else None, *strides, _vector(tokens, "tokens", torch.int32, n, device),
+                              _vector(parents, "parents", torch.int32, n, device) if parents is not None else None,
+                              _vector(accept, "accept", torch.float32, n, device), _vector(next, "next", torch.float32, n_seqs, device))
+    if path is None:
+        path = torch.empty((n_seqs, most), dtype=torch.int32, device=device)
+    elif not _on_gpu(path, "path", torch.int32, (n_seqs, most)).is_contiguous() or path.device != device:
+        raise ValueError("path must be contiguous, on the batch's device")
+    counts, token = torch.empty((n_seqs,), dtype=torch.int32, device=device), torch.empty((n_seqs,), dtype=torch.int32, device=device)
+    a.path, a.counts, a.token = path.data_ptr(), counts.data_ptr(), token.data_ptr()
+    a.vocab, a.path_stride, a.type = vocab, most, _PROBABILITIES[target.dtype]
+    L, need, ref = T.lib(), C.c_uint64(), C.byref(a)
+    _check(L.tent_kv_verify_workspace(batch.ref, ref, C.byref(need)), "tent_kv_verify_workspace")
+    if need.value:
+        if workspace is None:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+        elif not _on_gpu(workspace, "workspace", torch.uint8).is_contiguous() or workspace.device != device:
+            raise ValueError("workspace must be contiguous, on the batch's device")
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(L.tent_kv_verify(batch.ref, ref, _stream(device.index)), "tent_kv_verify")
+    return path, counts, token
+
+
+def verify_workspace(batch: Batch, vocab: int, parents: bool = False, draft: bool = False) -> int:
+    """Bytes of workspace that verify takes for such a batch, with or without `parents` and `draft`."""
+    return T.tent_kv_verify_workspace(batch.c, T.tent_kv_verify_args(vocab=vocab, parents=4 if parents else None, draft=4 if draft else None, type=T.TENT_FP32))
+
+
+def weigh(cache: Cache, batch: Batch, q, lse, weights=None, per_head: bool = True, scale: float = None, window: int = 0, causal: bool = True, out=None,
+          stream=None):
+    """`weights` and what the batch's rows add to them: the attention weight that each token gets from the rows that see it, [sequences,
+    kv_heads, max_kv] (float32; summed over the query heads of a head) or, without per_head, [sequences, max_kv] summed over all heads.
+
+    q, scale, window, causal: as attend had them; lse: float32 [rows, q_heads], what it has said with want_lse.  weights: None for
+    zeros; its lists may be longer than max_kv.  out may be weights."""
+    if stream is not None or cache.index != _current_device():
+        used = [x for x in (*cache.tensors, *batch.tensors, q, lse, weights, out) if x is not None]
+        return _on(cache.device, stream, used, lambda: weigh(cache, batch, q, lse, weights, per_head, scale, window, causal, out))
+    _together(cache, batch)
+    n, n_seqs, D, device = batch.n_rows, batch.c.n_seqs, cache.head_dim, cache.device
+    heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
+    q_stride = _rows(q, "q", cache.dtype, n, heads, D, device)
+    if not _on_gpu(lse, "lse", torch.float32, (n, heads)).is_contiguous() or lse.device != device:
+        raise ValueError("lse must be contiguous, on the cache's device")
+    if not 0 <= window < 1 << 31:
+        raise ValueError("window must be 0 or more and below 2^31")
+    lists = cache.kv_heads if per_head else 1
+    given = _by_list(weights, "weights", torch.float32, n_seqs, batch.max_kv, device) if weights is not None else None
+    if out is None:
+        out = torch.empty((n_seqs, lists, batch.max_kv) if per_head else (n_seqs, batch.max_kv), dtype=torch.float32, device=device) if given is None \
+            else _like(weights, *given, batch.max_kv)
+    made = _by_list(out, "out", torch.float32, n_seqs, batch.max_kv, device)
+    if made[0] != lists or given not in (None, made):
+        raise ValueError("weights and out must have a list for each head (or, without per_head, one), and the same strides")
+    a = T.tent_kv_weigh_args(q.data_ptr(), lse.data_ptr(), weights.data_ptr() if weights is not None else None, out.data_ptr(), q_stride, made[1], heads, lists,
+                             window, 0 if causal else T.TENT_KV_ATTEND_ALL, 1.0 / math.sqrt(D) if scale is None else scale, 0)
+    _check(T.lib().tent_kv_weigh(cache.ref, batch.ref, C.byref(a), _stream(cache.index)), "tent_kv_weigh")
+    return out
+
+
+def choose(batch: Batch, weights, budget: int, first: int = 0, recent: int = 0, stream=None):
+    """Which tokens every sequence of the batch keeps: lists [sequences, (heads,) budget] (int32, ascending, then -1) and counts [sequences].
+    All where there are no more than `budget`; else the `first` first, the `recent` last and those of the greatest weights.
+    weights: float32 [sequences, (heads,) max_kv or more], as weigh makes them."""
+    if stream is not None or batch.device.index != _current_device():
+        return _on(batch.device, stream, (*batch.tensors, weights), lambda: choose(batch, weights, budget, first, recent))
+    n_seqs, device = batch.c.n_seqs, batch.device
+    lists, apart = _by_list(weights, "weights", torch.float32, n_seqs, batch.max_kv, device)
+    if not 1 <= budget <= 1 << 30 or first < 0 or recent < 0 or first + recent > budget:
+        raise ValueError("budget must be 1 or more, and hold the first and the recent tokens")
+    out = torch.empty((*weights.shape[:-1], budget), dtype=torch.int32, device=device)
+    counts = torch.empty((n_seqs,), dtype=torch.int32, device=device)
+    a = T.tent_kv_choose_args(weights.data_ptr(), out.data_ptr(), counts.data_ptr(), apart, budget, lists, budget, first, recent)
+    _check(T.lib().tent_kv_choose(batch.ref, C.byref(a), _stream(device.index)), "tent_kv_choose")
+    return out, counts
+
+
+def keep(cache: Cache, batch: Batch, lists, counts, rows: bool = False, to_table=None, weights=None, weights_out=None, kv_len_out=None, stream=None):
+    """Move the tokens that every sequence keeps together; their number afterwards (int32 [sequences], a new tensor unless given), and with
+    `weights` these moved along.
+
+    Token j becomes what token lists[sequence, (head,) j] was, for j below counts[sequence]; one list for all heads or one for each.  With
+    rows=True lists name rows of the sequence (verify's path) and the context in front of them stays.  In place, unless to_table
+    (int32 [sequences, pages]) names other pages to write to.  weights: float32 [sequences, (heads,) max_kv or more], moved to weights_out
+    (in place itself unless given; a new tensor with to_table), behind the last kept token 0."""
+    if stream is not None or cache.index != _current_device():
+        used = [x for x in (*cache.tensors, *batch.tensors, lists, counts, to_table, weights, weights_out, kv_len_out) if x is not None]
+        return _on(cache.device, stream, used, lambda: keep(cache, batch, lists, counts, rows, to_table, weights, weights_out, kv_len_out))
+    _together(cache, batch)
+    n_seqs, device = batch.c.n_seqs, cache.device
+    n_lists, apart = _by_list(lists, "lists", torch.int32, n_seqs, 0, device)
+    if n_lists not in (1, cache.kv_heads):
+        raise ValueError("lists must be one for every head of the cache, or one for all")
+    a = T.tent_kv_keep_args(lists.data_ptr(), _vector(counts, "counts", torch.int32, n_seqs, device))
+    if to_table is not None:
+        _on_gpu(to_table, "to_table", torch.int32)
+        if to_table.dim() != 2 or to_table.shape[0] != n_seqs or to_table.device != device or (to_table.shape[1] > 1 and to_table.stride(1) != 1):
+            raise ValueError("to_table must be [sequences, pages] with contiguous rows, on the cache's device")
+        a.to_table, a.to_stride = to_table.data_ptr(), to_table.stride(0) if n_seqs > 1 else to_table.shape[1]
+        if n_seqs > 1 and a.to_stride < to_table.shape[1]:
+            raise ValueError("rows of to_table overlap")
+    if weights is not None:
+        a.n_weights, a.weights_stride = _by_list(weights, "weights", torch.float32, n_seqs, batch.max_kv, device)
+        if weights_out is None:
+            weights_out = weights if to_table is None else _like(weights, a.n_weights, a.weights_stride, batch.max_kv)
+        if _by_list(weights_out, "weights_out", torch.float32, n_seqs, batch.max_kv, device) != (a.n_weights, a.weights_stride):
+            raise ValueError("weights and weights_out must have the same heads and strides")
+        if a.n_weights not in (n_lists, cache.kv_heads):
+            raise ValueError("weights must have as many heads as lists, or one list for all heads")
+        a.weights, a.weights_out = weights.data_ptr(), weights_out.data_ptr()
+    elif weights_out is not None:
+        raise ValueError("weights_out goes with weights")
+    if kv_len_out is None:
+        kv_len_out = torch.empty((n_seqs,), dtype=torch.int32, device=device)
+    a.kv_len_out = _vector(kv_len_out, "kv_len_out", torch.int32, n_seqs, device)
+    a.list_stride, a.n_lists, a.most, a.flags = apart, n_lists, lists.shape[-1], T.TENT_KV_KEEP_ROWS if rows else 0
+    _check(T.lib().tent_kv_keep(cache.ref, batch.ref, C.byref(a), _stream(cache.index)), "tent_kv_keep")
+    return kv_len_out if weights is None else (kv_len_out, weights_out)
