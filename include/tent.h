@@ -682,6 +682,8 @@ typedef struct {
     float *weights_out;        /* device, laid out the same; may be `weights`                      */
     uint64_t q_stride;         /* values from a row to the next                                    */
     uint64_t weights_stride;   /* values from a list to the next, at least max_kv                  */
+    void *workspace;           /* device: tent_kv_weigh_workspace bytes; NULL where that is 0       */
+    uint64_t workspace_bytes;
     uint32_t q_heads;          /* a multiple of kv_heads, at most TENT_KV_MAX_HEADS                */
     uint32_t n_lists;          /* kv_heads: weights by head of the cache; 1: of all of them         */
     uint32_t window, flags;    /* as tent_kv_attend had them                                       */
@@ -739,6 +741,7 @@ int tent_kv_verify_workspace(const tent_kv_batch *batch, const tent_kv_verify_ar
  * that read head l (with one list all of them), of exp(scale q . k_t - lse).  Written for all t below max_kv: where nothing sees a
  * token its weight stays.  Rows whose lse is not finite add nothing.  A sequence that is left out, or has no rows, keeps its weights. */
 int tent_kv_weigh(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_weigh_args *args, void *stream);
+int tent_kv_weigh_workspace(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_weigh_args *args, uint64_t *bytes);
 
 /* Which tokens every sequence keeps: all where it has no more than `budget`; else its first `first` and last `recent` ones, and
  * of the others those with the greatest weights, of equal ones the first (NaN counts as minus infinity).  Takes n_seqs, kv_len and max_kv

@@ -30,7 +30,7 @@ EXPORTS = ["tent_create", "tent_destroy", "tent_register_segment", "tent_declare
            "tent_sim_fail", "tent_get_retries", "tent_monitor_init", "tent_monitor_update",
            "tent_plan_dispatch", "tent_get_modes", "tent_execute_bounded", "tent_probe_copy", "tent_declare_static",
            "tent_kv_packed_page", "tent_kv_append", "tent_kv_pack", "tent_kv_read", "tent_kv_attend_workspace", "tent_kv_attend",
-           "tent_kv_attend_tree", "tent_kv_verify_workspace", "tent_kv_verify", "tent_kv_weigh", "tent_kv_choose", "tent_kv_keep"]
+           "tent_kv_attend_tree", "tent_kv_verify_workspace", "tent_kv_verify", "tent_kv_weigh_workspace", "tent_kv_weigh", "tent_kv_choose", "tent_kv_keep"]
 
 
 class tent_config(C.Structure):
@@ -105,7 +105,7 @@ class tent_kv_verify_args(C.Structure):
 
 class tent_kv_weigh_args(C.Structure):
     _fields_ = [("q", C.c_void_p), ("lse", C.c_void_p), ("weights", C.c_void_p), ("weights_out", C.c_void_p), ("q_stride", C.c_uint64),
-                ("weights_stride", C.c_uint64), ("q_heads", C.c_uint32), ("n_lists", C.c_uint32), ("window", C.c_uint32),
+                ("weights_stride", C.c_uint64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("q_heads", C.c_uint32), ("n_lists", C.c_uint32), ("window", C.c_uint32),
                 ("flags", C.c_uint32), ("scale", C.c_float), ("reserved", C.c_uint32)]
 
 
@@ -183,6 +183,7 @@ def lib():
         L.tent_kv_attend_tree.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.POINTER(tent_kv_tree), C.c_void_p]
         L.tent_kv_verify_workspace.argtypes = [batch, C.POINTER(tent_kv_verify_args), C.POINTER(C.c_uint64)]
         L.tent_kv_verify.argtypes = [batch, C.POINTER(tent_kv_verify_args), C.c_void_p]
+        L.tent_kv_weigh_workspace.argtypes = [cache, batch, C.POINTER(tent_kv_weigh_args), C.POINTER(C.c_uint64)]
         L.tent_kv_weigh.argtypes = [cache, batch, C.POINTER(tent_kv_weigh_args), C.c_void_p]
         L.tent_kv_choose.argtypes = [batch, C.POINTER(tent_kv_choose_args), C.c_void_p]
         L.tent_kv_keep.argtypes = [cache, batch, C.POINTER(tent_kv_keep_args), C.c_void_p]
@@ -437,6 +438,12 @@ def tent_kv_verify_workspace(batch: tent_kv_batch, args: tent_kv_verify_args) ->
 
 def tent_kv_verify(batch: tent_kv_batch, args: tent_kv_verify_args, stream=None):
     _check(lib().tent_kv_verify(batch, args, _stream(stream)), "tent_kv_verify")
+
+
+def tent_kv_weigh_workspace(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_weigh_args) -> int:
+    n = C.c_uint64()
+    _check(lib().tent_kv_weigh_workspace(cache, batch, args, n), "tent_kv_weigh_workspace")
+    return n.value
 
 
 def tent_kv_weigh(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_weigh_args, stream=None):

@@ -439,15 +439,16 @@ def verify_workspace(batch: Batch, vocab: int, parents: bool = False, draft: boo
 
 
 def weigh(cache: Cache, batch: Batch, q, lse, weights=None, per_head: bool = True, scale: float = None, window: int = 0, causal: bool = True, out=None,
-          stream=None):
+          workspace=None, stream=None):
     """`weights` and what the batch's rows add to them: the attention weight that each token gets from the rows that see it, [sequences,
     kv_heads, max_kv] (float32; summed over the query heads of a head) or, without per_head, [sequences, max_kv] summed over all heads.
 
     q, scale, window, causal: as attend had them; lse: float32 [rows, q_heads], what it has said with want_lse.  weights: None for
-    zeros; its lists may be longer than max_kv.  out may be weights."""
+    zeros; its lists may be longer than max_kv.  out may be weights.  workspace: a contiguous uint8 tensor of at least weigh_workspace bytes
+    to use instead of a new one."""
     if stream is not None or cache.index != _current_device():
-        used = [x for x in (*cache.tensors, *batch.tensors, q, lse, weights, out) if x is not None]
-        return _on(cache.device, stream, used, lambda: weigh(cache, batch, q, lse, weights, per_head, scale, window, causal, out))
+        used = [x for x in (*cache.tensors, *batch.tensors, q, lse, weights, out, workspace) if x is not None]
+        return _on(cache.device, stream, used, lambda: weigh(cache, batch, q, lse, weights, per_head, scale, window, causal, out, workspace))
     _together(cache, batch)
     n, n_seqs, D, device = batch.n_rows, batch.c.n_seqs, cache.head_dim, cache.device
     heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
@@ -464,10 +465,26 @@ def weigh(cache: Cache, batch: Batch, q, lse, weights=None, per_head: bool = Tru
     made = _by_list(out, "out", torch.float32, n_seqs, batch.max_kv, device)
     if made[0] != lists or given not in (None, made):
         raise ValueError("weights and out must have a list for each head (or, without per_head, one), and the same strides")
-    a = T.tent_kv_weigh_args(q.data_ptr(), lse.data_ptr(), weights.data_ptr() if weights is not None else None, out.data_ptr(), q_stride, made[1], heads, lists,
-                             window, 0 if causal else T.TENT_KV_ATTEND_ALL, 1.0 / math.sqrt(D) if scale is None else scale, 0)
-    _check(T.lib().tent_kv_weigh(cache.ref, batch.ref, C.byref(a), _stream(cache.index)), "tent_kv_weigh")
+    a = T.tent_kv_weigh_args(q.data_ptr(), lse.data_ptr(), weights.data_ptr() if weights is not None else None, out.data_ptr(), q_stride, made[1], None, 0,
+                             heads, lists, window, 0 if causal else T.TENT_KV_ATTEND_ALL, 1.0 / math.sqrt(D) if scale is None else scale, 0)
+    L, ref = T.lib(), C.byref(a)
+    if lists != cache.kv_heads:                                          # with a list for each head none is needed
+        need = C.c_uint64()
+        _check(L.tent_kv_weigh_workspace(cache.ref, batch.ref, ref, C.byref(need)), "tent_kv_weigh_workspace")
+        if need.value:
+            if workspace is None:
+                workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+            elif not _on_gpu(workspace, "workspace", torch.uint8).is_contiguous() or workspace.device != device:
+                raise ValueError("workspace must be contiguous, on the cache's device")
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(L.tent_kv_weigh(cache.ref, batch.ref, ref, _stream(cache.index)), "tent_kv_weigh")
     return out
+
+
+def weigh_workspace(cache: Cache, batch: Batch, q_heads: int, per_head: bool = True) -> int:
+    """Bytes of workspace that weigh takes for such a batch."""
+    _together(cache, batch)
+    return T.tent_kv_weigh_workspace(cache.c, batch.c, T.tent_kv_weigh_args(q_heads=q_heads, n_lists=cache.kv_heads if per_head else 1, scale=1.0))
 
 
 def choose(batch: Batch, weights, budget: int, first: int = 0, recent: int = 0, stream=None):

@@ -24,7 +24,7 @@ def make_verify(T, **change):  # noqa: F811
 
 
 def make_weigh(T, **change):  # noqa: F811
-    d = dict(q=0x1000, lse=0x2000, weights=0x3000, weights_out=0x4000, q_stride=4096, weights_stride=1000, q_heads=32, n_lists=8, window=0, flags=0, scale=0.1, reserved=0)
+    d = dict(q=0x1000, lse=0x2000, weights=0x3000, weights_out=0x4000, q_stride=4096, weights_stride=1000, workspace=0x40000, workspace_bytes=1 << 40, q_heads=32, n_lists=8, window=0, flags=0, scale=0.1, reserved=0)
     return T.tent_kv_weigh_args(**{**d, **change})
 
 
@@ -214,14 +214,24 @@ def scenario_enqueued():
         args.workspace_bytes -= 1
         assert L.tent_kv_attend_tree(c, long, args, make_tree(T), stream) == RANGE
         for n_lists in (1, 8):
-            same(names(lambda: L.tent_kv_weigh(c, long, make_weigh(T, n_lists=n_lists, weights_stride=1 << 20), stream)), ["weigh"])
+            same(names(lambda: L.tent_kv_weigh(c, long, make_weigh(T, n_lists=n_lists, weights_stride=1 << 20), stream)), ["few"])
+            args, n = make_weigh(T, n_lists=n_lists), C.c_uint64()
+            same(names(lambda: L.tent_kv_weigh(c, many, args, stream)), ["many"] if n_lists == 8 else ["many", "weigh_join"])
+            assert L.tent_kv_weigh_workspace(c, many, args, n) == 0 and n.value == (0 if n_lists == 8 else 40 * 8 * 1000 * 4)
+            args.workspace_bytes = n.value
+            assert L.tent_kv_weigh(c, many, args, stream) == 0
+            if n.value:
+                args.workspace_bytes -= 1
+                assert L.tent_kv_weigh(c, many, args, stream) == RANGE
+                args.workspace_bytes, args.workspace = n.value, 0x40008
+                assert L.tent_kv_weigh(c, many, args, stream) == INVALID
             same(names(lambda: L.tent_kv_keep(c, short, make_keep(T, n_lists=n_lists), stream)), ["keep_kernel"])
         same(names(lambda: L.tent_kv_keep(c, short, make_keep(T, weights=0x5000, weights_out=0x5000, n_weights=8, weights_stride=200), stream)), ["keep_kernel", "keep_weights"])
         same(names(lambda: L.tent_kv_keep(c, short, make_keep(T, to_table=0x9000, to_stride=64, most=0), stream)), ["keep_kernel"])
     for batch in (short, make_batch(T, n_rows=0)):                       # sequences of no rows have tokens, too
         same(names(lambda: L.tent_kv_choose(batch, make_choose(T), stream)), ["choose"])
         same(names(lambda: L.tent_kv_keep(make_cache(T), batch, make_keep(T), stream)), ["keep_kernel"])
-        same(names(lambda: L.tent_kv_weigh(make_cache(T), batch, make_weigh(T), stream)), ["weigh"])
+        same(names(lambda: L.tent_kv_weigh(make_cache(T), batch, make_weigh(T), stream)), ["few"])
     for kind in range(3):
         for change in (dict(), dict(draft=None), dict(parents=None), dict(vocab=100), dict(vocab=1 << 24, target_stride=1 << 24, draft_stride=1 << 24)):
             args, n = make_verify(T, type=kind, path_stride=4000, **change), C.c_uint64()

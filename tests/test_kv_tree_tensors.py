@@ -27,6 +27,10 @@ class Gpus(Base.Gpus):
         self.args = T.tent_kv_verify_args.from_buffer_copy(args._obj)
         return self.call("verify", stream)
 
+    def tent_kv_weigh_workspace(self, cache, batch, args, need):
+        need._obj.value = 4096
+        return 0
+
     def tent_kv_weigh(self, cache, batch, args, stream):
         self.args = T.tent_kv_weigh_args.from_buffer_copy(args._obj)
         return self.call("weigh", stream)
@@ -170,6 +174,7 @@ def test_tensors_that_are_refused(gpus):
         (s.verify, "workspace", [on(torch.zeros(8192, dtype=torch.uint8)[::2]), away(torch.zeros(4096, dtype=torch.uint8))]),
         (s.weigh, "lse", [on(torch.zeros(3, 5)), on(torch.zeros(3, 8)[:, ::2]), away(torch.zeros(3, 4)), on(torch.zeros(3, 4, dtype=torch.bfloat16))]),
         (s.weigh, "weights", [on(torch.zeros(2, 2, 19)), on(torch.zeros(2, 20)), on(torch.zeros(2, 2, 40)[..., ::2]), on(torch.zeros(3, 2, 20)), away(torch.zeros(2, 2, 20))]),
+        (lambda **change: s.weigh(weights=None, per_head=False, **change), "workspace", [on(torch.zeros(8192, dtype=torch.uint8)[::2]), away(torch.zeros(4096, dtype=torch.uint8))]),
         (s.weigh, "out", [on(torch.zeros(2, 2, 21)), on(torch.zeros(2, 1, 20))]),
         (s.choose, "weights", [on(torch.zeros(2, 2, 19)), on(torch.zeros(2, 2, 20, dtype=torch.float16)), on(torch.zeros(1, 2, 20).expand(2, 2, 20)), away(torch.zeros(2, 2, 20))]),
         (s.keep, "lists", [on(torch.zeros(2, 3, 7, dtype=i32)), on(torch.zeros(1, 2, 7, dtype=i32)), on(torch.zeros(2, 2, 7)), on(torch.zeros(2, 2, 14, dtype=i32)[..., ::2])]),
@@ -201,7 +206,7 @@ def test_strides_are_handed_on(gpus):
     s.weigh(weights=wide, out=wide)
     assert gpus.args.weights_stride == 32 and gpus.args.weights == gpus.args.weights_out
     s.weigh(weights=None, per_head=False)
-    assert gpus.args.n_lists == 1 and gpus.args.weights is None and gpus.args.weights_stride == 20
+    assert gpus.args.n_lists == 1 and gpus.args.weights is None and gpus.args.weights_stride == 20 and gpus.args.workspace_bytes == 4096
     s.choose(weights=on(torch.zeros(2, 2, 32)), budget=5)
     assert (gpus.args.weights_stride, gpus.args.list_stride, gpus.args.n_lists) == (32, 5, 2)
     s.choose(weights=on(torch.zeros(2, 24)), budget=5)
