@@ -1,4 +1,6 @@
 // What a sequence of a key/value cache keeps, and the move that makes it the sequence: tent_kv_choose and tent_kv_keep.
+#include <type_traits>
+
 #include "kv_elem.h"
 
 namespace tent {
@@ -6,14 +8,23 @@ namespace {
 
 // ---- choosing ------------------------------------------------------------------------------------
 // A workgroup for each list.  The weight that the last chosen token has is found digit by digit: a histogram of the digits of those
-// weights whose higher digits are the wanted ones, then the digit at which as many lie above as are wanted.
+// weights whose higher digits are the wanted ones, then the digit at which as many lie above as are wanted.  Where up to 128 weights have
+// that digit they are put side by side and the one is found among them by its rank, most often after the second digit.  Up to 16,384 tokens
+// are held in registers for all of it; more are read again for each digit.
+//
+// Barriers and latencies bound it.  Measured: one list of 6,000 tokens 12.4 us (with four digits of 8 bits and no ranks 15.5), 256 lists of
+// 1,000 to 16,384 tokens, four fifths of whose weights are zero, 25 us (22.6).
 struct ChooseArgs {
     tent_kv_choose_args a;
     tent_kv_batch b;
     uint32_t first;                    // of the launch's workgroups
 };
-constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
-constexpr int kDigit = 256;
+constexpr uint32_t kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
+constexpr uint32_t kHeld = 16, kHeldTokens = kHeld * kChooseThreads;     // tokens of a thread, and of the workgroup
+// Weights are alike, often zero, and lanes side by side count the same digits: those that have the first lane's are counted at once, and four
+// copies of the counters, in banks side by side, keep the others apart.
+constexpr uint32_t kDigits = 2048, kCopies = 4;
+constexpr uint32_t kRanked = 128;      // each is compared with each
 
 // Larger weights as larger whole numbers; zeros are alike, NaN is minus infinity.
 __device__ __forceinline__ uint32_t weight_key(float w)
@@ -22,9 +33,19 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 
+// Calls f(i) for each of a thread's tokens, 1024 apart, where `n` are left.
+template <class F>
+__device__ __forceinline__ void each_held(uint32_t n, F f)
+{
+#pragma unroll
+    for (uint32_t i = 0; i < kHeld; ++i)
+        if (i * kChooseThreads < n) f(i);                                // the whole workgroup
+}
+
 __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs g)
 {
-    __shared__ uint32_t count[kDigit], wave_above[kChooseWaves], wave_equal[kChooseWaves], digit_lds, wanted_lds;
+    __shared__ __align__(16) uint32_t count[kDigits * kCopies];
+    __shared__ uint32_t before_lds[kHeld * kChooseWaves], digit_lds, wanted_lds, there_lds, all_lds;
     const tent_kv_choose_args& a = g.a;
     const uint32_t block = g.first + blockIdx.x, seq = block / a.n_lists, list = block - seq * a.n_lists;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
@@ -40,65 +61,152 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs
     }
     const float* const w = a.weights + (uint64_t)block * a.weights_stride;
     const uint32_t lo = a.first, hi = n - a.recent;                      // the tokens that weights decide on: more than are wanted of them
+    const bool once = n <= kHeldTokens;
+    uint32_t key[kHeld];
+    auto hold = [&](uint32_t t0) {                                       // the keys of kHeldTokens tokens from t0 on
+        float x[kHeld];
+        each_held(n - t0, [&](uint32_t i) {
+            const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
+            x[i] = t < n ? dev_load<float>(w + t) : 0.f;
+        });
+        each_held(n - t0, [&](uint32_t i) { key[i] = weight_key(x[i]); });
+    };
+    auto decided = [&](uint32_t t) -> bool { return t >= lo && t < hi; };
+    if (once) hold(0);
+    // Keys above `border` are kept, and the first `equal` of those at it; whatever is not decided on is.
     uint32_t wanted = a.budget - a.first - a.recent, border = 0xFFFFFFFFu, equal = 0;
     if (wanted) {
         uint32_t above = 0;                                              // the digits found, at their places
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (threadIdx.x < kDigit) count[threadIdx.x] = 0;
+        for (int shift = 21, bits = 11; ; bits = shift >= 10 ? 11 : 10, shift = shift >= 21 ? 10 : 0) {
+            const uint32_t digits = 1u << bits;
+#pragma unroll
+            for (uint32_t i = 0; i < kDigits * kCopies / 4 / kChooseThreads; ++i) *(u32x4*)&count[(i * kChooseThreads + threadIdx.x) * 4] = u32x4{0, 0, 0, 0};
             __syncthreads();
-            for (uint32_t t = lo + threadIdx.x; t < hi; t += kChooseThreads) {
-                const uint32_t key = weight_key(w[t]);
-                if (shift == 24 || key >> (shift + 8) == above >> (shift + 8)) atomicAdd(&count[key >> shift & 255u], 1u);
+            for (uint32_t t0 = 0; t0 < n; t0 += kHeldTokens) {
+                if (!once) hold(t0);
+                each_held(n - t0, [&](uint32_t i) {
+                    if (decided(t0 + i * kChooseThreads + threadIdx.x) && (shift == 21 || key[i] >> (shift + bits) == above >> (shift + bits))) {
+                        const uint32_t digit = key[i] >> shift & (digits - 1), one = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
+                        const uint64_t alike = __ballot(digit == one);
+                        if (digit != one) atomicAdd(&count[digit * kCopies + (lane & (kCopies - 1))], 1u);
+                        else if (lane == (uint32_t)__builtin_ctzll(alike)) atomicAdd(&count[one * kCopies + (wave & (kCopies - 1))], (uint32_t)__popcll(alike));
+                    }
+                });
             }
             __syncthreads();
-            if (wave == 0) {                                             // four digits a lane, the largest in lane 0
-                uint32_t mine[4], sum = 0;
+            uint32_t mine[2], up_to = 0;                                 // two digits a thread, the largest in the first
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum += mine[i] = count[255 - (4 * lane + i)];
-                uint32_t before = sum;
+            for (uint32_t i = 0; i < 2; ++i) {
+                const u32x4 c = *(const u32x4*)&count[(kDigits - 1 - 2 * threadIdx.x - i) * kCopies];
+                up_to += mine[i] = c[0] + c[1] + c[2] + c[3];
+            }
+            const uint32_t both = up_to;
 #pragma unroll
-                for (int m = 1; m < 64; m <<= 1) {
-                    const uint32_t up = __shfl_up(before, m, 64);
-                    before += lane >= (uint32_t)m ? up : 0u;
+            for (int m = 1; m < 64; m <<= 1) {
+                const uint32_t up = __shfl_up(up_to, m, 64);
+                up_to += lane >= (uint32_t)m ? up : 0u;
+            }
+            if (lane == 63) before_lds[wave] = up_to;
+            if (threadIdx.x == 0) there_lds = 0;
+            __syncthreads();
+            uint32_t before = up_to - both;
+            for (uint32_t i = 0; i < wave; ++i) before += before_lds[i];
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                if (before < wanted && before + mine[i] >= wanted) {
+                    digit_lds = kDigits - 1 - 2 * threadIdx.x - i;
+                    wanted_lds = wanted - before;
+                    all_lds = mine[i];
                 }
-                before -= sum;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (before < wanted && before + mine[i] >= wanted) {
-                        digit_lds = 255 - (4 * lane + i);
-                        wanted_lds = wanted - before;
-                    }
-                    before += mine[i];
-                }
+                before += mine[i];
             }
             __syncthreads();
             above |= digit_lds << shift;
             wanted = wanted_lds;
+            const uint32_t there = all_lds;
+            if (shift == 0) break;
+            if (there > kRanked) continue;
+            // Those with the digit, in any order, and the rank of each: the greater ones and, of the same, the earlier ones come before it.
+            for (uint32_t t0 = 0; t0 < n; t0 += kHeldTokens) {
+                if (!once) hold(t0);
+                each_held(n - t0, [&](uint32_t i) {
+                    const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
+                    if (decided(t) && key[i] >> shift == above >> shift) *(u32x2*)&count[2 * atomicAdd(&there_lds, 1u)] = u32x2{key[i], t};
+                });
+            }
+            __syncthreads();
+            if (threadIdx.x < there) {
+                const u32x2 me = *(const u32x2*)&count[2 * threadIdx.x];
+                uint32_t rank = 0, same = 0;
+#pragma unroll 8
+                for (uint32_t i = 0; i < there; ++i) {
+                    const u32x2 other = *(const u32x2*)&count[2 * i];
+                    const bool alike = other[0] == me[0] && other[1] < me[1];
+                    rank += other[0] > me[0] || alike;
+                    same += alike;
+                }
+                if (rank == wanted - 1) {
+                    digit_lds = me[0];
+                    wanted_lds = same + 1;
+                }
+            }
+            __syncthreads();
+            above = digit_lds;
+            wanted = wanted_lds;
+            break;
         }
         border = above;
         equal = wanted;                                                  // of those at the border the first so many
     }
-    // Tokens in their order: which are kept, and how many before them.
-    uint32_t base = 0, equal_before = 0;
-    for (uint32_t t0 = 0; t0 < n; t0 += kChooseThreads) {
-        const uint32_t t = t0 + threadIdx.x;
-        const bool there = t < n, decided = there && t >= lo && t < hi;
-        const uint32_t key = decided ? weight_key(w[t]) : 0u;
-        const bool always = there && !decided, more = always || (decided && equal && key > border), same = decided && equal && key == border;
-        const uint64_t more_mask = __ballot(more), same_mask = __ballot(same), below = (1ull << lane) - 1;
-        if (lane == 0) {
-            wave_above[wave] = (uint32_t)__popcll(more_mask);
-            wave_equal[wave] = (uint32_t)__popcll(same_mask);
+    // Tokens in their order: how many are kept before each, from counts of every wave's 64.
+    uint32_t more_before = 0, equal_before = 0;
+    for (uint32_t t0 = 0; t0 < n; t0 += kHeldTokens) {
+        if (!once) hold(t0);
+        auto kind = [&](uint32_t i, bool& more, bool& same) {
+            const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
+            more = t < n && (!decided(t) || (equal && key[i] > border));
+            same = t < n && decided(t) && equal && key[i] == border;
+        };
+        each_held(n - t0, [&](uint32_t i) {
+            bool more, same;
+            kind(i, more, same);
+            const uint32_t both = (uint32_t)__popcll(__ballot(more)) | (uint32_t)__popcll(__ballot(same)) << 16;    // at most 16,384 each
+            if (lane == 0) before_lds[i * kChooseWaves + wave] = both;
+        });
+        __syncthreads();
+        if (wave == 0) {
+            uint32_t mine[4], sum = 0;
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t at = lane * 4 + i;
+                sum += mine[i] = t0 + at / kChooseWaves * kChooseThreads < n ? before_lds[at] : 0u;
+            }
+            uint32_t up_to = sum;
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {
+                const uint32_t up = __shfl_up(up_to, m, 64);
+                up_to += lane >= (uint32_t)m ? up : 0u;
+            }
+            if (lane == 63) all_lds = up_to;
+            up_to -= sum;
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                before_lds[lane * 4 + i] = up_to;
+                up_to += mine[i];
+            }
         }
         __syncthreads();
-        uint32_t at = base + (uint32_t)__popcll(more_mask & below), eq = equal_before + (uint32_t)__popcll(same_mask & below);
-        for (uint32_t i = 0; i < kChooseWaves; ++i) {
-            const uint32_t m = wave_above[i], s = wave_equal[i];
-            if (i < wave) { at += m; eq += s; }
-            base += m;
-            equal_before += s;
-        }
-        if (more || (same && eq < equal)) to[at + (eq < equal ? eq : equal)] = (int32_t)t;
+        each_held(n - t0, [&](uint32_t i) {
+            bool more, same;
+            kind(i, more, same);
+            const uint64_t below = (1ull << lane) - 1, more_mask = __ballot(more), same_mask = __ballot(same);
+            const uint32_t both = before_lds[i * kChooseWaves + wave];
+            const uint32_t at = more_before + (both & 0xFFFFu) + (uint32_t)__popcll(more_mask & below);
+            const uint32_t eq = equal_before + (both >> 16) + (uint32_t)__popcll(same_mask & below);
+            if (more || (same && eq < equal)) to[at + (eq < equal ? eq : equal)] = (int32_t)(t0 + i * kChooseThreads + threadIdx.x);
+        });
+        more_before += all_lds & 0xFFFFu;
+        equal_before += all_lds >> 16;
         __syncthreads();
     }
 }
@@ -108,11 +216,10 @@ struct KeepArgs {
     KvCache c;
     tent_kv_batch b;
     tent_kv_keep_args a;
-    uint32_t columns;                  // workgroups that share a head's row, in place
-    uint32_t parts;                    // workgroups that share a list, to other pages
+    uint32_t columns;                  // in place: workgroups that share a head's row
+    uint32_t parts;                    // to other pages: workgroups that share a list
     uint32_t first;                    // of the launch's workgroups
 };
-constexpr uint32_t kEntries = 128;     // of a list at a time
 constexpr uint64_t kNowhere = ~0ull;
 
 // What a sequence's lists are about: tokens from `base` on, `have` of them, of which `count` entries are kept.
@@ -124,89 +231,98 @@ __device__ __forceinline__ Kept kept_of(const tent_kv_keep_args& a, const KvSeq&
     k.bad = q.bad || k.base < 0 || k.count < 0 || (uint32_t)k.count > a.most || (!a.to_table && k.count > k.have);
     return k;
 }
+// By one thread of the sequence's workgroups.
+__device__ __forceinline__ void tell_length(const KeepArgs& g, const Kept& k, uint32_t seq)
+{
+    if (k.bad) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
+    if (g.a.kv_len_out) g.a.kv_len_out[seq] = k.bad ? g.b.kv_len[seq] : k.base + k.count;
+}
 __device__ __forceinline__ bool entry_ok(const tent_kv_keep_args& a, const Kept& k, int32_t entry, int32_t j)
 {
     return entry < k.have && entry >= (a.to_table ? 0 : j);
 }
 
-// A workgroup has a head's rows of K or V (in place a column of them), and of the list all entries in turn, or (to other pages) some.  In
-// place every entry is at or behind its own place, so what a batch of entries writes no later one reads; within a batch all is
-// read before anything is written.  Columns have nothing to do with each other.
+// Where a token is: its page, and the number in it of its row of a head.  The page is kNowhere where the table names none.
+struct Place { uint64_t page; uint32_t row; };
+__device__ __forceinline__ Place place_of(const KvCache& c, const int32_t* table, uint32_t entries, uint32_t token, uint32_t head)
+{
+    const uint32_t at = token >> c.page_shift, page = at < entries ? (uint32_t)table[at] : ~0u;
+    return Place{page < c.n_pages ? page * c.page_stride : kNowhere, (token & ((1u << c.page_shift) - 1u)) * c.heads + head};
+}
+template <int D>
+__device__ __forceinline__ uint64_t scales_at(const KvCache& c, const Place& p)
+{
+    return p.page + ((uint64_t)(c.heads * (D / 2)) << c.page_shift) + (uint64_t)p.row * (D / 32);
+}
+template <int D>
+using Scales = std::conditional_t<D == 64, uint16_t, std::conditional_t<D == 128, uint32_t, u32x2>>;     // of a row
+
+// In place.  A workgroup has a column of a head's rows of K and V, and takes the list's entries in turn.  Every entry is at or behind its own
+// place, so what a batch of entries writes no later one reads; within a batch all is read before anything is written.  Columns have
+// nothing to do with each other.  The next batch's places are looked up while a batch's rows are on their way.
+constexpr uint32_t kEntries = 64;      // of a batch
 template <int D, int kBits>
 __global__ void __launch_bounds__(256) keep_kernel(const KeepArgs g)
 {
     constexpr uint32_t kChunks = kBits == 16 ? D / 8 : D / 32;           // vectors of a head's row, without the scales
-    constexpr uint32_t kItems = kEntries * kChunks / 256;                // of a thread, of a whole row
-    constexpr uint32_t kScale = D / 32;                                  // bytes of scales
-    __shared__ uint64_t from[kEntries], to[kEntries], from_scale[kBits == 4 ? kEntries : 1], to_scale[kBits == 4 ? kEntries : 1];
+    constexpr uint32_t kItems = (2 * kEntries * kChunks + 255) / 256;    // of a thread, of a whole row of K and V
+    __shared__ Place from[3][kEntries], to[3][kEntries];                 // of this batch, of the next, and of the one that others may still be storing
     const tent_kv_keep_args& a = g.a;
     uint32_t x = g.first + blockIdx.x;
     const uint32_t column = x % g.columns; x /= g.columns;
-    const uint32_t is_v = x & 1u; x >>= 1;
-    const uint32_t head = x % g.c.heads; x /= g.c.heads;
-    const uint32_t part = x % g.parts, seq = x / g.parts;
+    const uint32_t head = x % g.c.heads, seq = x / g.c.heads;
+    const int32_t* const list = a.lists + ((uint64_t)seq * a.n_lists + (a.n_lists == 1 ? 0u : head)) * a.list_stride;
+    int32_t entry_ahead = threadIdx.x < kEntries && threadIdx.x < a.most ? list[threadIdx.x] : -1;       // on its way beside the lengths
     const KvSeq q = kv_sequence(g.b, seq);
     const Kept k = kept_of(a, q, seq);
-    const bool tells = column == 0 && is_v == 0 && head == 0 && part == 0 && threadIdx.x == 0;
-    if (tells) {
-        if (k.bad) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
-        if (a.kv_len_out) a.kv_len_out[seq] = k.bad ? g.b.kv_len[seq] : k.base + k.count;
-    }
+    if (column == 0 && head == 0 && threadIdx.x == 0) tell_length(g, k, seq);
     if (k.bad) return;
-    uint8_t* const pool = is_v ? g.c.v : g.c.k;
-    const int32_t* const list = a.lists + ((uint64_t)seq * a.n_lists + (a.n_lists == 1 ? 0u : head)) * a.list_stride;
+    const int32_t* const table = g.b.page_table + (uint64_t)seq * g.b.table_stride;
+    const uint32_t count = (uint32_t)k.count;
     const uint32_t wide = kChunks / g.columns, chunk0 = column * wide, wide_log = 31 - __builtin_clz(wide);      // vectors of the column, a power of two
-    const bool in_place = !a.to_table;
-    auto place = [&](uint32_t token, const int32_t* table, uint64_t stride, uint32_t entries, uint64_t& row, uint64_t& scale) {
-        const uint32_t at = token >> g.c.page_shift;
-        const uint32_t page = at < entries ? (uint32_t)table[seq * stride + at] : ~0u;
-        if (page >= g.c.n_pages) return false;
-        const uint32_t r = (token & ((1u << g.c.page_shift) - 1u)) * g.c.heads + head;
-        row = page * g.c.page_stride + (uint64_t)r * (kBits == 16 ? D * 2 : D / 2);
-        scale = page * g.c.page_stride + ((uint64_t)(g.c.heads * (D / 2)) << g.c.page_shift) + (uint64_t)r * kScale;
-        return true;
-    };
-    const uint32_t first = part * kEntries, step = g.parts * kEntries;
-    for (uint32_t j0 = first; j0 < (uint32_t)k.count; j0 += step) {
-        const uint32_t n = (uint32_t)k.count - j0 < kEntries ? (uint32_t)k.count - j0 : kEntries;
-        if (threadIdx.x < n) {
-            const int32_t j = (int32_t)(j0 + threadIdx.x), entry = list[j];
-            uint64_t row = kNowhere, scale = 0, to_row = 0, to_sc = 0;
-            int32_t wrong = 0;
-            if (!entry_ok(a, k, entry, j)) wrong = TENT_KV_BAD_POSITION;
-            else if (!in_place || entry != j) {
-                const bool read = place((uint32_t)(k.base + entry), g.b.page_table, g.b.table_stride, g.b.table_stride, row, scale);
-                const bool write = place((uint32_t)(k.base + j), in_place ? g.b.page_table : a.to_table, in_place ? g.b.table_stride : a.to_stride,
-                                         in_place ? g.b.table_stride : a.to_stride, to_row, to_sc);
-                if (!read || !write) {
-                    wrong = TENT_KV_BAD_PAGE;
-                    row = kNowhere;
-                }
-            }
-            if (wrong && column == 0 && is_v == 0) kv_note(g.b.errors, wrong);
-            from[threadIdx.x] = row;
-            to[threadIdx.x] = to_row;
-            if constexpr (kBits == 4) {
-                from_scale[threadIdx.x] = scale;
-                to_scale[threadIdx.x] = to_sc;
+    auto find = [&](uint32_t j0, int32_t entry, uint32_t buffer) {
+        const uint32_t j = j0 + threadIdx.x;
+        if (threadIdx.x >= kEntries || j >= count) return;
+        Place read{kNowhere, 0}, write{kNowhere, 0};
+        int32_t wrong = 0;
+        if (!entry_ok(a, k, entry, (int32_t)j)) wrong = TENT_KV_BAD_POSITION;
+        else if (entry != (int32_t)j) {
+            read = place_of(g.c, table, g.b.table_stride, (uint32_t)(k.base + entry), head);
+            write = place_of(g.c, table, g.b.table_stride, (uint32_t)k.base + j, head);
+            if (read.page == kNowhere || write.page == kNowhere) {
+                wrong = TENT_KV_BAD_PAGE;
+                read.page = kNowhere;
             }
         }
-        __syncthreads();
+        if (wrong && column == 0) kv_note(g.b.errors, wrong);
+        from[buffer][threadIdx.x] = read;
+        to[buffer][threadIdx.x] = write;
+    };
+    if (count == 0) return;
+    find(0, entry_ahead, 0);
+    __syncthreads();
+    uint32_t buffer = 0;
+    for (uint32_t j0 = 0; j0 < count; j0 += kEntries) {
+        const uint32_t n = count - j0 < kEntries ? count - j0 : kEntries, next = buffer == 2 ? 0u : buffer + 1;
+        const uint32_t half = n << wide_log;                             // vectors of K, then as many of V
         u32x4 v[kItems] = {};
-        u32x2 s = {0, 0};
-        const uint32_t items = n * wide;
+        Scales<D> s = {};
+        auto vector = [&](const Place& p, uint32_t item) -> uint8_t* {
+            return (item >= half ? g.c.v : g.c.k) + p.page + (uint64_t)p.row * (kChunks * 16) + (chunk0 + ((item >= half ? item - half : item) & (wide - 1))) * 16;
+        };
+        auto entry_of = [&](uint32_t item) -> uint32_t { return (item >= half ? item - half : item) >> wide_log; };
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i) {
             const uint32_t item = i * 256 + threadIdx.x;
-            if (item < items && from[item >> wide_log] != kNowhere) v[i] = dev_load<u32x4>(pool + from[item >> wide_log] + (chunk0 + (item & (wide - 1))) * 16);
+            if (item < 2 * half && from[buffer][entry_of(item)].page != kNowhere) v[i] = dev_load<u32x4>(vector(from[buffer][entry_of(item)], item));
         }
-        if constexpr (kBits == 4) {
-            if (column == 0 && threadIdx.x < n && from[threadIdx.x] != kNowhere) {
-                const uint8_t* const p = pool + from_scale[threadIdx.x];
-                if constexpr (kScale == 2) s[0] = dev_load<uint16_t>(p);
-                else if constexpr (kScale == 4) s[0] = dev_load<uint32_t>(p);
-                else s = dev_load<u32x2>(p);
-            }
+        const uint32_t e = threadIdx.x % kEntries;                       // a thread for the scales of each entry of K, then of V
+        uint8_t* const scale_pool = threadIdx.x < kEntries ? g.c.k : g.c.v;
+        const bool scales = kBits == 4 && column == 0 && threadIdx.x < 2 * kEntries && e < n && from[buffer][e].page != kNowhere;
+        if (scales) s = dev_load<Scales<D>>(scale_pool + scales_at<D>(g.c, from[buffer][e]));
+        if (j0 + kEntries < count) {
+            const uint32_t j = j0 + kEntries + threadIdx.x;
+            find(j0 + kEntries, threadIdx.x < kEntries && j < count ? list[j] : -1, next);
         }
         // all of it is here before any of it is written
 #pragma unroll
@@ -216,17 +332,79 @@ __global__ void __launch_bounds__(256) keep_kernel(const KeepArgs g)
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i) {
             const uint32_t item = i * 256 + threadIdx.x;
-            if (item < items && from[item >> wide_log] != kNowhere) dev_store(pool + to[item >> wide_log] + (chunk0 + (item & (wide - 1))) * 16, v[i]);
+            if (item < 2 * half && from[buffer][entry_of(item)].page != kNowhere) dev_store(vector(to[buffer][entry_of(item)], item), v[i]);
         }
-        if constexpr (kBits == 4) {
-            if (column == 0 && threadIdx.x < n && from[threadIdx.x] != kNowhere) {
-                uint8_t* const p = pool + to_scale[threadIdx.x];
-                if constexpr (kScale == 2) dev_store(p, (uint16_t)s[0]);
-                else if constexpr (kScale == 4) dev_store(p, s[0]);
-                else dev_store(p, s);
+        if (scales) dev_store(scale_pool + scales_at<D>(g.c, to[buffer][e]), s);
+        buffer = next;
+    }
+}
+
+// To other pages, so nothing that is written is read.  A workgroup has some entries of a list: the rows of K and V of its head or, where one
+// list is for all heads, of all of them, which lie side by side.
+constexpr uint32_t kCopyEntries = 32;
+template <int D, int kBits>
+__global__ void __launch_bounds__(256) keep_copy_kernel(const KeepArgs g)
+{
+    constexpr uint32_t kChunks = kBits == 16 ? D / 8 : D / 32;
+    constexpr uint32_t kAhead = 4;                                       // vectors of a lane in flight
+    __shared__ Place from[kCopyEntries], to[kCopyEntries];
+    const tent_kv_keep_args& a = g.a;
+    // All heads of some entries go to one XCD one after the other: heads of a token share lines of its page.
+    const uint32_t block = g.first + blockIdx.x, eight = block / (8 * a.n_lists), in_eight = block - eight * 8 * a.n_lists;
+    const uint32_t unit = eight * 8 + in_eight % 8, head = in_eight / 8;
+    if (unit >= g.b.n_seqs * g.parts) return;
+    const uint32_t seq = unit % g.b.n_seqs, j0 = unit / g.b.n_seqs * kCopyEntries;
+    const KvSeq q = kv_sequence(g.b, seq);
+    const Kept k = kept_of(a, q, seq);
+    if (head == 0 && j0 == 0 && threadIdx.x == 0) tell_length(g, k, seq);
+    if (k.bad || j0 >= (uint32_t)k.count) return;
+    const uint32_t n = (uint32_t)k.count - j0 < kCopyEntries ? (uint32_t)k.count - j0 : kCopyEntries;
+    if (threadIdx.x < n) {
+        const int32_t j = (int32_t)(j0 + threadIdx.x), entry = a.lists[((uint64_t)seq * a.n_lists + head) * a.list_stride + j];
+        Place read{kNowhere, 0}, write{kNowhere, 0};
+        if (!entry_ok(a, k, entry, j)) {
+            kv_note(g.b.errors, TENT_KV_BAD_POSITION);
+        } else {
+            read = place_of(g.c, g.b.page_table + (uint64_t)seq * g.b.table_stride, g.b.table_stride, (uint32_t)(k.base + entry), head);
+            write = place_of(g.c, a.to_table + (uint64_t)seq * a.to_stride, a.to_stride, (uint32_t)(k.base + j), head);
+            if (read.page == kNowhere || write.page == kNowhere) {
+                kv_note(g.b.errors, TENT_KV_BAD_PAGE);
+                read.page = kNowhere;
             }
         }
-        __syncthreads();                                                 // the places are written anew
+        from[threadIdx.x] = read;
+        to[threadIdx.x] = write;
+    }
+    __syncthreads();
+    const uint32_t heads = a.n_lists == 1 ? g.c.heads : 1u, wide = heads * kChunks, half = n * wide, items = 2 * half;      // vectors of K, and of both
+    for (uint32_t first = threadIdx.x; first < items; first += kAhead * 256) {
+        u32x4 v[kAhead];
+        uint8_t* where[kAhead];
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) {
+            const uint32_t item = first + i * 256 < items ? first + i * 256 : first;
+            const bool is_v = item >= half;
+            const uint32_t y = is_v ? item - half : item, e = y / wide, chunk = y - e * wide;
+            const Place p = from[e], t = to[e];
+            uint8_t* const pool = is_v ? g.c.v : g.c.k;
+            where[i] = p.page == kNowhere ? nullptr : pool + t.page + (uint64_t)t.row * (kChunks * 16) + chunk * 16;
+            v[i] = dev_load<u32x4>(p.page == kNowhere ? pool : pool + p.page + (uint64_t)p.row * (kChunks * 16) + chunk * 16);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i)
+            if (first + i * 256 < items && where[i]) dev_store(where[i], v[i]);
+    }
+    if constexpr (kBits == 4) {
+        for (uint32_t item = threadIdx.x; item < 2 * n * heads; item += 256) {
+            const bool is_v = item >= n * heads;
+            const uint32_t y = is_v ? item - n * heads : item, e = y / heads, h = y - e * heads;
+            Place p = from[e], t = to[e];
+            if (p.page == kNowhere) continue;
+            p.row += h;
+            t.row += h;
+            uint8_t* const pool = is_v ? g.c.v : g.c.k;
+            dev_store(pool + scales_at<D>(g.c, t), dev_load<Scales<D>>(pool + scales_at<D>(g.c, p)));
+        }
     }
 }
 
@@ -268,16 +446,16 @@ template <int D, int kBits>
 int launch_keep(KeepArgs g, hipStream_t s)
 {
     constexpr uint32_t kChunks = kBits == 16 ? D / 8 : D / 32;
-    const uint64_t lists = (uint64_t)g.b.n_seqs * 2 * g.c.heads;
-    g.columns = 1;
-    g.parts = 1;
     if (g.a.to_table) {
-        g.parts = (g.a.most + kEntries - 1) / kEntries;
-        if (g.parts < 1) g.parts = 1;
-    } else {
-        while (lists * g.columns < 512 && kChunks / g.columns > 4) g.columns *= 2;
+        g.parts = g.a.most ? (g.a.most + kCopyEntries - 1) / kCopyEntries : 1;
+        return launch_blocks(((uint64_t)g.b.n_seqs * g.parts + 7) / 8 * 8 * g.a.n_lists, [&](uint32_t first, uint32_t blocks) {
+            g.first = first;
+            hipLaunchKernelGGL((keep_copy_kernel<D, kBits>), dim3(blocks), dim3(256), 0, s, g);
+        });
     }
-    return launch_blocks(lists * g.columns * g.parts, [&](uint32_t first, uint32_t blocks) {
+    const uint64_t lists = (uint64_t)g.b.n_seqs * g.c.heads;
+    while (lists * g.columns < 512 && kChunks / g.columns > 4) g.columns *= 2;
+    return launch_blocks(lists * g.columns, [&](uint32_t first, uint32_t blocks) {
         g.first = first;
         hipLaunchKernelGGL((keep_kernel<D, kBits>), dim3(blocks), dim3(256), 0, s, g);
     });

@@ -257,12 +257,11 @@ __global__ void __launch_bounds__(256) few_kernel(const WeighArgs g)
 // prompts of 4k tokens, 4 bits).  A workgroup takes a tile of 128 tokens and then the one that is as far from the end: of a prompt
 // the first tile is seen by all rows, the last by few.
 constexpr int32_t kTileTokens = 128;
-template <int D>
-constexpr int many_threads() { return D == 256 ? 512 : 512; }
+constexpr int kManyThreads = 512;
 template <class E, int D, int kBits>
-__global__ void __launch_bounds__(many_threads<D>(), 2) many_kernel(const WeighArgs g)
+__global__ void __launch_bounds__(kManyThreads, 2) many_kernel(const WeighArgs g)
 {
-    constexpr int kBlocks = D == 256 ? 1 : 2, kSubs = 4 / kBlocks, kThreads = many_threads<D>(), kParts = kThreads / 64 / kSubs;  // blocks of 32 tokens of a wave; waves for the tokens; waves for the lines
+    constexpr int kBlocks = D == 256 ? 1 : 2, kSubs = 4 / kBlocks, kThreads = kManyThreads, kParts = kThreads / 64 / kSubs;  // blocks of 32 tokens of a wave; waves for the tokens; waves for the lines
     constexpr int32_t kStepLines = 32 * kParts;
     constexpr int kK = D / 16, kItems = (kStepLines * D / 8 + kThreads - 1) / kThreads;          // vectors of a step that a thread loads
     constexpr int kApart = kThreads * 8 / D;                             // lines between them, a multiple of 16
@@ -520,7 +519,7 @@ int launch(bool few, WeighArgs g, hipStream_t s)
     g.tiles = (uint32_t)((max_kv + 2 * kTileTokens - 1) / (2 * kTileTokens));
     const int rc = launch_blocks((uint64_t)g.tiles * g.b.n_seqs * g.c.heads, [&](uint32_t first, uint32_t blocks) {
         g.first = first;
-        hipLaunchKernelGGL((many_kernel<E, D, kBits>), dim3(blocks), dim3(many_threads<D>()), 0, s, g);
+        hipLaunchKernelGGL((many_kernel<E, D, kBits>), dim3(blocks), dim3(kManyThreads), 0, s, g);
     }, kMostBlocks / 4);
     if (rc != TENT_OK || !g.by_head) return rc;
     return launch_blocks((max_kv + 255) / 256 * g.b.n_seqs, [&](uint32_t first, uint32_t blocks) {
