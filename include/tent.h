@@ -649,7 +649,7 @@ int tent_kv_attend(const tent_kv_cache *cache, const tent_kv_batch *batch, const
  * and graphs holds for them; none takes atomics but the error bits, so results repeat bit for bit.
  */
 enum { TENT_KV_KEEP_ROWS = 1u << 0 };                       /* tent_kv_keep_args.flags: lists name rows, not tokens   */
-enum { TENT_KV_MAX_VOCAB = 1 << 24 };
+enum { TENT_KV_MAX_VOCAB = 1 << 20 };
 
 typedef struct {
     const uint64_t *masks;     /* device [n_rows][mask_stride]: bit j of a row's words: it sees row j of its sequence */

@@ -62,7 +62,7 @@ SLICE_DTYPE = np.dtype(
 TENT_BF16, TENT_FP16, TENT_FP32 = 0, 1, 2
 TENT_KV_BAD_SEQUENCE, TENT_KV_BAD_PAGE, TENT_KV_BAD_POSITION, TENT_KV_BAD_TOKEN = 1, 2, 4, 8
 TENT_KV_MAX_HEADS, TENT_KV_MAX_PAGE_TOKENS = 1024, 1024
-TENT_KV_MAX_VOCAB = 1 << 24
+TENT_KV_MAX_VOCAB = 1 << 20
 TENT_KV_ROPE_PAIRS, TENT_KV_ATTEND_ALL, TENT_KV_KEEP_ROWS = 1, 1, 1
 
 

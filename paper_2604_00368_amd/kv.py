@@ -359,6 +359,8 @@ _PROBABILITIES = {**_TYPES, torch.float32: T.TENT_FP32}
 
 def _vector(tensor, name, dtype, n, device):
     """A contiguous tensor of `n` values on `device`; its address."""
+    if type(tensor) is torch.Tensor and tensor.dtype is dtype and tensor.shape == (n,) and tensor.device == device and not tensor.requires_grad and tensor.is_contiguous():
+        return tensor.data_ptr()
     if not _on_gpu(tensor, name, dtype, (n,)).is_contiguous() or tensor.device != device:
         raise ValueError(f"{name} must be contiguous, on the batch's device")
     return tensor.data_ptr()

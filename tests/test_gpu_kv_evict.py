@@ -456,7 +456,7 @@ def test_a_run_of_speculation_and_eviction(kv, bits):
 def test_steps_in_a_graph(kv):
     """A step of all five, captured and replayed with other inputs in the same tensors, between eager steps and synchronizations."""
     rows, before = [5, 1, 9], [3000, 40, 511]
-    n, total, vocab = 3, 15, 20000
+    n, total, vocab = 3, 15, 140001
     s = Setup(kv, rows, [r + b for r, b in zip(rows, before)], BF16, 16, 8, 2, 128, 16, seed=50)
     trees = [[i - 1 if i % 2 else max(0, i - 2) - (i == 0) for i in range(r)] for r in rows]
     parents = torch.tensor([p for t in trees for p in t], **I32)
@@ -518,12 +518,12 @@ def test_steps_in_a_graph(kv):
 
 def test_calls_on_several_streams_do_not_share_their_workspaces(kv):
     from test_gpu_kv_tree import Drafts
-    sets = [Drafts(kv, [9, 17, 5], 50257, torch.float32, True, seed=60 + i) for i in range(3)]
+    sets = [Drafts(kv, [9, 17, 5], 140001, torch.float32, True, seed=60 + i) for i in range(3)]
     ins = [(d.target.cuda(), d.tokens.cuda(), d.accept.cuda(), d.next.cuda(), d.parents.cuda(), d.draft.cuda()) for d in sets]
     want = [kv.verify(d.batch, *x) for d, x in zip(sets, ins)]
     for d, w in zip(sets, want):
         d.check(*w)
-    need = kv.verify_workspace(sets[0].batch, 50257, parents=True, draft=True)
+    need = kv.verify_workspace(sets[0].batch, 140001, parents=True, draft=True)
     assert need > 0
     streams = [torch.cuda.Stream() for _ in range(3)]
     torch.cuda.synchronize()

@@ -247,7 +247,7 @@ class Drafts:
         return lengths
 
 
-VOCABS = [1, 2, 63, 1000, 8191, 8192, 8193, 16385, 50257]
+VOCABS = [1, 2, 63, 1000, 2047, 2048, 2049, 8191, 8192, 8193, 16385, 50257, 131072, 131073, 200003]
 
 
 @pytest.mark.parametrize("drawn", [True, False])
@@ -261,8 +261,9 @@ def test_verify(kv, vocab, drawn):
 @pytest.mark.parametrize("drawn", [True, False])
 @pytest.mark.parametrize("dtype", [BF16, FP16, torch.float32])
 @pytest.mark.parametrize("spare", [0, 1, 3, 8])
-def test_verify_types_and_strides(kv, dtype, drawn, spare):
-    d = Drafts(kv, [6, 12, 3, 7], 20011, dtype, drawn, seed=spare + 1, spare=spare)
+@pytest.mark.parametrize("vocab", [20011, 131075])
+def test_verify_types_and_strides(kv, dtype, drawn, spare, vocab):
+    d = Drafts(kv, [6, 12, 3, 7], vocab, dtype, drawn, seed=spare + 1, spare=spare)
     d.check(*d.run())
 
 
@@ -285,9 +286,10 @@ def test_verify_trees_of_many_rows(kv, drawn):
         d.check(*d.run())
 
 
-def test_verify_where_every_row_is_refused(kv):
-    # sums for up to 24 refusals of a sequence, more than are made side by side
-    d = Drafts(kv, [25, 25, 3], 30000, torch.float32, True, seed=3)
+@pytest.mark.parametrize("vocab", [30000, 140001])
+def test_verify_where_every_row_is_refused(kv, vocab):
+    # sums for up to 24 refusals of a sequence, the first of them ahead or not
+    d = Drafts(kv, [25, 25, 3], vocab, torch.float32, True, seed=3)
     d.trees = [[-1] + [0] * (n - 1) for n in d.rows]
     d.parents = torch.tensor([p for t in d.trees for p in t], dtype=torch.int32)
     least = d.target.argmin(1).to(torch.int32)

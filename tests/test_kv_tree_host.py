@@ -39,6 +39,9 @@ def make_keep(T, **change):  # noqa: F811
     return T.tent_kv_keep_args(**{**d, **change})
 
 
+LONG = dict(vocab=1 << 20, target_stride=1 << 20, draft_stride=1 << 20)     # a vocabulary that takes a workspace
+
+
 def calls(T, cache, batch):  # noqa: F811
     L = T.lib()
     return {"tree": L.tent_kv_attend_tree(cache, batch, make_attend(T), make_tree(T), None), "verify": L.tent_kv_verify(batch, make_verify(T), None),
@@ -86,9 +89,9 @@ def test_a_tree_needs_a_bit_for_every_row(T):  # noqa: F811
 @pytest.mark.parametrize("change,status", [
     (dict(target=None), INVALID), (dict(tokens=None), INVALID), (dict(accept=None), INVALID), (dict(next=None), INVALID), (dict(path=None), INVALID), (dict(counts=None), INVALID),
     (dict(token=None), INVALID), (dict(type=3), INVALID), (dict(reserved=1), INVALID), (dict(target=0x1002), INVALID), (dict(draft=0x2001), INVALID), (dict(tokens=0x3001), INVALID),
-    (dict(parents=0x4002), INVALID), (dict(token=0x9001), INVALID), (dict(vocab=0), RANGE), (dict(vocab=(1 << 24) + 1), RANGE), (dict(target_stride=49999), RANGE),
-    (dict(draft_stride=49999), RANGE), (dict(target_stride=1 << 60), RANGE), (dict(path_stride=1), RANGE), (dict(workspace=None), INVALID), (dict(workspace=0x40008), INVALID),
-    (dict(workspace_bytes=8), RANGE)])
+    (dict(parents=0x4002), INVALID), (dict(token=0x9001), INVALID), (dict(vocab=0), RANGE), (dict(vocab=(1 << 20) + 1), RANGE), (dict(target_stride=49999), RANGE),
+    (dict(draft_stride=49999), RANGE), (dict(target_stride=1 << 60), RANGE), (dict(path_stride=1), RANGE), (dict(workspace=None, **LONG), INVALID), (dict(workspace=0x40008, **LONG), INVALID),
+    (dict(workspace_bytes=8, **LONG), RANGE)])
 def test_verify_arguments_that_are_refused(T, change, status):  # noqa: F811
     assert T.lib().tent_kv_verify(make_batch(T), make_verify(T, **change), None) == status
 
@@ -233,19 +236,19 @@ def scenario_enqueued():
         same(names(lambda: L.tent_kv_keep(make_cache(T), batch, make_keep(T), stream)), ["keep_kernel"])
         same(names(lambda: L.tent_kv_weigh(make_cache(T), batch, make_weigh(T), stream)), ["few"])
     for kind in range(3):
-        for change in (dict(), dict(draft=None), dict(parents=None), dict(vocab=100), dict(vocab=1 << 24, target_stride=1 << 24, draft_stride=1 << 24)):
+        for change in (dict(), dict(draft=None), dict(parents=None), dict(vocab=100), dict(vocab=1 << 20, target_stride=1 << 20, draft_stride=1 << 20)):
             args, n = make_verify(T, type=kind, path_stride=4000, **change), C.c_uint64()
             for batch in (short, many):
                 assert L.tent_kv_verify_workspace(batch, args, n) == 0
                 got = names(lambda: L.tent_kv_verify(batch, args, stream))
-                assert "last" in got[-1] and all("pieces" in x for x in got[:-1])
+                assert "verify_kernel" in got[-1] and all("ahead" in x for x in got[:-1]) and len(got) <= 2 and (len(got) == 2) == (n.value > 0)
                 args.workspace_bytes = n.value
                 assert L.tent_kv_verify(batch, args, stream) == 0
                 if n.value:
                     args.workspace_bytes -= 1
                     assert L.tent_kv_verify(batch, args, stream) == RANGE
                 args.workspace_bytes = 1 << 40
-        same(names(lambda: L.tent_kv_verify(make_batch(T, n_rows=0), make_verify(T, target=None, tokens=None, accept=None, next=None), stream)), ["last"])
+        same(names(lambda: L.tent_kv_verify(make_batch(T, n_rows=0), make_verify(T, target=None, tokens=None, accept=None, next=None), stream)), ["verify_kernel"])
 
 
 def test_calls_enqueue_kernels_only(fake):  # noqa: F811
@@ -283,7 +286,7 @@ def scenario_large_calls():
     assert small(lambda: L.tent_kv_weigh(heads, every, make_weigh(T, q_heads=1024, q_stride=65536, n_lists=1024, weights_stride=64), None)) >= 65535 * 1024
     long = make_batch(T, n_rows=1, max_rows=1, n_seqs=1, max_kv=1 << 30, table_stride=1 << 30)
     assert small(lambda: L.tent_kv_weigh(tiny, long, make_weigh(T, q_heads=1, q_stride=64, n_lists=1, weights_stride=1 << 30), None)) > 1000
-    assert small(lambda: L.tent_kv_verify(every, make_verify(T, vocab=1 << 24, target_stride=1 << 24, draft_stride=1 << 24), None)) > 65535
+    assert small(lambda: L.tent_kv_verify(every, make_verify(T, vocab=1 << 20, target_stride=1 << 20, draft_stride=1 << 20), None)) > 65535
 
 
 def test_calls_of_any_size_stay_below_what_a_launch_takes(fake):  # noqa: F811
