@@ -286,7 +286,9 @@ def scenario_large_calls():
     assert small(lambda: L.tent_kv_weigh(heads, every, make_weigh(T, q_heads=1024, q_stride=65536, n_lists=1024, weights_stride=64), None)) >= 65535 * 1024
     long = make_batch(T, n_rows=1, max_rows=1, n_seqs=1, max_kv=1 << 30, table_stride=1 << 30)
     assert small(lambda: L.tent_kv_weigh(tiny, long, make_weigh(T, q_heads=1, q_stride=64, n_lists=1, weights_stride=1 << 30), None)) > 1000
-    assert small(lambda: L.tent_kv_verify(every, make_verify(T, vocab=1 << 20, target_stride=1 << 20, draft_stride=1 << 20), None)) > 65535
+    assert small(lambda: L.tent_kv_verify(every, make_verify(T, vocab=1 << 20, target_stride=1 << 20, draft_stride=1 << 20), None)) == 65535
+    few = make_batch(T, n_seqs=128, n_rows=1280, max_rows=10)
+    assert small(lambda: L.tent_kv_verify(few, make_verify(T, path_stride=10, **LONG), None)) == 128 * (512 // 4 + 1)
 
 
 def test_calls_of_any_size_stay_below_what_a_launch_takes(fake):  # noqa: F811
