@@ -721,9 +721,10 @@ typedef struct {
 /* tent_kv_attend for rows that are a tree (or anything else that masks say): with base = kv_len - its sequence's rows, a row sees the
  * context, tokens 0 .. base - 1, and token base + j where bit j of its mask is set and row j is one of its sequence.  Of a window (at
  * least max_rows, else TENT_ERR_RANGE) the rows that its mask names come first, the last tokens of the context have the rest.
- * TENT_KV_ATTEND_ALL is refused.  The workspace is tent_kv_attend_workspace's. */
+ * TENT_KV_ATTEND_ALL is refused.  The workspace is a tree's own. */
 int tent_kv_attend_tree(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_attend_args *args, const tent_kv_tree *tree,
                         void *stream);
+int tent_kv_attend_tree_workspace(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_attend_args *args, uint64_t *bytes);
 
 /* Which rows of a sequence stand, and the token behind them.  The first row stands.  From the row c that stands last the rows behind it
  * are tried in their order: row i with token x stands if accept[i] * draft[c][x] < r[x], and then it is tried from there; r is target[c]

@@ -30,7 +30,7 @@ EXPORTS = ["tent_create", "tent_destroy", "tent_register_segment", "tent_declare
            "tent_sim_fail", "tent_get_retries", "tent_monitor_init", "tent_monitor_update",
            "tent_plan_dispatch", "tent_get_modes", "tent_execute_bounded", "tent_probe_copy", "tent_declare_static",
            "tent_kv_packed_page", "tent_kv_append", "tent_kv_pack", "tent_kv_read", "tent_kv_attend_workspace", "tent_kv_attend",
-           "tent_kv_attend_tree", "tent_kv_verify_workspace", "tent_kv_verify", "tent_kv_weigh_workspace", "tent_kv_weigh", "tent_kv_choose", "tent_kv_keep"]
+           "tent_kv_attend_tree_workspace", "tent_kv_attend_tree", "tent_kv_verify_workspace", "tent_kv_verify", "tent_kv_weigh_workspace", "tent_kv_weigh", "tent_kv_choose", "tent_kv_keep"]
 
 
 class tent_config(C.Structure):
@@ -180,6 +180,7 @@ def lib():
         L.tent_kv_read.argtypes = [cache, batch, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
         L.tent_kv_attend_workspace.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.POINTER(C.c_uint64)]
         L.tent_kv_attend.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.c_void_p]
+        L.tent_kv_attend_tree_workspace.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.POINTER(C.c_uint64)]
         L.tent_kv_attend_tree.argtypes = [cache, batch, C.POINTER(tent_kv_attend_args), C.POINTER(tent_kv_tree), C.c_void_p]
         L.tent_kv_verify_workspace.argtypes = [batch, C.POINTER(tent_kv_verify_args), C.POINTER(C.c_uint64)]
         L.tent_kv_verify.argtypes = [batch, C.POINTER(tent_kv_verify_args), C.c_void_p]
@@ -424,6 +425,12 @@ def tent_kv_attend_workspace(cache: tent_kv_cache, batch: tent_kv_batch, args: t
 
 def tent_kv_attend(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_attend_args, stream=None):
     _check(lib().tent_kv_attend(cache, batch, args, _stream(stream)), "tent_kv_attend")
+
+
+def tent_kv_attend_tree_workspace(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_attend_args) -> int:
+    n = C.c_uint64()
+    _check(lib().tent_kv_attend_tree_workspace(cache, batch, args, n), "tent_kv_attend_tree_workspace")
+    return n.value
 
 
 def tent_kv_attend_tree(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_attend_args, tree: tent_kv_tree, stream=None):

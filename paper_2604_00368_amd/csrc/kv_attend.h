@@ -1,4 +1,5 @@
-// Softmax attention over the pages of a key/value cache: tent_kv_attend.
+// Softmax attention over the pages of a key/value cache: tent_kv_attend, and with kTree tent_kv_attend_tree, whose rows see of each other what
+// their masks name (struct Sight).
 //
 //   s_rt = scale q_r . k_t,  m_r = max_t s_rt,  l_r = sum_t exp(s_rt - m_r),  o_r = sum_t exp(s_rt - m_r) v_t / l_r
 //
@@ -12,7 +13,8 @@
 //   narrow_kernel  up to 64 lines: 16 lines to a matrix tile, each wave takes tokens of its own, the cache streams from HBM
 //                  through registers; bound by its loads
 //   wide_kernel    more lines: 128 to a workgroup, 32 to a wave, tiles of 64 tokens in LDS for all four waves; bound by the
-//                  matrix units and the softmax's vector work beside them
+//                  matrix units and the softmax's vector work beside them.  For trees of 33 to 64 lines 64 to a workgroup, of
+//                  which two waves take 32, each half of a tile's tokens
 //
 // Measured, 32 heads on 8 of 128 dimensions: 32 rows over 2k-8k tokens each in 4 bits 44 us and 5 for the join (152 MB, 3.4 TB/s; no more
 // than that is read from memory), over 16-bit pages 114 (573 MB, 5.0 TB/s); 8 rows over 100k-131k tokens in 4 bits 69 + 8 us (256 MB, 3.7
@@ -876,7 +878,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const AttendArgs g)
 
 // ---- many lines ----------------------------------------------------------------------------------
 constexpr int kWideTile = 64;          // tokens of a step
-constexpr int kWideLines = 128;        // 32 a wave
+constexpr int kWideLines = 128;        // 32 a wave, where four waves have lines of their own
 
 // What a workgroup is for.  Heads vary fastest, so a head stays on an XCD where there are eight, and its tokens in that XCD's cache;
 // the rows that see the most tokens come first.
@@ -896,10 +898,14 @@ __device__ __forceinline__ WideUnit wide_unit(const AttendArgs& g, uint32_t bloc
 // 32 lines a wave, so that scores, outputs and queries of two waves fit a SIMD's registers (one wave for 256 dimensions): a wave's
 // vector work can run beside the other's products as well as beside its own.  Four waves share a tile because LDS, read by every wave
 // in full, would otherwise be what is short: 128 bytes a cycle feed four SIMDs of these products exactly.
-template <class E, int D, int kBits, bool kTree>
+// kGroups: waves with lines of their own, 4 or 2.  Two lots of 32 lines have two waves each, which take half of a tile's tokens, 32, and whose
+// sums are joined at the end.
+template <class E, int D, int kBits, bool kTree, int kGroups>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const AttendArgs g)
 {
     constexpr int kK = D / 16, kDims = D / 32;
+    constexpr int kS = kGroups / 2, kLines = 32 * kGroups;               // lots of 32 tokens that a wave takes of a tile; lines of the workgroup
+    constexpr int kPairs = 8 * kS;                                       // of a lane's weights
     constexpr int kPerRow = kBits == 16 ? D / 8 : D / 32;                // lanes to a row
     constexpr int kItems = 2 * kWideTile * kPerRow / 256;                // of a thread: K's rows, then V's
     constexpr uint32_t kPlane = kWideTile * D * 2;
@@ -909,25 +915,27 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
     __shared__ RowAt<kBits> rows_at[4][kWideTile];
     __shared__ uint64_t there_lds[4];
     __shared__ uint32_t unfinite_lds;                                    // a value was infinite or NaN in a tile that is not whole
+    __shared__ f32x2 joined[kGroups == 4 ? 1 : 2][kGroups == 4 ? 1 : 64]; // maxima and sums of the waves with the second tokens
 
     const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t m = lane & 31u, upper = lane >> 5;
+    const uint32_t lot = kGroups == 4 ? wave : wave & 1u, part = kGroups == 4 ? 0u : wave >> 1;      // of the lines; of a tile's tokens
     const WideUnit unit = wide_unit(g, g.first + blockIdx.x);
     const uint32_t head = unit.head, seq = unit.seq, split = unit.split, line_tile = unit.line_tile;
     const KvSeq q = kv_sequence(g.b, seq);
     if (q.bad && threadIdx.x == 0 && split == 0 && head == 0 && line_tile == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
-    const int32_t lines = q.rows * (int32_t)g.group, line0 = (int32_t)line_tile * kWideLines;
+    const int32_t lines = q.rows * (int32_t)g.group, line0 = (int32_t)line_tile * kLines;
     if (line0 >= lines || split >= splits_of<kTree>(g, q)) return;
-    const int32_t last_line = line0 + kWideLines < lines ? line0 + kWideLines - 1 : lines - 1;
+    const int32_t last_line = line0 + kLines < lines ? line0 + kLines - 1 : lines - 1;
     const Range range = token_range<kTree>(g, q, line0, last_line, split);
 
-    const int32_t line = line0 + (int32_t)(wave * 32 + m);
+    const int32_t line = line0 + (int32_t)(lot * 32 + m);
     const bool mine = line < lines;
     const int32_t row = mine ? line / (int32_t)g.group : q.rows - 1, h = mine ? line - row * (int32_t)g.group : 0;
     const Sight<kTree> see = sight<kTree>(g, q, row);
     const uint32_t q_head = head * g.group + (uint32_t)h;
     // what the wave's first and last lines see
-    const int32_t wave_first = line0 + (int32_t)wave * 32, wave_last = wave_first + 31 < lines ? wave_first + 31 : lines - 1;
+    const int32_t wave_first = line0 + (int32_t)lot * 32, wave_last = wave_first + 31 < lines ? wave_first + 31 : lines - 1;
     const bool idle = wave_first >= lines;
     const int32_t first_row = idle ? 0 : wave_first / (int32_t)g.group, last_row = idle ? 0 : wave_last / (int32_t)g.group;
     const KvSpan wave_any = seen_by_any<kTree>(g, q, first_row, last_row), wave_all = seen_by_rows<kTree>(g, q, first_row, last_row);
@@ -1040,18 +1048,18 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         if (unfinite) unfinite_lds = 1;
     };
 
-    // S^T of a tile, in s[a][i] the score of token 32 a + 8 (i / 4) + 4 upper + i % 4.  Operands are read two steps ahead; `beside(k)`
+    // S^T of a tile, in s[a][i] the score of token 32 (a + part) + 8 (i / 4) + 4 upper + i % 4.  Operands are read two steps ahead; `beside(k)`
     // is done beside step k, and nothing is moved from step to step.
-    auto scores = [&](const uint8_t* from, f32x16 (&s)[2], auto beside) {
+    auto scores = [&](const uint8_t* from, f32x16 (&s)[kS], auto beside) {
         const uint32_t x = spread<D>(upper) ^ k_swap(m);                 // the same 32 tokens on
-        const uint8_t* p = from + m * (D * 2);
-        u32x4 kf[kK][2];
+        const uint8_t* p = from + (kGroups == 4 ? m : part * 32 + m) * (D * 2);
+        u32x4 kf[kK][kS];
         auto read = [&](int k) {
 #pragma unroll
-            for (int a = 0; a < 2; ++a) kf[k][a] = *(const u32x4*)(p + a * (32 * D * 2) + ((spread<D>(2 * k) ^ x) << 4));
+            for (int a = 0; a < kS; ++a) kf[k][a] = *(const u32x4*)(p + a * (32 * D * 2) + ((spread<D>(2 * k) ^ x) << 4));
         };
 #pragma unroll
-        for (int a = 0; a < 2; ++a)
+        for (int a = 0; a < kS; ++a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[a][i] = 0.f;
         read(0);
@@ -1060,15 +1068,15 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         for (int k = 0; k < kK; ++k) {
             if (k + 2 < kK) read(k + 2);
 #pragma unroll
-            for (int a = 0; a < 2; ++a) s[a] = E::mfma32(kf[k][a], qf[k], s[a]);
+            for (int a = 0; a < kS; ++a) s[a] = E::mfma32(kf[k][a], qf[k], s[a]);
             beside(k);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto largest = [&](const f32x16 (&s)[2]) -> float {
+    auto largest = [&](const f32x16 (&s)[kS]) -> float {
         float big = s[0][0];
 #pragma unroll
-        for (int i = 1; i < 32; ++i) big = fmaxf(big, s[i >> 4][i & 15]);
+        for (int i = 1; i < 16 * kS; ++i) big = fmaxf(big, s[i >> 4][i & 15]);
         return big;
     };
 
@@ -1079,7 +1087,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
     uint64_t there = 0;
     float big_of = 0.f;                                                  // largest of a step's scores, of this lane's
     // `k_from` has the next tile's keys, `v_from` this tile's values.
-    auto step = [&](int32_t tile, f32x16 (&s)[2], f32x16 (&next)[2], uint8_t* k_from, uint8_t* k_to, uint8_t* v_from, uint8_t* v_to) {
+    auto step = [&](int32_t tile, f32x16 (&s)[kS], f32x16 (&next)[kS], uint8_t* k_from, uint8_t* k_to, uint8_t* v_from, uint8_t* v_to) {
         const int32_t t0 = range.lo + tile * kWideTile;
         load_rows(tile + 2, k_to, tile + 1, v_to);
         const uint64_t there_next = same_in_wave(there_lds[(tile + 1) & 3]);
@@ -1093,9 +1101,9 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
                     if (see.hi < t0 + kWideTile) seen = see.hi > t0 ? seen & ~(~0ull << (see.hi - t0)) : 0;
                     if (see.lo > t0) seen = see.lo < t0 + kWideTile ? seen & ~0ull << (see.lo - t0) : 0;
                 }
-                seen >>= 4 * upper;
+                seen >>= 32 * part + 4 * upper;
 #pragma unroll
-                for (int a = 0; a < 2; ++a) {
+                for (int a = 0; a < kS; ++a) {
                     const uint32_t half = (uint32_t)(seen >> (32 * a));
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[a][i] = half & (1u << (8 * (i >> 2) + (i & 3))) ? s[a][i] : -INFINITY;
@@ -1110,7 +1118,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
                 for (int d = 0; d < kDims; ++d) o[d] = o[d] * f * f;
             }
             const float against = E::kWeightShift - (top == -INFINITY ? 0.f : top);
-            u32x4 p[4];
+            u32x4 p[kPairs / 4];
             float add[2] = {0.f, 0.f};
             auto weights = [&](int from, int to) {                       // pairs of them
 #pragma unroll
@@ -1124,10 +1132,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             };
             // O^T's first operand: step u takes tokens 16 u + {0, 8} + 4 upper + 0 .. 3
             const uint32_t i16 = lane & 15u, low = 2 * ((lane >> 4) & 1u) + ((i16 >> 1) & 1u);
-            constexpr int kSteps = 4 * kDims;
+            constexpr int kSteps = 2 * kS * kDims;
             u32x4 vf[kSteps];
             auto read = [&](int i) {
-                const uint32_t ta = 16 * (i / kDims) + 4 * upper + (i16 >> 2);
+                const uint32_t ta = 32 * part + 16 * (i / kDims) + 4 * upper + (i16 >> 2);
                 const uint8_t *row_a = v_from + ta * (D * 2) + (i16 & 1u) * 8, *row_b = row_a + 8 * (D * 2);
                 const uint32_t at = (spread<D>(4 * (i % kDims)) ^ spread<D>(low) ^ v_swap(ta)) << 4;     // the same eight tokens on
                 const u32x2 a = read_transposed(row_a + at), b = read_transposed(row_b + at);
@@ -1135,7 +1143,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             };
             __builtin_amdgcn_sched_barrier(0);
             scores(k_from, next, [&](int k) {
-                weights(12 * k / kK, 12 * (k + 1) / kK);
+                weights(kPairs * 3 / 4 * k / kK, kPairs * 3 / 4 * (k + 1) / kK);
                 if (k == kK - 1) { read(0); read(1); }
             });
             big_of = next[0][0];
@@ -1144,10 +1152,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
                 if (i + 2 < kSteps) read(i + 2);
                 o[i % kDims] = E::mfma32(vf[i], p[i / kDims], o[i % kDims]);
                 if (i < kSteps / 2) {
-                    weights(12 + 4 * i / (kSteps / 2), 12 + 4 * (i + 1) / (kSteps / 2));
+                    weights(kPairs * 3 / 4 + kPairs / 4 * i / (kSteps / 2), kPairs * 3 / 4 + kPairs / 4 * (i + 1) / (kSteps / 2));
                 } else {
 #pragma unroll
-                    for (int j = 32 * (i - kSteps / 2) / (kSteps / 2); j < 32 * (i + 1 - kSteps / 2) / (kSteps / 2); ++j) big_of = fmaxf(big_of, next[j >> 4][j & 15]);
+                    for (int j = 16 * kS * (i - kSteps / 2) / (kSteps / 2); j < 16 * kS * (i + 1 - kSteps / 2) / (kSteps / 2); ++j) big_of = fmaxf(big_of, next[j >> 4][j & 15]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -1183,7 +1191,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kK; ++k) arrived(qf[k]);
-        f32x16 s0[2], s1[2];
+        f32x16 s0[kS], s1[kS];
         scores(k_even, s0, [](int) {});
         big_of = largest(s0);
         __syncthreads();
@@ -1194,6 +1202,29 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
     }
 
     if (bad_page) kv_note(g.b.errors, TENT_KV_BAD_PAGE);
+    sum = sum_over32(sum);
+    if constexpr (kGroups == 2) {
+        // The waves with the second tokens hand theirs over: what takes a tile in the loop holds a wave's sums exactly.  The loop's last
+        // barrier is behind its last read.
+        float* const theirs = (float*)(lot ? v_even : k_even);
+        if (part) {
+#pragma unroll
+            for (int d = 0; d < kDims; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) theirs[(d * 16 + i) * 64 + lane] = o[d][i];
+            joined[lot][lane] = f32x2{top, sum};
+        }
+        __syncthreads();
+        if (part) return;
+        const f32x2 other = joined[lot][lane];
+        const float now = fmaxf(top, other[0]), mine_by = rescale(top, now), theirs_by = rescale(other[0], now);
+        sum = sum * mine_by * mine_by + other[1] * theirs_by * theirs_by;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * mine_by * mine_by + theirs[(d * 16 + i) * 64 + lane] * theirs_by * theirs_by;
+        top = now;
+    }
     if (tiles > 0 && unfinite_lds && !idle) {                            // behind the loop's last barrier
 #pragma unroll 1
         for (int32_t tile = 0; tile < tiles; ++tile) {
@@ -1221,7 +1252,6 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             }
         }
     }
-    sum = sum_over32(sum);
     bool large = false;                                                  // this line's sums passed 32 bits
     if constexpr (E::kLarge) {
         float x = 0.f;
@@ -1235,10 +1265,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) wide_kernel(const Atten
             const AttendArgs& a = args_again();
             const WideUnit u = wide_unit(a, a.first + blockIdx.x);
             const KvSeq q = kv_sequence(a.b, u.seq);
-            const int32_t line0 = (int32_t)u.line_tile * kWideLines, lines = q.rows * (int32_t)a.group;
-            const Range range = token_range<kTree>(a, q, line0, line0 + kWideLines < lines ? line0 + kWideLines - 1 : lines - 1, u.split);
+            const int32_t line0 = (int32_t)u.line_tile * kLines, lines = q.rows * (int32_t)a.group;
+            const Range range = token_range<kTree>(a, q, line0, line0 + kLines < lines ? line0 + kLines - 1 : lines - 1, u.split);
             const Unfinite<D> unfinite = find_unfinite<E, D, kBits>(a, u.seq, u.head, range);
-            const int32_t first_line = line0 + (int32_t)wave * 32, my_line = first_line + (int32_t)(lane_again() & 31u);
+            const int32_t first_line = line0 + (int32_t)lot * 32, my_line = first_line + (int32_t)(lane_again() & 31u);
             const Sight<kTree> see = sight<kTree>(a, q, my_line < lines ? my_line / (int32_t)a.group : 0);
             bool more = false;
 #pragma unroll
@@ -1361,7 +1391,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs g)
 // ---- host ----------------------------------------------------------------------------------------
 struct Shape {
     uint32_t line_tiles;       // narrow: 16-line tiles of a workgroup (1, 2 or 4); wide: workgroups over the lines
-    bool wide;
+    bool wide, half;           // half: 64 lines to a workgroup
     uint32_t n_splits, split_tokens;
     uint64_t workspace;
 };
@@ -1375,19 +1405,25 @@ struct Shape {
 // little, to leave none with much more to do than others.  Three chunks of 511 rows, 384 workgroups, 4 bits, whole and in the rule's
 // three: behind 8k tokens 265 and 275 us, 16k 527 and 511, 32k 1047 and 977; 1024 workgroups stay whole behind 16k (1116, and
 // 1198 in two).
-inline Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_attend_args& a)
+//
+// Trees of 33 to 64 lines take the wide kernel with two waves to 32 lines; the narrow one has one wave to a SIMD then.  16 rows of 32 heads on
+// 8 of 128 dimensions, narrow, wide and so: 32 of them over 5k tokens in 4 bits 160, 131 and 96 us, in 16 bits 222, 153 and 145; 4 over 32k
+// 138, 86 and 83, 189, 125 and 122; 500 tokens 18.5, and 18.5 so, 20.7 and 16.8; of 64 dimensions 13 and 15.  Of these workgroups 512 are
+// enough: 32 trees over 2k to 8k tokens take 149 us with 512, with 256, 1024 and 1536 229, 152 and 168.
+inline Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_attend_args& a, bool tree)
 {
     Shape s{};
     const uint32_t group = a.q_heads / c.kv_heads;
     const uint64_t lines = (uint64_t)b.max_rows * group;
-    s.wide = lines > (c.head_dim == 256 ? 32u : 64u);
+    s.wide = lines > (tree || c.head_dim == 256 ? 32u : 64u);
+    s.half = tree && s.wide && lines <= 64;
     s.line_tiles = s.wide ? (uint32_t)((lines + kWideLines - 1) / kWideLines) : lines <= 16 ? 1 : lines <= 32 ? 2 : 4;
     uint64_t span = b.max_kv;                                            // most tokens that a sequence's rows see together
     if (a.window && !(a.flags & TENT_KV_ATTEND_ALL) && (uint64_t)a.window + b.max_rows < span) span = (uint64_t)a.window + b.max_rows;
     if (a.window && (a.flags & TENT_KV_ATTEND_ALL) && a.window < span) span = a.window;
     span += kStep;                                                       // the first token is rounded down
     const uint64_t units = (uint64_t)b.n_seqs * c.kv_heads * (s.wide ? s.line_tiles : 1);
-    const bool filled = s.wide && units >= 256;
+    const bool filled = s.wide && !s.half && units >= 256;
     const uint64_t wanted = filled ? 1024 : s.wide ? 512 : 1536, least = filled ? 4096 : s.wide ? 512 : 256;
     uint64_t n = (wanted + units - 1) / units, most = filled ? span / least : (span + least - 1) / least;
     n = n > most ? most : n;
@@ -1424,13 +1460,16 @@ int launch(const Shape& s, AttendArgs g, hipStream_t stream)
         const dim3 grid(blocks);
         g.first = first;
         if (s.wide) {
-            hipLaunchKernelGGL((wide_kernel<E, D, kBits, kTree>), grid, threads, 0, stream, g);
+            if constexpr (kTree) {
+                if (s.half) hipLaunchKernelGGL((wide_kernel<E, D, kBits, kTree, 2>), grid, threads, 0, stream, g);
+            }
+            if (!s.half) hipLaunchKernelGGL((wide_kernel<E, D, kBits, kTree, 4>), grid, threads, 0, stream, g);
         } else if (s.line_tiles == 1) {
             hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 1, kTree>), grid, threads, 0, stream, g);
         } else if (s.line_tiles == 2) {
             hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 2, kTree>), grid, threads, 0, stream, g);
         } else {
-            if constexpr (D != 256) hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 4, kTree>), grid, threads, 0, stream, g);
+            if constexpr (D != 256 && !kTree) hipLaunchKernelGGL((narrow_kernel<E, D, kBits, 4, kTree>), grid, threads, 0, stream, g);
         }
     });
     if (rc != TENT_OK) return rc;
@@ -1455,7 +1494,7 @@ int attend(const tent_kv_cache* cache, const tent_kv_batch* batch, const tent_kv
     if ((rc = kv_check_rows(args->q, args->q_stride, args->q_heads, D, batch->n_rows)) != TENT_OK) return rc;
     if ((rc = kv_check_rows(args->out, args->out_stride, args->q_heads, D, batch->n_rows)) != TENT_OK) return rc;
     if ((uintptr_t)args->lse & 3u) return TENT_ERR_INVALID;
-    const Shape s = shape_of(*cache, *batch, *args);
+    const Shape s = shape_of(*cache, *batch, *args, kTree);
     if (s.workspace && (!args->workspace || !kv_aligned(args->workspace))) return TENT_ERR_INVALID;
     if (s.workspace > args->workspace_bytes) return TENT_ERR_RANGE;
     AttendArgs g{};

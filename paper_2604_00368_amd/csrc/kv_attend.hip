@@ -9,7 +9,7 @@ extern "C" int tent_kv_attend_workspace(const tent_kv_cache* cache, const tent_k
     const int rc = check(cache, batch, args);
     if (rc != TENT_OK) return rc;
     if (!bytes) return TENT_ERR_INVALID;
-    *bytes = batch->n_seqs == 0 || batch->n_rows == 0 ? 0 : shape_of(*cache, *batch, *args).workspace;
+    *bytes = batch->n_seqs == 0 || batch->n_rows == 0 ? 0 : shape_of(*cache, *batch, *args, false).workspace;
     return TENT_OK;
 }
 

@@ -59,7 +59,7 @@ struct Bf16 {
     // Softmax weights are held times 2^this, so that those which decide a result near the type's least values (2^-133) are not
     // below what 32 bits and the matrix instructions hold as normal numbers.
     static constexpr float kWeightShift = 16.f;
-    static constexpr bool kLarge = true;                                 // sums of weights times values may pass 32 bits (see kv_attend.hip)
+    static constexpr bool kLarge = true;                                 // sums of weights times values may pass 32 bits (see kv_attend.h)
     static __device__ __forceinline__ float to_float(uint32_t half) { return __uint_as_float(half << 16); }
     static __device__ __forceinline__ uint32_t pack2(float a, float b)
     {
@@ -91,7 +91,7 @@ struct Fp16 {
     using Oct = f16x8;
     static constexpr int kLow = -23, kHigh = 13;
     static constexpr uint32_t kInf = 0x7C00u;
-    // A weight is at most 1 (2^8 while the maximum lags, see kv_attend.hip): times 2^7 it stays below 65504, and weights
+    // A weight is at most 1 (2^8 while the maximum lags, see kv_attend.h): times 2^7 it stays below 65504, and weights
     // down to 2^-21 keep all 11 bits.
     static constexpr float kWeightShift = 7.f;
     static constexpr bool kLarge = false;                                // 2^30 times 2^15 times 65504 is far below

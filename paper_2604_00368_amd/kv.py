@@ -332,7 +332,10 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
     a = T.tent_kv_attend_args(q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else None, q_stride, out_stride, None, 0, heads, window,
                               0 if causal else T.TENT_KV_ATTEND_ALL, 1.0 / math.sqrt(D) if scale is None else scale)
     L, need, ref = T.lib(), C.c_uint64(), C.byref(a)
-    _check(L.tent_kv_attend_workspace(cache.ref, batch.ref, ref, C.byref(need)), "tent_kv_attend_workspace")
+    if tree is None:
+        _check(L.tent_kv_attend_workspace(cache.ref, batch.ref, ref, C.byref(need)), "tent_kv_attend_workspace")
+    else:
+        _check(L.tent_kv_attend_tree_workspace(cache.ref, batch.ref, ref, C.byref(need)), "tent_kv_attend_tree_workspace")
     if need.value:
         if workspace is None:
             workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
@@ -347,11 +350,11 @@ def attend(cache: Cache, batch: Batch, q, scale: float = None, window: int = 0, 
     return (out, lse) if want_lse else out
 
 
-def attend_workspace(cache: Cache, batch: Batch, q_heads: int, window: int = 0, causal: bool = True) -> int:
-    """Bytes of workspace that attend takes for such a batch."""
+def attend_workspace(cache: Cache, batch: Batch, q_heads: int, window: int = 0, causal: bool = True, tree: bool = False) -> int:
+    """Bytes of workspace that attend takes for such a batch, with or without `tree`."""
     _together(cache, batch)
-    return T.tent_kv_attend_workspace(cache.c, batch.c, T.tent_kv_attend_args(q_heads=q_heads, window=window, scale=1.0,
-                                                                             flags=0 if causal else T.TENT_KV_ATTEND_ALL))
+    bytes_of = T.tent_kv_attend_tree_workspace if tree else T.tent_kv_attend_workspace
+    return bytes_of(cache.c, batch.c, T.tent_kv_attend_args(q_heads=q_heads, window=window, scale=1.0, flags=0 if causal else T.TENT_KV_ATTEND_ALL))
 
 
 _PROBABILITIES = {**_TYPES, torch.float32: T.TENT_FP32}
@@ -368,6 +371,10 @@ def _vector(tensor, name, dtype, n, device):
 
 def _by_list(tensor, name, dtype, n_seqs, width, device):
     """A tensor [sequences, values] or [sequences, heads, values] of `width` values at least, lists at one distance; heads, distance."""
+    if type(tensor) is torch.Tensor and tensor.dtype is dtype and tensor.device == device and not tensor.requires_grad and tensor.is_contiguous():
+        shape = tensor.shape
+        if len(shape) in (2, 3) and shape[0] == n_seqs and shape[-1] >= max(width, 1):
+            return shape[1] if len(shape) == 3 else 1, shape[-1]
     _on_gpu(tensor, name, dtype)
     if tensor.device != device or tensor.dim() not in (2, 3) or tensor.shape[0] != n_seqs or tensor.shape[-1] < width:
         raise ValueError(f"{name} must be [sequences, (heads,) values] with {width} values at least, on the batch's device, not {tuple(tensor.shape)}")
@@ -404,15 +411,18 @@ def verify(batch: Batch, target, tokens, accept, next, parents=None, draft=None,
     n, n_seqs, most, device = batch.n_rows, batch.c.n_seqs, batch.c.max_rows, batch.device
     if not isinstance(target, torch.Tensor) or target.dim() != 2 or target.dtype not in _PROBABILITIES:
         raise ValueError("target must be float32, bfloat16 or float16 [rows, vocab]")
-    vocab, strides = target.shape[1], []
-    for x, name in ((target, "target"), (draft, "draft")):
+    vocab, strides = target.shape[1], [0, 0]
+    for i, (x, name) in enumerate(((target, "target"), (draft, "draft"))):
         if x is None:
-            strides.append(0)
             continue
-        _on_gpu(x, name, target.dtype, (n, vocab))
-        if x.device != device or (vocab > 1 and x.stride(1) != 1) or (n > 1 and x.stride(0) < vocab):
-            raise ValueError(f"{name} must have contiguous rows, on the batch's device")
-        strides.append(x.stride(0) if n > 1 else vocab)
+        if type(x) is not torch.Tensor or x.dtype is not target.dtype or x.shape != (n, vocab) or x.device != device or x.requires_grad:
+            _on_gpu(x, name, target.dtype, (n, vocab))
+            if x.device != device:
+                raise ValueError(f"{name} must be on the batch's device")
+        stride = x.stride()
+        if (vocab > 1 and stride[1] != 1) or (n > 1 and stride[0] < vocab):
+            raise ValueError(f"{name} must have contiguous rows (strides {stride})")
+        strides[i] = stride[0] if n > 1 else vocab
     a = T.tent_kv_verify_args(target.data_ptr(), draft.data_ptr() if draft is not None else None, *strides, _vector(tokens, "tokens", torch.int32, n, device),
                               _vector(parents, "parents", torch.int32, n, device) if parents is not None else None,
                               _vector(accept, "accept", torch.float32, n, device), _vector(next, "next", torch.float32, n_seqs, device))

@@ -90,7 +90,7 @@ def test_long_contexts_are_split_and_joined(kv, rows, q_heads, bits):
     rng = random.Random(q_heads)
     seen = [TR.ancestors(some_tree(rng, n)) for n in rows]
     for window in (0, 4096):
-        assert kv.attend_workspace(s.cache, s.batch, q_heads, window) > 0
+        assert kv.attend_workspace(s.cache, s.batch, q_heads, window, tree=True) > 0
         got = [kv.attend(s.cache, s.batch, s.q.cuda(), tree=masks_of(seen, rng=rng), window=window, want_lse=True) for _ in range(2)]
         check_tree(s, seen, *got[0], window)
         assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])

@@ -207,11 +207,12 @@ def scenario_enqueued():
 
     for change in (dict(), dict(type=1), dict(bits=4, page_stride=8704), dict(type=1, bits=4, page_stride=8704)):
         c = make_cache(T, **change)
-        for batch, kinds in ((short, ["narrow"]), (long, ["narrow", "join"]), (many, ["wide"])):
+        sixteen = make_batch(T, n_rows=32, max_rows=16, max_kv=200)
+        for batch, kinds in ((short, ["narrow"]), (long, ["narrow", "join"]), (sixteen, ["wide"]), (many, ["wide"])):
             same(names(lambda: L.tent_kv_attend_tree(c, batch, make_attend(T), make_tree(T, mask_stride=63), stream)), kinds)
         n = C.c_uint64()
         args = make_attend(T)
-        assert L.tent_kv_attend_workspace(c, long, args, n) == 0
+        assert L.tent_kv_attend_tree_workspace(c, long, args, n) == 0
         args.workspace_bytes = n.value
         assert L.tent_kv_attend_tree(c, long, args, make_tree(T), stream) == 0
         args.workspace_bytes -= 1

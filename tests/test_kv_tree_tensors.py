@@ -15,6 +15,9 @@ NAMES = ("attend_tree", "verify", "weigh", "choose", "keep")
 
 
 class Gpus(Base.Gpus):
+    def tent_kv_attend_tree_workspace(self, cache, batch, args, need):
+        return self.tent_kv_attend_workspace(cache, batch, args, need)
+
     def tent_kv_attend_tree(self, cache, batch, args, tree, stream):
         self.words = tree._obj.mask_stride
         return self.call("attend_tree", stream)
