@@ -679,7 +679,7 @@ typedef struct {
     const void *q;             /* device [n_rows][q_heads][head_dim]                               */
     const float *lse;          /* device [n_rows][q_heads], as tent_kv_attend has given them        */
     const float *weights;      /* device [n_seqs][n_lists][weights_stride]: so far, or NULL: 0      */
-    float *weights_out;        /* device, laid out the same; may be `weights`                      */
+    float *weights_out;        /* device, laid out the same; may be `weights`, else shares nothing with it */
     uint64_t q_stride;         /* values from a row to the next                                    */
     uint64_t weights_stride;   /* values from a list to the next, at least max_kv                  */
     void *workspace;           /* device: tent_kv_weigh_workspace bytes; NULL where that is 0       */
@@ -694,7 +694,7 @@ typedef struct {
 typedef struct {
     const float *weights;      /* device [n_seqs][n_lists][weights_stride]                         */
     int32_t *lists;            /* device [n_seqs][n_lists][list_stride]: tokens, ascending, then -1 up to budget */
-    int32_t *counts;           /* device [n_seqs]: how many of them                                 */
+    int32_t *counts;           /* device [n_seqs]: how many of them; not the batch's kv_len         */
     uint64_t weights_stride, list_stride;   /* values, at least max_kv, and at least budget        */
     uint32_t n_lists;          /* 1 .. TENT_KV_MAX_HEADS                                           */
     uint32_t budget;           /* tokens to keep, 1 .. 2^30                                        */
@@ -705,9 +705,9 @@ typedef struct {
     const int32_t *lists;      /* device [n_seqs][n_lists][list_stride]                            */
     const int32_t *counts;     /* device [n_seqs]: entries of a sequence's lists                   */
     const int32_t *to_table;   /* device [n_seqs][to_stride]: pages that the kept tokens go to; NULL: the batch's, in place */
-    int32_t *kv_len_out;       /* device [n_seqs]: tokens afterwards; not the batch's kv_len       */
+    int32_t *kv_len_out;       /* device [n_seqs]: tokens afterwards, or NULL; not the batch's kv_len, nor `counts` */
     const float *weights;      /* device [n_seqs][n_weights][weights_stride]: moved with the tokens; or NULL */
-    float *weights_out;        /* device, laid out the same; in place it may be `weights`          */
+    float *weights_out;        /* device, laid out the same; in place it may be `weights`, else shares nothing with it */
     uint64_t list_stride;      /* entries from a list to the next                                  */
     uint64_t weights_stride;   /* values, at least max_kv                                          */
     uint32_t n_lists;          /* kv_heads: a list for every head of the cache; 1: one for all      */
@@ -739,7 +739,7 @@ int tent_kv_verify(const tent_kv_batch *batch, const tent_kv_verify_args *args, 
 int tent_kv_verify_workspace(const tent_kv_batch *batch, const tent_kv_verify_args *args, uint64_t *bytes);
 
 /* Attention weights onto the tokens: weights_out[s][l][t] = weights[s][l][t] + the sum over the rows that see token t, and the query heads
- * that read head l (with one list all of them), of exp(scale q . k_t - lse).  Written for all t below max_kv: where nothing sees a
+ * that read head l (with one list all of them), of exp(scale q . k_t - lse); rows see what tent_kv_attend lets them see, not a tree.  Written for all t below max_kv: where nothing sees a
  * token its weight stays.  Rows whose lse is not finite add nothing.  A sequence that is left out, or has no rows, keeps its weights. */
 int tent_kv_weigh(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_weigh_args *args, void *stream);
 int tent_kv_weigh_workspace(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_weigh_args *args, uint64_t *bytes);
@@ -754,7 +754,7 @@ int tent_kv_choose(const tent_kv_batch *batch, const tent_kv_choose_args *args, 
  * with base = kv_len - its rows, token base + j becomes what token base + lists[s][l][j] was, and kv_len_out is base + counts[s].
  * In place an entry must not be below its own number j, so that lists may name a token twice and nothing is read that was written;
  * with to_table, whose pages must not be ones that are read, entries may be anything below kv_len (below the rows).  An entry that is not
- * is left out and noted (TENT_KV_BAD_POSITION); wrong pages likewise.  A sequence with a count that is negative, more than
+ * is left out and noted (TENT_KV_BAD_POSITION); wrong pages likewise.  Pages that are written are to be of one sequence.  A sequence with a count that is negative, more than
  * `most`, or more than it has (in place), with
  * rows of which some are at negative positions, and one that is left out, stay as they are, with their kv_len, noted as
  * TENT_KV_BAD_SEQUENCE. */

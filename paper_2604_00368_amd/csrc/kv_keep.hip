@@ -476,6 +476,7 @@ extern "C" int tent_kv_choose(const tent_kv_batch* batch, const tent_kv_choose_a
     if (((uintptr_t)args->weights | (uintptr_t)args->lists | (uintptr_t)args->counts) & 3u) return TENT_ERR_INVALID;
     if (args->n_lists < 1 || args->n_lists > TENT_KV_MAX_HEADS || args->budget < 1 || args->budget > (1u << 30)) return TENT_ERR_RANGE;
     if ((uint64_t)args->first + args->recent > args->budget) return TENT_ERR_RANGE;
+    if (kv_meet(args->counts, batch->n_seqs * 4ull, batch->kv_len, batch->n_seqs * 4ull)) return TENT_ERR_INVALID;     // read by workgroups of every list
     const uint64_t lists = (uint64_t)batch->n_seqs * args->n_lists, most = ((uint64_t)1 << 60) / lists;
     if (args->weights_stride < batch->max_kv || args->weights_stride > most || args->list_stride < args->budget || args->list_stride > most) return TENT_ERR_RANGE;
     ChooseArgs g{*args, *batch, 0};
@@ -494,7 +495,10 @@ extern "C" int tent_kv_keep(const tent_kv_cache* cache, const tent_kv_batch* bat
     if (!args || args->reserved || (args->flags & ~(uint32_t)TENT_KV_KEEP_ROWS)) return TENT_ERR_INVALID;
     if (batch->n_seqs == 0) return TENT_OK;
     if ((rc = kv_check_table(cache, batch)) != TENT_OK) return rc;
-    if ((!args->lists && args->most) || !args->counts || args->kv_len_out == batch->kv_len) return TENT_ERR_INVALID;
+    if ((!args->lists && args->most) || !args->counts) return TENT_ERR_INVALID;
+    const uint64_t a_number_each = batch->n_seqs * 4ull;                 // other workgroups read lengths and counts
+    if (kv_meet(args->kv_len_out, a_number_each, batch->kv_len, a_number_each) || kv_meet(args->kv_len_out, a_number_each, args->counts, a_number_each) ||
+        kv_meet(args->kv_len_out, a_number_each, batch->row_start, a_number_each + 4)) return TENT_ERR_INVALID;
     if (((uintptr_t)args->lists | (uintptr_t)args->counts | (uintptr_t)args->to_table | (uintptr_t)args->kv_len_out | (uintptr_t)args->weights |
          (uintptr_t)args->weights_out) & 3u) return TENT_ERR_INVALID;
     if ((!args->weights) != (!args->weights_out) || (args->to_table && args->weights && args->weights == args->weights_out)) return TENT_ERR_INVALID;
@@ -504,6 +508,7 @@ extern "C" int tent_kv_keep(const tent_kv_cache* cache, const tent_kv_batch* bat
     if (args->weights) {
         if ((args->n_weights != 1 && args->n_weights != cache->kv_heads) || args->n_weights < args->n_lists) return TENT_ERR_RANGE;
         if (args->weights_stride < batch->max_kv || args->weights_stride > most) return TENT_ERR_RANGE;
+        if (kv_lists_meet(args->weights, args->weights_out, (uint64_t)batch->n_seqs * args->n_weights, batch->max_kv, args->weights_stride)) return TENT_ERR_INVALID;
     }
     KeepArgs g{kv_cache_dev(*cache), *batch, *args, 1, 1, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);

@@ -67,6 +67,22 @@ inline int kv_check_table(const tent_kv_cache* c, const tent_kv_batch* b)
     return b->max_kv > (uint64_t)b->table_stride * c->page_tokens ? TENT_ERR_RANGE : TENT_OK;
 }
 
+// Whether one range of bytes has any of another.
+inline bool kv_meet(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && (x < y ? y - x < a_bytes : x - y < b_bytes);
+}
+// Whether values of other places share memory where two tensors have `lists` lists of `width` floats, `stride` (at least width) apart.  They do
+// not where the two are one and the same, nor where lists of one lie between those of the other.
+inline bool kv_lists_meet(const float* a, const float* b, uint64_t lists, uint64_t width, uint64_t stride)
+{
+    if (!a || !b || a == b || !width || !lists) return false;
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    const uint64_t apart = (x < y ? y - x : x - y) / 4, k = apart / stride, r = apart % stride;
+    return (r < width && k < lists) || (stride - r < width && k + 1 < lists);
+}
+
 // Rows of `heads` heads: a base, and a stride that holds them, in whole vectors of 16 bytes.
 inline int kv_check_rows(const void* p, uint64_t stride, uint32_t heads, uint32_t head_dim, uint32_t n_rows)
 {

@@ -3,9 +3,8 @@
 //   w_t += sum over the lines l (rows and query heads of a cache head) that see token t of exp(scale q_l . k_t - lse_l)
 //
 // Both kernels compute S = Q K^T, 32 lines by 32 tokens: a lane then has scores of one token, and adds its weights up in a register.
-// (S^T, with a line to a lane, takes 31 exchanges
-// between lanes for each tile of tokens: 82 us instead of 27 for 32 rows over 5,120 tokens each in 4 bits, 8 heads of 128 dimensions.)  Each weight
-// is written by one workgroup, in an order that does not change.
+// (S^T, with a line to a lane, takes 31 exchanges between lanes for each tile of tokens: 82 us instead of 27 for 32 rows over 5,120 tokens
+// each in 4 bits, 8 heads of 128 dimensions.)  Each weight is written by one workgroup, in an order that does not change.
 //
 //   few_kernel   up to 32 lines: the queries stay in registers, the keys stream through; bound by its loads
 //   many_kernel  more lines: the keys stay, the queries go through LDS for the four waves that share them; bound by the exponentials
@@ -565,6 +564,7 @@ extern "C" int tent_kv_weigh(const tent_kv_cache* cache, const tent_kv_batch* ba
     }
     if ((!args->weights_out && batch->max_kv) || (((uintptr_t)args->lse | (uintptr_t)args->weights | (uintptr_t)args->weights_out) & 3u)) return TENT_ERR_INVALID;
     if (args->weights_stride < batch->max_kv || args->weights_stride > ((uint64_t)1 << 60) / ((uint64_t)batch->n_seqs * args->n_lists)) return TENT_ERR_RANGE;
+    if (kv_lists_meet(args->weights, args->weights_out, (uint64_t)batch->n_seqs * args->n_lists, batch->max_kv, args->weights_stride)) return TENT_ERR_INVALID;
     const uint64_t need = workspace_of(*cache, *batch, *args);
     if (need && (!args->workspace || !kv_aligned(args->workspace))) return TENT_ERR_INVALID;
     if (need > args->workspace_bytes) return TENT_ERR_RANGE;

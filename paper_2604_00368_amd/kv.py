@@ -455,8 +455,8 @@ def weigh(cache: Cache, batch: Batch, q, lse, weights=None, per_head: bool = Tru
     """`weights` and what the batch's rows add to them: the attention weight that each token gets from the rows that see it, [sequences,
     kv_heads, max_kv] (float32; summed over the query heads of a head) or, without per_head, [sequences, max_kv] summed over all heads.
 
-    q, scale, window, causal: as attend had them; lse: float32 [rows, q_heads], what it has said with want_lse.  weights: None for
-    zeros; its lists may be longer than max_kv.  out may be weights.  workspace: a contiguous uint8 tensor of at least weigh_workspace bytes
+    q, scale, window, causal: as attend had them (without `tree`: of a tree the rows that stand can be weighed, once keep has made them the
+    sequence); lse: float32 [rows, q_heads], what it has said with want_lse.  weights: None for zeros; its lists may be longer than max_kv.  out may be weights.  workspace: a contiguous uint8 tensor of at least weigh_workspace bytes
     to use instead of a new one."""
     if stream is not None or cache.index != _current_device():
         used = [x for x in (*cache.tensors, *batch.tensors, q, lse, weights, out, workspace) if x is not None]

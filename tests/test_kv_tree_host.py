@@ -24,17 +24,17 @@ def make_verify(T, **change):  # noqa: F811
 
 
 def make_weigh(T, **change):  # noqa: F811
-    d = dict(q=0x1000, lse=0x2000, weights=0x3000, weights_out=0x4000, q_stride=4096, weights_stride=1000, workspace=0x40000, workspace_bytes=1 << 40, q_heads=32, n_lists=8, window=0, flags=0, scale=0.1, reserved=0)
+    d = dict(q=0x1000, lse=0x2000, weights=0x3000, weights_out=0x3000, q_stride=4096, weights_stride=1000, workspace=0x40000, workspace_bytes=1 << 40, q_heads=32, n_lists=8, window=0, flags=0, scale=0.1, reserved=0)
     return T.tent_kv_weigh_args(**{**d, **change})
 
 
 def make_choose(T, **change):  # noqa: F811
-    d = dict(weights=0x1000, lists=0x2000, counts=0x3000, weights_stride=1000, list_stride=100, n_lists=8, budget=100, first=4, recent=20)
+    d = dict(weights=0x1000, lists=0x2000, counts=0x90000000, weights_stride=1000, list_stride=100, n_lists=8, budget=100, first=4, recent=20)
     return T.tent_kv_choose_args(**{**d, **change})
 
 
 def make_keep(T, **change):  # noqa: F811
-    d = dict(lists=0x1000, counts=0x2000, to_table=None, kv_len_out=0x7000, weights=None, weights_out=None, list_stride=100, weights_stride=0, n_lists=8, n_weights=0,
+    d = dict(lists=0x1000, counts=0x2000, to_table=None, kv_len_out=0x90000000, weights=None, weights_out=None, list_stride=100, weights_stride=0, n_lists=8, n_weights=0,
              to_stride=0, most=100, flags=0, reserved=0)
     return T.tent_kv_keep_args(**{**d, **change})
 
@@ -100,7 +100,7 @@ def test_verify_arguments_that_are_refused(T, change, status):  # noqa: F811
     (dict(q=None), INVALID), (dict(lse=None), INVALID), (dict(weights_out=None), INVALID), (dict(weights=0x3002), INVALID), (dict(lse=0x2001), INVALID), (dict(flags=2), INVALID),
     (dict(reserved=1), INVALID), (dict(q_stride=4100), INVALID), (dict(q_stride=4088), RANGE), (dict(q_heads=0), RANGE), (dict(q_heads=12), RANGE), (dict(n_lists=2), RANGE),
     (dict(n_lists=0), RANGE), (dict(window=(1 << 30) + 1), RANGE), (dict(scale=0.0), RANGE), (dict(scale=math.inf), RANGE), (dict(weights_stride=999), RANGE),
-    (dict(weights_stride=1 << 60), RANGE)])
+    (dict(weights_stride=1 << 60), RANGE), (dict(weights_out=0x3004), INVALID), (dict(weights=0x3000 + 4 * 1999), INVALID)])
 def test_weigh_arguments_that_are_refused(T, change, status):  # noqa: F811
     assert T.lib().tent_kv_weigh(make_cache(T), make_batch(T), make_weigh(T, **change), None) == status
 
@@ -108,17 +108,20 @@ def test_weigh_arguments_that_are_refused(T, change, status):  # noqa: F811
 @pytest.mark.parametrize("change,status", [
     (dict(weights=None), INVALID), (dict(lists=None), INVALID), (dict(counts=None), INVALID), (dict(lists=0x2002), INVALID), (dict(n_lists=0), RANGE), (dict(n_lists=1025), RANGE),
     (dict(budget=0, first=0, recent=0), RANGE), (dict(budget=(1 << 30) + 1, list_stride=1 << 31), RANGE), (dict(recent=97), RANGE), (dict(first=0xFFFFFFFF, recent=1), RANGE),
-    (dict(weights_stride=999), RANGE), (dict(list_stride=99), RANGE), (dict(list_stride=1 << 60), RANGE)])
+    (dict(weights_stride=999), RANGE), (dict(list_stride=99), RANGE), (dict(list_stride=1 << 60), RANGE), (dict(counts=0x4000), INVALID),
+    (dict(counts=0x4004), INVALID), (dict(counts=0x3FFC), INVALID)])
 def test_choose_arguments_that_are_refused(T, change, status):  # noqa: F811
     assert T.lib().tent_kv_choose(make_batch(T), make_choose(T, **change), None) == status
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(lists=None), INVALID), (dict(counts=None), INVALID), (dict(lists=0x1002), INVALID), (dict(to_table=0x9001), INVALID), (dict(kv_len_out=0x4000), INVALID),
+    (dict(kv_len_out=0x4004), INVALID), (dict(kv_len_out=0x2000), INVALID), (dict(counts=0x90000004), INVALID), (dict(kv_len_out=0x5004), INVALID),
     (dict(flags=2), INVALID), (dict(reserved=1), INVALID), (dict(weights=0x5000), INVALID), (dict(weights_out=0x5000), INVALID),
     (dict(weights=0x5000, weights_out=0x5000, n_weights=8, weights_stride=1000, to_table=0x9000, to_stride=64), INVALID), (dict(n_lists=2), RANGE), (dict(n_lists=0), RANGE),
     (dict(most=101), RANGE), (dict(list_stride=1 << 60), RANGE), (dict(weights=0x5000, weights_out=0x6000, n_weights=1, weights_stride=1000), RANGE),
-    (dict(weights=0x5000, weights_out=0x6000, n_weights=4, weights_stride=1000), RANGE), (dict(weights=0x5000, weights_out=0x6000, n_weights=8, weights_stride=999), RANGE)])
+    (dict(weights=0x5000, weights_out=0x6000, n_weights=4, weights_stride=1000), RANGE), (dict(weights=0x5000, weights_out=0x6000, n_weights=8, weights_stride=999), RANGE),
+    (dict(weights=0x5000, weights_out=0x6000, n_weights=8, weights_stride=1000), INVALID)])
 def test_keep_arguments_that_are_refused(T, change, status):  # noqa: F811
     assert T.lib().tent_kv_keep(make_cache(T), make_batch(T), make_keep(T, **change), None) == status
 
@@ -187,6 +190,47 @@ def test_what_rows_of_a_tree_see_on_the_host(tmp_path):
     src = tmp_path / "seen.cpp"
     src.write_text(SEEN)
     exe = tmp_path / "seen"
+    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover", "-I",
+                           os.path.join(ROOT, "paper_2604_00368_amd", "csrc"), "-o", str(exe), str(src)])
+    assert subprocess.check_output([str(exe)]).decode() == "ok\n"
+
+
+MEET = r'''
+#include <assert.h>
+#include <stdio.h>
+#include <stdlib.h>
+#include "kv_pages.h"
+using namespace tent;
+int main()
+{
+    static float pool[400];
+    srand(7);
+    for (int round = 0; round < 50000; ++round) {
+        const int lists = 1 + rand() % 4, width = rand() % 9, stride = width + rand() % 12 + (width == 0);
+        const int a = rand() % 200, b = rand() % 3 ? rand() % 200 : a + (rand() % 5 - 2) * stride;
+        if (b < 0) continue;
+        bool meet = false;                                     // a value of one where one of another place is in the other
+        for (int i = 0; i < lists; ++i) for (int j = 0; j < lists; ++j) for (int x = 0; x < width; ++x) {
+            const int y = a + i * stride + x - b - j * stride;
+            meet |= y >= 0 && y < width && a != b;
+        }
+        assert(kv_lists_meet(pool + a, pool + b, lists, width, stride) == meet);
+        const int x_bytes = rand() % 40, y_bytes = rand() % 40;
+        const char *x = (const char*)pool + a, *y = (const char*)pool + b;
+        meet = x_bytes && y_bytes && x < y + y_bytes && y < x + x_bytes;
+        if (x_bytes && y_bytes) assert(kv_meet(x, x_bytes, y, y_bytes) == meet);
+    }
+    assert(!kv_lists_meet(nullptr, pool, 2, 2, 2) && !kv_meet(nullptr, 4, pool, 4));
+    printf("ok\n");
+    return 0;
+}
+'''
+
+
+def test_memory_that_two_arguments_share_is_found_on_the_host(tmp_path):
+    src = tmp_path / "meet.cpp"
+    src.write_text(MEET)
+    exe = tmp_path / "meet"
     subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover", "-I",
                            os.path.join(ROOT, "paper_2604_00368_amd", "csrc"), "-o", str(exe), str(src)])
     assert subprocess.check_output([str(exe)]).decode() == "ok\n"
