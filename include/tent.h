@@ -650,6 +650,7 @@ int tent_kv_attend(const tent_kv_cache *cache, const tent_kv_batch *batch, const
  */
 enum { TENT_KV_KEEP_ROWS = 1u << 0 };                       /* tent_kv_keep_args.flags: lists name rows, not tokens   */
 enum { TENT_KV_MAX_VOCAB = 1 << 20 };
+enum { TENT_KV_CHOOSE_WHOLE = 16384 };                      /* tent_kv_choose takes no workspace where max_kv is no more */
 
 typedef struct {
     const uint64_t *masks;     /* device [n_rows][mask_stride]: bit j of a row's words: it sees row j of its sequence */
@@ -696,6 +697,8 @@ typedef struct {
     int32_t *lists;            /* device [n_seqs][n_lists][list_stride]: tokens, ascending, then -1 up to budget */
     int32_t *counts;           /* device [n_seqs]: how many of them; not the batch's kv_len         */
     uint64_t weights_stride, list_stride;   /* values, at least max_kv, and at least budget        */
+    void *workspace;           /* device: tent_kv_choose_workspace bytes; NULL where that is 0      */
+    uint64_t workspace_bytes;
     uint32_t n_lists;          /* 1 .. TENT_KV_MAX_HEADS                                           */
     uint32_t budget;           /* tokens to keep, 1 .. 2^30                                        */
     uint32_t first, recent;    /* that many first and last tokens are kept whatever their weights: budget at most */
@@ -748,6 +751,7 @@ int tent_kv_weigh_workspace(const tent_kv_cache *cache, const tent_kv_batch *bat
  * of the others those with the greatest weights, of equal ones the first (NaN counts as minus infinity).  Takes n_seqs, kv_len and max_kv
  * of the batch, no pages.  A sequence that is left out gets count 0. */
 int tent_kv_choose(const tent_kv_batch *batch, const tent_kv_choose_args *args, void *stream);
+int tent_kv_choose_workspace(const tent_kv_batch *batch, const tent_kv_choose_args *args, uint64_t *bytes);
 
 /* Token j becomes what token lists[s][l][j] was, for j < counts[s] and head l (with one list every head): K, V, and `weights` if
  * given, whose places behind the last kept token up to max_kv become 0.  kv_len_out is counts[s].  With TENT_KV_KEEP_ROWS lists name rows:

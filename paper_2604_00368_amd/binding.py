@@ -30,7 +30,8 @@ EXPORTS = ["tent_create", "tent_destroy", "tent_register_segment", "tent_declare
            "tent_sim_fail", "tent_get_retries", "tent_monitor_init", "tent_monitor_update",
            "tent_plan_dispatch", "tent_get_modes", "tent_execute_bounded", "tent_probe_copy", "tent_declare_static",
            "tent_kv_packed_page", "tent_kv_append", "tent_kv_pack", "tent_kv_read", "tent_kv_attend_workspace", "tent_kv_attend",
-           "tent_kv_attend_tree_workspace", "tent_kv_attend_tree", "tent_kv_verify_workspace", "tent_kv_verify", "tent_kv_weigh_workspace", "tent_kv_weigh", "tent_kv_choose", "tent_kv_keep"]
+           "tent_kv_attend_tree_workspace", "tent_kv_attend_tree", "tent_kv_verify_workspace", "tent_kv_verify", "tent_kv_weigh_workspace", "tent_kv_weigh", "tent_kv_choose_workspace",
+           "tent_kv_choose", "tent_kv_keep"]
 
 
 class tent_config(C.Structure):
@@ -63,6 +64,7 @@ TENT_BF16, TENT_FP16, TENT_FP32 = 0, 1, 2
 TENT_KV_BAD_SEQUENCE, TENT_KV_BAD_PAGE, TENT_KV_BAD_POSITION, TENT_KV_BAD_TOKEN = 1, 2, 4, 8
 TENT_KV_MAX_HEADS, TENT_KV_MAX_PAGE_TOKENS = 1024, 1024
 TENT_KV_MAX_VOCAB = 1 << 20
+TENT_KV_CHOOSE_WHOLE = 16384
 TENT_KV_ROPE_PAIRS, TENT_KV_ATTEND_ALL, TENT_KV_KEEP_ROWS = 1, 1, 1
 
 
@@ -111,7 +113,8 @@ class tent_kv_weigh_args(C.Structure):
 
 class tent_kv_choose_args(C.Structure):
     _fields_ = [("weights", C.c_void_p), ("lists", C.c_void_p), ("counts", C.c_void_p), ("weights_stride", C.c_uint64),
-                ("list_stride", C.c_uint64), ("n_lists", C.c_uint32), ("budget", C.c_uint32), ("first", C.c_uint32), ("recent", C.c_uint32)]
+                ("list_stride", C.c_uint64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("n_lists", C.c_uint32), ("budget", C.c_uint32),
+                ("first", C.c_uint32), ("recent", C.c_uint32)]
 
 
 class tent_kv_keep_args(C.Structure):
@@ -186,6 +189,7 @@ def lib():
         L.tent_kv_verify.argtypes = [batch, C.POINTER(tent_kv_verify_args), C.c_void_p]
         L.tent_kv_weigh_workspace.argtypes = [cache, batch, C.POINTER(tent_kv_weigh_args), C.POINTER(C.c_uint64)]
         L.tent_kv_weigh.argtypes = [cache, batch, C.POINTER(tent_kv_weigh_args), C.c_void_p]
+        L.tent_kv_choose_workspace.argtypes = [batch, C.POINTER(tent_kv_choose_args), C.POINTER(C.c_uint64)]
         L.tent_kv_choose.argtypes = [batch, C.POINTER(tent_kv_choose_args), C.c_void_p]
         L.tent_kv_keep.argtypes = [cache, batch, C.POINTER(tent_kv_keep_args), C.c_void_p]
         _lib = L
@@ -455,6 +459,12 @@ def tent_kv_weigh_workspace(cache: tent_kv_cache, batch: tent_kv_batch, args: te
 
 def tent_kv_weigh(cache: tent_kv_cache, batch: tent_kv_batch, args: tent_kv_weigh_args, stream=None):
     _check(lib().tent_kv_weigh(cache, batch, args, _stream(stream)), "tent_kv_weigh")
+
+
+def tent_kv_choose_workspace(batch: tent_kv_batch, args: tent_kv_choose_args) -> int:
+    n = C.c_uint64()
+    _check(lib().tent_kv_choose_workspace(batch, args, n), "tent_kv_choose_workspace")
+    return n.value
 
 
 def tent_kv_choose(batch: tent_kv_batch, args: tent_kv_choose_args, stream=None):

@@ -10,14 +10,21 @@ namespace {
 // A workgroup for each list.  The weight that the last chosen token has is found digit by digit: a histogram of the digits of those
 // weights whose higher digits are the wanted ones, then the digit at which as many lie above as are wanted.  Where up to 128 weights have
 // that digit they are put side by side and the one is found among them by its rank, most often after the second digit.  Up to 16,384 tokens
-// are held in registers for all of it; more are read again for each digit.
+// are held in registers for all of it; more are read again for each digit, or, where lists are few, shared by several workgroups
+// (choose_part_kernel).
 //
-// Barriers and latencies bound it.  Measured: one list of 6,000 tokens 12.4 us (with four digits of 8 bits and no ranks 15.5), 256 lists of
-// 1,000 to 16,384 tokens, four fifths of whose weights are zero, 25 us (22.6).
+// Barriers and latencies bound it.  Measured: one list of 6,000 tokens 13.0 us, 256 lists of 1,000 to 16,384 tokens, four fifths of whose
+// weights are zero, 26 us (with four digits of 8 bits and no ranks 15.5 and 22.6); one list of 131,072 tokens 43 us, by one workgroup 182.
 struct ChooseArgs {
     tent_kv_choose_args a;
     tent_kv_batch b;
     uint32_t first;                    // of the launch's workgroups
+};
+struct ChoosePartArgs : ChooseArgs {
+    uint32_t* counts;                  // [2][lists][parts][kDigits]: of the digits of two launches, in turn
+    uint32_t* before;                  // [lists][parts]: weights above the digits found that lie in the parts before
+    u32x2* found;                      // [2][lists]: the digits found, and how many weights are wanted of those that have them; in turn, too
+    uint32_t parts, part_tokens;       // workgroups to a list, and their tokens: a multiple of kHeldTokens
 };
 constexpr uint32_t kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
 constexpr uint32_t kHeld = 16, kHeldTokens = kHeld * kChooseThreads;     // tokens of a thread, and of the workgroup
@@ -42,13 +49,119 @@ __device__ __forceinline__ void each_held(uint32_t n, F f)
         if (i * kChooseThreads < n) f(i);                                // the whole workgroup
 }
 
+// The keys of kHeldTokens tokens from t0 on, of which `n` less t0 are there.
+__device__ __forceinline__ void hold_keys(uint32_t (&key)[kHeld], const float* w, uint32_t t0, uint32_t n)
+{
+    float x[kHeld];
+    each_held(n - t0, [&](uint32_t i) {
+        const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
+        x[i] = t < n ? dev_load<float>(w + t) : 0.f;
+    });
+    each_held(n - t0, [&](uint32_t i) { key[i] = weight_key(x[i]); });
+}
+
+__device__ __forceinline__ void clear_counts(uint32_t* count)
+{
+#pragma unroll
+    for (uint32_t i = 0; i < kDigits * kCopies / 4 / kChooseThreads; ++i) *(u32x4*)&count[(i * kChooseThreads + threadIdx.x) * 4] = u32x4{0, 0, 0, 0};
+}
+// Counts a digit; lanes that do not count are not here.
+__device__ __forceinline__ void count_digit(uint32_t* count, uint32_t digit)
+{
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, one = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
+    const uint64_t alike = __ballot(digit == one);
+    if (digit != one) atomicAdd(&count[digit * kCopies + (lane & (kCopies - 1))], 1u);
+    else if (lane == (uint32_t)__builtin_ctzll(alike)) atomicAdd(&count[one * kCopies + (wave & (kCopies - 1))], (uint32_t)__popcll(alike));
+}
+__device__ __forceinline__ uint32_t counted(const uint32_t* count, uint32_t digit)
+{
+    const u32x4 c = *(const u32x4*)&count[digit * kCopies];
+    return c[0] + c[1] + c[2] + c[3];
+}
+// Finds the digit that the weight has which is the wanted one from the largest on, of which there are mine[0] and mine[1] with the thread's two
+// digits, the larger one first; says into digit_lds which, into wanted_lds the how manieth of them, and into all_lds how many there are.
+__device__ __forceinline__ uint32_t first_digit() { return kDigits - 1 - 2 * threadIdx.x; }
+__device__ __forceinline__ void find_digit(const uint32_t (&mine)[2], uint32_t wanted, uint32_t* before_lds, uint32_t& digit_lds, uint32_t& wanted_lds, uint32_t& all_lds)
+{
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, both = mine[0] + mine[1];
+    uint32_t up_to = both;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const uint32_t up = __shfl_up(up_to, m, 64);
+        up_to += lane >= (uint32_t)m ? up : 0u;
+    }
+    if (lane == 63) before_lds[wave] = up_to;
+    __syncthreads();
+    uint32_t before = up_to - both;
+    for (uint32_t i = 0; i < wave; ++i) before += before_lds[i];
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        if (before < wanted && before + mine[i] >= wanted) {
+            digit_lds = first_digit() - i;
+            wanted_lds = wanted - before;
+            all_lds = mine[i];
+        }
+        before += mine[i];
+    }
+    __syncthreads();
+}
+// Puts the tokens that are kept of kHeldTokens from t0 on into the list, in their order: how many there are before each, from counts of every
+// wave's 64.  kind(i, more, same): whether the thread's token i is kept, or at the border, of which the first `equal` are.
+// more_before and equal_before: of the list, in front of t0; then behind.
+template <class Kind>
+__device__ __forceinline__ void put_tokens(int32_t* to, uint32_t t0, uint32_t n, uint32_t equal, uint32_t& more_before, uint32_t& equal_before,
+                                           uint32_t* before_lds, uint32_t& all_lds, Kind kind)
+{
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    each_held(n - t0, [&](uint32_t i) {
+        bool more, same;
+        kind(i, more, same);
+        const uint32_t both = (uint32_t)__popcll(__ballot(more)) | (uint32_t)__popcll(__ballot(same)) << 16;    // at most 16,384 each
+        if (lane == 0) before_lds[i * kChooseWaves + wave] = both;
+    });
+    __syncthreads();
+    if (wave == 0) {
+        uint32_t mine[4], sum = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t at = lane * 4 + i;
+            sum += mine[i] = t0 + at / kChooseWaves * kChooseThreads < n ? before_lds[at] : 0u;
+        }
+        uint32_t up_to = sum;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const uint32_t up = __shfl_up(up_to, m, 64);
+            up_to += lane >= (uint32_t)m ? up : 0u;
+        }
+        if (lane == 63) all_lds = up_to;
+        up_to -= sum;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            before_lds[lane * 4 + i] = up_to;
+            up_to += mine[i];
+        }
+    }
+    __syncthreads();
+    each_held(n - t0, [&](uint32_t i) {
+        bool more, same;
+        kind(i, more, same);
+        const uint64_t below = (1ull << lane) - 1, more_mask = __ballot(more), same_mask = __ballot(same);
+        const uint32_t both = before_lds[i * kChooseWaves + wave];
+        const uint32_t at = more_before + (both & 0xFFFFu) + (uint32_t)__popcll(more_mask & below);
+        const uint32_t eq = equal_before + (both >> 16) + (uint32_t)__popcll(same_mask & below);
+        if (more || (same && eq < equal)) to[at + (eq < equal ? eq : equal)] = (int32_t)(t0 + i * kChooseThreads + threadIdx.x);
+    });
+    more_before += all_lds & 0xFFFFu;
+    equal_before += all_lds >> 16;
+    __syncthreads();
+}
+
 __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs g)
 {
     __shared__ __align__(16) uint32_t count[kDigits * kCopies];
     __shared__ uint32_t before_lds[kHeld * kChooseWaves], digit_lds, wanted_lds, there_lds, all_lds;
     const tent_kv_choose_args& a = g.a;
     const uint32_t block = g.first + blockIdx.x, seq = block / a.n_lists, list = block - seq * a.n_lists;
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const KvSeq q = kv_sequence(g.b, seq);
     if (q.bad && threadIdx.x == 0 && list == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
     const uint32_t n = (uint32_t)q.len, kept = n < a.budget ? n : a.budget;      // 0 of a bad sequence
@@ -63,14 +176,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs
     const uint32_t lo = a.first, hi = n - a.recent;                      // the tokens that weights decide on: more than are wanted of them
     const bool once = n <= kHeldTokens;
     uint32_t key[kHeld];
-    auto hold = [&](uint32_t t0) {                                       // the keys of kHeldTokens tokens from t0 on
-        float x[kHeld];
-        each_held(n - t0, [&](uint32_t i) {
-            const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
-            x[i] = t < n ? dev_load<float>(w + t) : 0.f;
-        });
-        each_held(n - t0, [&](uint32_t i) { key[i] = weight_key(x[i]); });
-    };
+    auto hold = [&](uint32_t t0) { hold_keys(key, w, t0, n); };
     auto decided = [&](uint32_t t) -> bool { return t >= lo && t < hi; };
     if (once) hold(0);
     // Keys above `border` are kept, and the first `equal` of those at it; whatever is not decided on is.
@@ -79,48 +185,19 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs
         uint32_t above = 0;                                              // the digits found, at their places
         for (int shift = 21, bits = 11; ; bits = shift >= 10 ? 11 : 10, shift = shift >= 21 ? 10 : 0) {
             const uint32_t digits = 1u << bits;
-#pragma unroll
-            for (uint32_t i = 0; i < kDigits * kCopies / 4 / kChooseThreads; ++i) *(u32x4*)&count[(i * kChooseThreads + threadIdx.x) * 4] = u32x4{0, 0, 0, 0};
+            clear_counts(count);
             __syncthreads();
             for (uint32_t t0 = 0; t0 < n; t0 += kHeldTokens) {
                 if (!once) hold(t0);
                 each_held(n - t0, [&](uint32_t i) {
-                    if (decided(t0 + i * kChooseThreads + threadIdx.x) && (shift == 21 || key[i] >> (shift + bits) == above >> (shift + bits))) {
-                        const uint32_t digit = key[i] >> shift & (digits - 1), one = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
-                        const uint64_t alike = __ballot(digit == one);
-                        if (digit != one) atomicAdd(&count[digit * kCopies + (lane & (kCopies - 1))], 1u);
-                        else if (lane == (uint32_t)__builtin_ctzll(alike)) atomicAdd(&count[one * kCopies + (wave & (kCopies - 1))], (uint32_t)__popcll(alike));
-                    }
+                    if (decided(t0 + i * kChooseThreads + threadIdx.x) && (shift == 21 || key[i] >> (shift + bits) == above >> (shift + bits)))
+                        count_digit(count, key[i] >> shift & (digits - 1));
                 });
             }
             __syncthreads();
-            uint32_t mine[2], up_to = 0;                                 // two digits a thread, the largest in the first
-#pragma unroll
-            for (uint32_t i = 0; i < 2; ++i) {
-                const u32x4 c = *(const u32x4*)&count[(kDigits - 1 - 2 * threadIdx.x - i) * kCopies];
-                up_to += mine[i] = c[0] + c[1] + c[2] + c[3];
-            }
-            const uint32_t both = up_to;
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const uint32_t up = __shfl_up(up_to, m, 64);
-                up_to += lane >= (uint32_t)m ? up : 0u;
-            }
-            if (lane == 63) before_lds[wave] = up_to;
             if (threadIdx.x == 0) there_lds = 0;
-            __syncthreads();
-            uint32_t before = up_to - both;
-            for (uint32_t i = 0; i < wave; ++i) before += before_lds[i];
-#pragma unroll
-            for (uint32_t i = 0; i < 2; ++i) {
-                if (before < wanted && before + mine[i] >= wanted) {
-                    digit_lds = kDigits - 1 - 2 * threadIdx.x - i;
-                    wanted_lds = wanted - before;
-                    all_lds = mine[i];
-                }
-                before += mine[i];
-            }
-            __syncthreads();
+            const uint32_t mine[2] = {counted(count, first_digit()), counted(count, first_digit() - 1)};
+            find_digit(mine, wanted, before_lds, digit_lds, wanted_lds, all_lds);
             above |= digit_lds << shift;
             wanted = wanted_lds;
             const uint32_t there = all_lds;
@@ -158,56 +235,112 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs
         border = above;
         equal = wanted;                                                  // of those at the border the first so many
     }
-    // Tokens in their order: how many are kept before each, from counts of every wave's 64.
     uint32_t more_before = 0, equal_before = 0;
     for (uint32_t t0 = 0; t0 < n; t0 += kHeldTokens) {
         if (!once) hold(t0);
-        auto kind = [&](uint32_t i, bool& more, bool& same) {
+        put_tokens(to, t0, n, equal, more_before, equal_before, before_lds, all_lds, [&](uint32_t i, bool& more, bool& same) {
             const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
             more = t < n && (!decided(t) || (equal && key[i] > border));
             same = t < n && decided(t) && equal && key[i] == border;
-        };
-        each_held(n - t0, [&](uint32_t i) {
-            bool more, same;
-            kind(i, more, same);
-            const uint32_t both = (uint32_t)__popcll(__ballot(more)) | (uint32_t)__popcll(__ballot(same)) << 16;    // at most 16,384 each
-            if (lane == 0) before_lds[i * kChooseWaves + wave] = both;
         });
+    }
+}
+
+// Several workgroups to a list, each with tokens of its own, in four launches: kStage 0 to 2 count the digits of 11, 11 and 10 bits, each of
+// the weights that have the digits found before, and 3 puts the tokens into the list.  Every workgroup finds the digit of the launch before
+// it by itself, from all workgroups' counts of its list, and how many weights above it lie in front of its own tokens.
+template <int kStage>
+__global__ void __launch_bounds__(kChooseThreads) choose_part_kernel(const ChoosePartArgs g)
+{
+    __shared__ __align__(16) uint32_t count[kDigits * kCopies];
+    __shared__ uint32_t before_lds[kHeld * kChooseWaves], digit_lds, wanted_lds, all_lds, above_lds[kChooseWaves], same_lds;
+    constexpr int kShift = kStage == 0 ? 21 : kStage == 1 ? 10 : 0, kBefore = kStage == 1 ? 21 : kStage == 2 ? 10 : 0;      // of this stage's digit; of the last one's
+    const tent_kv_choose_args& a = g.a;
+    const uint32_t block = g.first + blockIdx.x, at = block / g.parts, part = block - at * g.parts, seq = at / a.n_lists, list = at - seq * a.n_lists;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const KvSeq q = kv_sequence(g.b, seq);
+    const uint32_t n = (uint32_t)q.len, kept = n < a.budget ? n : a.budget;      // 0 of a bad sequence
+    const uint32_t t_first = part * g.part_tokens, t_end = n - t_first < g.part_tokens ? n : t_first + g.part_tokens;     // where t_first < n
+    int32_t* const to = a.lists + (uint64_t)at * a.list_stride;
+    if constexpr (kStage == 3) {
+        if (q.bad && threadIdx.x == 0 && list == 0 && part == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
+        if (threadIdx.x == 0 && list == 0 && part == 0) a.counts[seq] = (int32_t)kept;
+        for (uint64_t j = kept + part * kChooseThreads + threadIdx.x; j < a.budget; j += (uint64_t)g.parts * kChooseThreads) to[j] = -1;
+        if (n <= a.budget) {
+            for (uint64_t j = part * kChooseThreads + threadIdx.x; j < n; j += (uint64_t)g.parts * kChooseThreads) to[j] = (int32_t)j;
+            return;
+        }
+    }
+    uint32_t wanted = a.budget - a.first - a.recent;
+    if (t_first >= n || n <= a.budget || (kStage < 3 && !wanted)) return;
+    const float* const w = a.weights + (uint64_t)at * a.weights_stride;
+    const uint32_t lo = a.first, hi = n - a.recent;
+    auto decided = [&](uint32_t t) -> bool { return t >= lo && t < hi; };
+    uint32_t key[kHeld];
+    hold_keys(key, w, t_first, t_end);                                   // beside the counts
+    const uint64_t lists = (uint64_t)g.b.n_seqs * a.n_lists, half = lists * g.parts * kDigits;
+    uint32_t above = 0, more_before = 0, equal_before = 0;
+    if (kStage > 0 && wanted) {
+        const uint32_t* const counts = g.counts + (kStage & 1 ? 0 : half) + (uint64_t)at * g.parts * kDigits;
+        const uint32_t used = (n - 1) / g.part_tokens + 1;
+        uint32_t mine[2] = {0, 0}, in_front[2] = {0, 0};                 // of the thread's two digits: all, and those of the parts before
+        for (uint32_t p = 0; p < used; ++p) {
+            const u32x2 c = *(const u32x2*)(counts + (uint64_t)p * kDigits + first_digit() - 1);
+            mine[0] += c[1];
+            mine[1] += c[0];
+            in_front[0] += p < part ? c[1] : 0u;
+            in_front[1] += p < part ? c[0] : 0u;
+        }
+        if (kStage > 1) {
+            const u32x2 found = g.found[(kStage & 1 ? 0 : lists) + at];
+            above = found[0];
+            wanted = found[1];
+            more_before = g.before[(uint64_t)at * g.parts + part];
+        }
+        find_digit(mine, wanted, before_lds, digit_lds, wanted_lds, all_lds);
+        const uint32_t digit = digit_lds;
+        uint32_t sum = (first_digit() > digit ? in_front[0] : 0u) + (first_digit() - 1 > digit ? in_front[1] : 0u);
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m, 64);
+        if (lane == 0) above_lds[wave] = sum;
+        if (first_digit() == digit) same_lds = in_front[0];
+        if (first_digit() - 1 == digit) same_lds = in_front[1];
         __syncthreads();
-        if (wave == 0) {
-            uint32_t mine[4], sum = 0;
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-                const uint32_t at = lane * 4 + i;
-                sum += mine[i] = t0 + at / kChooseWaves * kChooseThreads < n ? before_lds[at] : 0u;
-            }
-            uint32_t up_to = sum;
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const uint32_t up = __shfl_up(up_to, m, 64);
-                up_to += lane >= (uint32_t)m ? up : 0u;
-            }
-            if (lane == 63) all_lds = up_to;
-            up_to -= sum;
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-                before_lds[lane * 4 + i] = up_to;
-                up_to += mine[i];
-            }
+        for (uint32_t i = 0; i < kChooseWaves; ++i) more_before += above_lds[i];
+        equal_before = same_lds;                                         // at the border itself after the last digit
+        above |= digit << kBefore;
+        wanted = wanted_lds;
+    }
+    if constexpr (kStage < 3) {
+        if (kStage > 0 && threadIdx.x == 0) {
+            g.before[(uint64_t)at * g.parts + part] = more_before;
+            if (part == 0) g.found[(kStage & 1 ? lists : 0) + at] = u32x2{above, wanted};
+        }
+        clear_counts(count);
+        __syncthreads();
+        for (uint32_t t0 = t_first; t0 < t_end; t0 += kHeldTokens) {
+            if (t0 != t_first) hold_keys(key, w, t0, t_end);
+            each_held(t_end - t0, [&](uint32_t i) {
+                const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
+                if (t < t_end && decided(t) && (kStage == 0 || key[i] >> kBefore == above >> kBefore))
+                    count_digit(count, key[i] >> kShift & (kStage == 2 ? kDigits / 2 - 1 : kDigits - 1));
+            });
         }
         __syncthreads();
-        each_held(n - t0, [&](uint32_t i) {
-            bool more, same;
-            kind(i, more, same);
-            const uint64_t below = (1ull << lane) - 1, more_mask = __ballot(more), same_mask = __ballot(same);
-            const uint32_t both = before_lds[i * kChooseWaves + wave];
-            const uint32_t at = more_before + (both & 0xFFFFu) + (uint32_t)__popcll(more_mask & below);
-            const uint32_t eq = equal_before + (both >> 16) + (uint32_t)__popcll(same_mask & below);
-            if (more || (same && eq < equal)) to[at + (eq < equal ? eq : equal)] = (int32_t)(t0 + i * kChooseThreads + threadIdx.x);
-        });
-        more_before += all_lds & 0xFFFFu;
-        equal_before += all_lds >> 16;
-        __syncthreads();
+        uint32_t* const counts = g.counts + (kStage & 1 ? half : 0) + ((uint64_t)at * g.parts + part) * kDigits;
+        *(u32x2*)(counts + first_digit() - 1) = u32x2{counted(count, first_digit() - 1), counted(count, first_digit())};
+    } else {
+        const uint32_t border = wanted ? above : 0xFFFFFFFFu, equal = wanted;
+        more_before += (t_first < lo ? t_first : lo) + (t_first > hi ? t_first - hi : 0u);      // tokens in front that are not decided on
+        for (uint32_t t0 = t_first; t0 < t_end; t0 += kHeldTokens) {
+            if (t0 != t_first) hold_keys(key, w, t0, t_end);
+            put_tokens(to, t0, t_end, equal, more_before, equal_before, before_lds, all_lds, [&](uint32_t i, bool& more, bool& same) {
+                const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
+                more = t < t_end && (!decided(t) || (equal && key[i] > border));
+                same = t < t_end && decided(t) && equal && key[i] == border;
+            });
+        }
     }
 }
 
@@ -442,6 +575,36 @@ __global__ void __launch_bounds__(256) keep_weights_kernel(const KeepArgs g)
     for (int32_t t = base + count + (int32_t)threadIdx.x; t < most; t += 256) to[t] = 0.f;
 }
 
+// Whether several workgroups share a list, and how many: each finds the digits from the counts of all of them, so there are not many.
+// Quarters of lists, with a workgroup to a list, to 16,384 and to 8,192 tokens: 1 list of 17,000 tokens 33, 31 and 29 us, 32,768 50, 39 and
+// 32, 131,072 182, 45 and 43; 64 lists 34, 34 and 33, 51, 43 and 38, 185, 77 and 110; 128 lists 34, 36 and 46, 52, 46 and 49, 190, 140 and 204;
+// 256 lists of 65,536 105, 129 and 188, as they fill the card by themselves.
+struct ChooseShape { uint32_t parts, part_tokens; uint64_t workspace; };
+constexpr uint32_t kMostParts = 64, kMostSplit = 128;
+static_assert(kHeldTokens == TENT_KV_CHOOSE_WHOLE, "lists of up to that many tokens take no workspace");
+ChooseShape choose_shape(const tent_kv_batch& b, const tent_kv_choose_args& a)
+{
+    ChooseShape s{1, kHeldTokens, 0};
+    const uint64_t lists = (uint64_t)b.n_seqs * a.n_lists;
+    if (b.max_kv <= kHeldTokens || lists > kMostSplit) return s;
+    const uint32_t halves = (b.max_kv + kHeldTokens / 2 - 1) / (kHeldTokens / 2);
+    uint32_t parts = lists * halves <= kMostSplit ? halves : (halves + 1) / 2;
+    if (parts > kMostParts) parts = kMostParts;
+    const uint32_t step = b.max_kv > kMostParts * kHeldTokens ? kHeldTokens : kChooseThreads;      // whole rounds of a workgroup
+    s.part_tokens = ((b.max_kv + parts - 1) / parts + step - 1) / step * step;
+    s.parts = (b.max_kv + s.part_tokens - 1) / s.part_tokens;
+    s.workspace = lists * (s.parts * (2 * kDigits + 1) * 4ull + 2 * sizeof(u32x2));
+    return s;
+}
+template <int kStage>
+int launch_part(ChoosePartArgs g, hipStream_t stream)
+{
+    return launch_blocks((uint64_t)g.b.n_seqs * g.a.n_lists * g.parts, [&](uint32_t first, uint32_t blocks) {
+        g.first = first;
+        hipLaunchKernelGGL((choose_part_kernel<kStage>), dim3(blocks), dim3(kChooseThreads), 0, stream, g);
+    }, kMostBlocks / 4);
+}
+
 template <int D, int kBits>
 int launch_keep(KeepArgs g, hipStream_t s)
 {
@@ -466,6 +629,16 @@ int launch_keep(KeepArgs g, hipStream_t s)
 
 using namespace tent;
 
+extern "C" int tent_kv_choose_workspace(const tent_kv_batch* batch, const tent_kv_choose_args* args, uint64_t* bytes)
+{
+    const int rc = kv_check_sequences(batch);
+    if (rc != TENT_OK) return rc;
+    if (!args || !bytes) return TENT_ERR_INVALID;
+    if (args->n_lists < 1 || args->n_lists > TENT_KV_MAX_HEADS) return TENT_ERR_RANGE;
+    *bytes = batch->n_seqs == 0 ? 0 : choose_shape(*batch, *args).workspace;
+    return TENT_OK;
+}
+
 extern "C" int tent_kv_choose(const tent_kv_batch* batch, const tent_kv_choose_args* args, void* stream)
 {
     const int rc = kv_check_sequences(batch);
@@ -479,8 +652,20 @@ extern "C" int tent_kv_choose(const tent_kv_batch* batch, const tent_kv_choose_a
     if (kv_meet(args->counts, batch->n_seqs * 4ull, batch->kv_len, batch->n_seqs * 4ull)) return TENT_ERR_INVALID;     // read by workgroups of every list
     const uint64_t lists = (uint64_t)batch->n_seqs * args->n_lists, most = ((uint64_t)1 << 60) / lists;
     if (args->weights_stride < batch->max_kv || args->weights_stride > most || args->list_stride < args->budget || args->list_stride > most) return TENT_ERR_RANGE;
-    ChooseArgs g{*args, *batch, 0};
+    const ChooseShape shape = choose_shape(*batch, *args);
+    if (shape.workspace && (!args->workspace || !kv_aligned(args->workspace))) return TENT_ERR_INVALID;
+    if (shape.workspace > args->workspace_bytes) return TENT_ERR_RANGE;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (shape.parts > 1) {
+        uint32_t* const counts = static_cast<uint32_t*>(args->workspace);
+        u32x2* const found = reinterpret_cast<u32x2*>(counts + 2 * lists * shape.parts * kDigits);
+        const ChoosePartArgs g{{*args, *batch, 0}, counts, reinterpret_cast<uint32_t*>(found + 2 * lists), found, shape.parts, shape.part_tokens};
+        int status = launch_part<0>(g, s);
+        if (status == TENT_OK) status = launch_part<1>(g, s);
+        if (status == TENT_OK) status = launch_part<2>(g, s);
+        return status == TENT_OK ? launch_part<3>(g, s) : status;
+    }
+    ChooseArgs g{*args, *batch, 0};
     return launch_blocks(lists, [&](uint32_t first, uint32_t blocks) {
         g.first = first;
         hipLaunchKernelGGL(choose_kernel, dim3(blocks), dim3(kChooseThreads), 0, s, g);

@@ -499,21 +499,38 @@ def weigh_workspace(cache: Cache, batch: Batch, q_heads: int, per_head: bool = T
     return T.tent_kv_weigh_workspace(cache.c, batch.c, T.tent_kv_weigh_args(q_heads=q_heads, n_lists=cache.kv_heads if per_head else 1, scale=1.0))
 
 
-def choose(batch: Batch, weights, budget: int, first: int = 0, recent: int = 0, stream=None):
+def choose(batch: Batch, weights, budget: int, first: int = 0, recent: int = 0, workspace=None, stream=None):
     """Which tokens every sequence of the batch keeps: lists [sequences, (heads,) budget] (int32, ascending, then -1) and counts [sequences].
     All where there are no more than `budget`; else the `first` first, the `recent` last and those of the greatest weights.
-    weights: float32 [sequences, (heads,) max_kv or more], as weigh makes them."""
+    weights: float32 [sequences, (heads,) max_kv or more], as weigh makes them.  workspace: a contiguous uint8 tensor of at least
+    choose_workspace bytes to use instead of a new one."""
     if stream is not None or batch.device.index != _current_device():
-        return _on(batch.device, stream, (*batch.tensors, weights), lambda: choose(batch, weights, budget, first, recent))
+        used = (*batch.tensors, weights) if workspace is None else (*batch.tensors, weights, workspace)
+        return _on(batch.device, stream, used, lambda: choose(batch, weights, budget, first, recent, workspace))
     n_seqs, device = batch.c.n_seqs, batch.device
     lists, apart = _by_list(weights, "weights", torch.float32, n_seqs, batch.max_kv, device)
     if not 1 <= budget <= 1 << 30 or first < 0 or recent < 0 or first + recent > budget:
         raise ValueError("budget must be 1 or more, and hold the first and the recent tokens")
     out = torch.empty((*weights.shape[:-1], budget), dtype=torch.int32, device=device)
     counts = torch.empty((n_seqs,), dtype=torch.int32, device=device)
-    a = T.tent_kv_choose_args(weights.data_ptr(), out.data_ptr(), counts.data_ptr(), apart, budget, lists, budget, first, recent)
-    _check(T.lib().tent_kv_choose(batch.ref, C.byref(a), _stream(device.index)), "tent_kv_choose")
+    a = T.tent_kv_choose_args(weights.data_ptr(), out.data_ptr(), counts.data_ptr(), apart, budget, None, 0, lists, budget, first, recent)
+    L, ref = T.lib(), C.byref(a)
+    if batch.max_kv > T.TENT_KV_CHOOSE_WHOLE:                            # up to there none is needed
+        need = C.c_uint64()
+        _check(L.tent_kv_choose_workspace(batch.ref, ref, C.byref(need)), "tent_kv_choose_workspace")
+        if need.value:
+            if workspace is None:
+                workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+            elif not _on_gpu(workspace, "workspace", torch.uint8).is_contiguous() or workspace.device != device:
+                raise ValueError("workspace must be contiguous, on the batch's device")
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(L.tent_kv_choose(batch.ref, ref, _stream(device.index)), "tent_kv_choose")
     return out, counts
+
+
+def choose_workspace(batch: Batch, lists: int = 1) -> int:
+    """Bytes of workspace that choose takes for such a batch and so many lists of each sequence."""
+    return T.tent_kv_choose_workspace(batch.c, T.tent_kv_choose_args(n_lists=lists))
 
 
 def keep(cache: Cache, batch: Batch, lists, counts, rows: bool = False, to_table=None, weights=None, weights_out=None, kv_len_out=None, stream=None):

@@ -198,6 +198,33 @@ def test_choose_weights_that_are_negative_infinite_or_nan(kv):
         check_choice(kv, w, [2200, 2100, 2000], budget, min(3, budget), 0)
 
 
+@pytest.mark.parametrize("tokens", [[16385, 100, 70001, 32768, 0], [49152, 49153], [1050001]])
+@pytest.mark.parametrize("kind", ["any", "equal", "few", "odd"])
+def test_choose_from_long_lists(kv, tokens, kind):
+    """Several workgroups to a list: borders at the ends of their tokens, equal weights on both sides, a workgroup that is behind the last token."""
+    g = torch.Generator().manual_seed(len(tokens))
+    n = max(tokens)
+    shape = (len(tokens), 2, n) if n < 100000 else (1, n)
+    w = torch.zeros(shape) if kind == "equal" else torch.randint(0, 5, shape, generator=g).float() if kind == "few" else torch.randn(shape, generator=g)
+    if kind == "odd":
+        w[..., 3::5] = math.nan
+        w[..., 4::9] = math.inf
+        w[..., 5::9] = -math.inf
+    for budget, first, recent in ((1, 0, 0), (3, 1, 2), (4096, 0, 0), (20000, 16390, 5), (33000, 4, 16390), (n - 1, 2, 3), (40, 30, 10)):
+        check_choice(kv, w, tokens, budget, first, recent, spare=budget % 2)
+
+
+def test_choose_takes_a_workspace_of_any_contents(kv):
+    batch, w = a_batch(kv, [40000, 20000]), torch.randn(2, 3, 40000, generator=torch.Generator().manual_seed(9)).cuda()
+    need = kv.choose_workspace(batch, 3)
+    assert need > 0 and kv.choose_workspace(a_batch(kv, [16384]), 3) == 0
+    want = kv.choose(batch, w, 5000, 4, 100)
+    for byte in (0, 1, 255):
+        work = torch.full((need + 64,), byte, dtype=torch.uint8, device="cuda")
+        got = kv.choose(batch, w, 5000, 4, 100, workspace=work[:need])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool((work[need:] == byte).all())
+
+
 def test_choose_sequences_that_are_left_out(kv):
     batch = a_batch(kv, [50, 60, 70], most=65)
     w = torch.rand(3, 65, generator=torch.Generator().manual_seed(4))

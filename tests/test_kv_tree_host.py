@@ -138,7 +138,7 @@ def test_structures_are_laid_out_as_in_the_header(T, tmp_path):  # noqa: F811
         lines.append(f'printf("{n} %zu", sizeof({n}));')
         lines += [f'printf(" %zu", offsetof({n}, {f}));' for f, _ in getattr(T, n)._fields_]
         lines.append('printf("\\n");')
-    consts = ["TENT_FP32", "TENT_KV_BAD_TOKEN", "TENT_KV_MAX_VOCAB", "TENT_KV_KEEP_ROWS"]
+    consts = ["TENT_FP32", "TENT_KV_BAD_TOKEN", "TENT_KV_MAX_VOCAB", "TENT_KV_KEEP_ROWS", "TENT_KV_CHOOSE_WHOLE"]
     lines.append('printf("consts' + " %d" * len(consts) + '\\n", ' + ", ".join(f"(int){c}" for c in consts) + ");")
     src = tmp_path / "layout.c"
     src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "tent.h"\nint main(void) {\n' + "\n".join(lines) + "\nreturn 0; }\n")
@@ -280,6 +280,19 @@ def scenario_enqueued():
         same(names(lambda: L.tent_kv_choose(batch, make_choose(T), stream)), ["choose"])
         same(names(lambda: L.tent_kv_keep(make_cache(T), batch, make_keep(T), stream)), ["keep_kernel"])
         same(names(lambda: L.tent_kv_weigh(make_cache(T), batch, make_weigh(T), stream)), ["few"])
+    n, args = C.c_uint64(), make_choose(T, weights_stride=1 << 20, workspace=0x40000, workspace_bytes=1 << 40)
+    for tokens in (16384, 16385, 100000):
+        batch = make_batch(T, max_kv=tokens, table_stride=6400)
+        same(names(lambda: L.tent_kv_choose(batch, args, stream)), ["choose_kernel"] if tokens == 16384 else ["choose_part"] * 4)
+        assert L.tent_kv_choose_workspace(batch, args, n) == 0 and (n.value == 0) == (tokens == 16384)
+    args.workspace_bytes = n.value
+    assert L.tent_kv_choose(batch, args, stream) == 0
+    args.workspace_bytes -= 1
+    assert L.tent_kv_choose(batch, args, stream) == RANGE
+    args.workspace_bytes, args.workspace = n.value, 0x40008
+    assert L.tent_kv_choose(batch, args, stream) == INVALID
+    args.n_lists = 0
+    assert L.tent_kv_choose_workspace(batch, args, n) == RANGE and L.tent_kv_choose_workspace(batch, None, n) == INVALID
     for kind in range(3):
         for change in (dict(), dict(draft=None), dict(parents=None), dict(vocab=100), dict(vocab=1 << 20, target_stride=1 << 20, draft_stride=1 << 20)):
             args, n = make_verify(T, type=kind, path_stride=4000, **change), C.c_uint64()
@@ -332,6 +345,7 @@ def scenario_large_calls():
     long = make_batch(T, n_rows=1, max_rows=1, n_seqs=1, max_kv=1 << 30, table_stride=1 << 30)
     assert small(lambda: L.tent_kv_weigh(tiny, long, make_weigh(T, q_heads=1, q_stride=64, n_lists=1, weights_stride=1 << 30), None)) > 1000
     assert small(lambda: L.tent_kv_verify(every, make_verify(T, vocab=1 << 20, target_stride=1 << 20, draft_stride=1 << 20), None)) == 65535
+    assert small(lambda: L.tent_kv_choose(long, make_choose(T, n_lists=1, weights_stride=1 << 30, workspace=0x40000, workspace_bytes=1 << 40), None)) == 4 * 64
     few = make_batch(T, n_seqs=128, n_rows=1280, max_rows=10)
     assert small(lambda: L.tent_kv_verify(few, make_verify(T, path_stride=10, **LONG), None)) == 128 * (512 // 4 + 1)
 

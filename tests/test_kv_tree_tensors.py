@@ -38,6 +38,10 @@ class Gpus(Base.Gpus):
         self.args = T.tent_kv_weigh_args.from_buffer_copy(args._obj)
         return self.call("weigh", stream)
 
+    def tent_kv_choose_workspace(self, batch, args, need):
+        need._obj.value = 2048
+        return 0
+
     def tent_kv_choose(self, batch, args, stream):
         self.args = T.tent_kv_choose_args.from_buffer_copy(args._obj)
         return self.call("choose", stream)
@@ -127,6 +131,21 @@ def test_tensors_that_are_passed_in_are_not_made_anew(gpus):
         assert ("record", t.data_ptr(), 0x55) in gpus.log and ("record", t.data_ptr(), 0) not in gpus.log
 
 
+def test_choose_from_long_lists_takes_a_workspace(gpus):
+    s = Step(gpus)
+    i32 = dict(dtype=torch.int32)
+    batch = kv.Batch(s.on(torch.zeros(2, 20000, **i32)), s.on(torch.zeros(2, **i32)), s.on(torch.zeros(3, **i32)), 3, 2, 20000)
+    weights, room = s.on(torch.zeros(2, 2, 20000)), s.on(torch.zeros(2100, dtype=torch.uint8))
+    gpus.log.clear()
+    kv.choose(batch, weights, 9, stream=0x55)
+    assert gpus.args.workspace_bytes == 2048 and len([e for e in gpus.log if e[0] == "new"]) == 3
+    kv.choose(batch, weights, 9, workspace=room, stream=0x55)
+    assert (gpus.args.workspace, gpus.args.workspace_bytes) == (room.data_ptr(), 2100) and ("record", room.data_ptr(), 0x55) in gpus.log
+    for wrong in (s.on(torch.zeros(2100, **i32)), s.on(torch.zeros(2, 4096, dtype=torch.uint8)[:, :2100]), torch.zeros(2100, dtype=torch.uint8)):
+        with pytest.raises(ValueError):
+            kv.choose(batch, weights, 9, workspace=wrong)
+
+
 @pytest.mark.parametrize("index", [0, 1])
 def test_calls_go_to_the_device_of_their_tensors(gpus, index):
     s = Step(gpus, index)
@@ -213,7 +232,7 @@ def test_strides_are_handed_on(gpus):
     s.choose(weights=on(torch.zeros(2, 2, 32)), budget=5)
     assert (gpus.args.weights_stride, gpus.args.list_stride, gpus.args.n_lists) == (32, 5, 2)
     s.choose(weights=on(torch.zeros(2, 24)), budget=5)
-    assert (gpus.args.weights_stride, gpus.args.n_lists) == (24, 1)
+    assert (gpus.args.weights_stride, gpus.args.n_lists, gpus.args.workspace) == (24, 1, None)
     s.keep(lists=on(torch.zeros(2, 9, dtype=torch.int32)[:, :4]), to_table=on(torch.zeros(2, 8, dtype=torch.int32)[:, :3]), rows=True)
     assert (gpus.args.list_stride, gpus.args.most, gpus.args.n_lists, gpus.args.to_stride, gpus.args.n_weights, gpus.args.flags) == (9, 4, 1, 8, 2, 1)
     assert gpus.args.weights != gpus.args.weights_out                    # to other pages: not in place
