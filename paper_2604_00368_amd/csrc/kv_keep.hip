@@ -393,6 +393,8 @@ using Scales = std::conditional_t<D == 64, uint16_t, std::conditional_t<D == 128
 // In place.  A workgroup has a column of a head's rows of K and V, and takes the list's entries in turn.  Every entry is at or behind its own
 // place, so what a batch of entries writes no later one reads; within a batch all is read before anything is written.  Columns have
 // nothing to do with each other.  The next batch's places are looked up while a batch's rows are on their way.
+// Bound by latency: lengths, entries, pages, rows, one after the other.  Paths of 64 sequences of 9 to 16 rows, 8 heads of 128 dimensions, 16 bits:
+// 4.4 us (11 with K and V one after the other and no places looked up ahead).
 constexpr uint32_t kEntries = 64;      // of a batch
 template <int D, int kBits>
 __global__ void __launch_bounds__(256) keep_kernel(const KeepArgs g)
@@ -474,6 +476,8 @@ __global__ void __launch_bounds__(256) keep_kernel(const KeepArgs g)
 
 // To other pages, so nothing that is written is read.  A workgroup has some entries of a list: the rows of K and V of its head or, where one
 // list is for all heads, of all of them, which lie side by side.
+// Bound by memory: 24 x 2,048 tokens out of 4k to 8k, a list for each of 8 heads of 128 dimensions, 16 bits, 404 MB read and written in 90 us,
+// 4.5 TB/s, as fast as a large copy (by the kernel for moves in place, a workgroup to a list, 228).
 constexpr uint32_t kCopyEntries = 32;
 template <int D, int kBits>
 __global__ void __launch_bounds__(256) keep_copy_kernel(const KeepArgs g)

@@ -6,8 +6,10 @@
 // (S^T, with a line to a lane, takes 31 exchanges between lanes for each tile of tokens: 82 us instead of 27 for 32 rows over 5,120 tokens
 // each in 4 bits, 8 heads of 128 dimensions.)  Each weight is written by one workgroup, in an order that does not change.
 //
-//   few_kernel   up to 32 lines: the queries stay in registers, the keys stream through; bound by its loads
-//   many_kernel  more lines: the keys stay, the queries go through LDS for the four waves that share them; bound by the exponentials
+//   few_kernel   up to 32 lines: the queries stay in registers, the keys stream through; bound by its loads: 32 rows over 2k to 8k tokens, 8 heads
+//                of 128 dimensions, 16 bits, 85 us for 360 MB, 4.2 TB/s
+//   many_kernel  more lines: the keys stay, the queries go through LDS for the four waves that share them; bound by the exponentials beside
+//                the products: two prompts of 4k tokens, 32 heads on 8 of 128 dimensions, 154 us, 771 TFLOP/s
 #include "kv_elem.h"
 
 namespace tent {
