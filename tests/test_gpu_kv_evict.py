@@ -561,3 +561,51 @@ def test_calls_on_several_streams_do_not_share_their_workspaces(kv):
             torch.full((need,), 0x7F, dtype=torch.uint8, device="cuda")
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_pools_beyond_four_gib(kv, bits):
+    """Pages 256 MiB apart give what pages side by side give."""
+    results = []
+    for spare in (0, 1 << 28):
+        s = Setup(kv, [9, 17], [150, 170], BF16, bits, 8, 2, 128, 16, seed=70, spare_bytes=spare)
+        parents = torch.tensor([max(i - 2, 0) - (i == 0) for n in s.rows for i in range(n)], **I32)
+        out = list(kv.attend(s.cache, s.batch, s.q.cuda(), tree=kv.tree_masks(parents, s.batch.row_start, 17)[0], want_lse=True))
+        lse = kv.attend(s.cache, s.batch, s.q.cuda(), want_lse=True)[1]
+        weights = kv.weigh(s.cache, s.batch, s.q.cuda(), lse)
+        many = kv.weigh(s.cache, s.batch, s.q.cuda(), lse, per_head=False)
+        lists, counts = kv.choose(s.batch, weights, 16, 2, 5)
+        used = set(s.table.flatten().tolist())
+        free = [p for p in range(s.k16.shape[0]) if p not in used]
+        table = torch.tensor(free, **I32)[:, None]
+        out += [weights, many, lists, kv.keep(s.cache, s.batch, lists, counts, to_table=table)]
+        out += [raw(s, p, i, 16, table.cpu()) for p in (s.k_pool, s.v_pool) for i in (0, 1)]
+        out += kv.keep(s.cache, s.batch, lists, counts, weights=weights)
+        out += [raw(s, p, i) for p in (s.k_pool, s.v_pool) for i in (0, 1)]
+        assert int(s.batch.errors) == 0
+        results.append([x.cpu() if isinstance(x, torch.Tensor) else torch.from_numpy(np.ascontiguousarray(x)) for x in out])
+        assert spare * s.k16.shape[0] == 0 or s.k_pool.stride(0) * s.k_pool.element_size() * (s.k16.shape[0] - 1) > 1 << 32
+        del s
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(*results))
+
+
+def test_rows_and_lists_beyond_four_gib(kv):
+    """Rows of probabilities and lists of weights 4.8 GB apart."""
+    apart, vocab = 1_200_000_000, 30011
+    store = torch.empty(apart + 200000, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(71)
+    target = torch.softmax(2 * torch.randn(2, vocab, device="cuda", generator=g), -1)
+    far = store.as_strided((2, vocab), (apart, 1))
+    far.copy_(target)
+    batch = kv.Batch(torch.zeros(1, 20, **I32), torch.tensor([20], **I32), torch.tensor([0, 2], **I32), 2, 2, 20)
+    best = int(target[0].argmax())
+    args = (torch.tensor([0, best], **I32), torch.zeros(2, device="cuda"), torch.tensor([0.7], device="cuda"))
+    got, want = kv.verify(batch, far, *args), kv.verify(batch, target, *args)
+    assert got[1].tolist() == [2] and all(torch.equal(a, b) for a, b in zip(got, want))
+    for tokens in (5000, 100000):
+        w = torch.randn(2, tokens, device="cuda", generator=g)
+        far = store.as_strided((2, tokens), (apart, 1))
+        far.copy_(w)
+        batch = a_batch(kv, [tokens, tokens - 7])
+        got, want = kv.choose(batch, far, 700, 3, 40), kv.choose(batch, w, 700, 3, 40)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and got[0][1, 699] == tokens - 8
