@@ -13,8 +13,8 @@ namespace {
 // are held in registers for all of it; more are read again for each digit, or, where lists are few, shared by several workgroups
 // (choose_part_kernel).
 //
-// Barriers and latencies bound it.  Measured: one list of 6,000 tokens 13.0 us, 256 lists of 1,000 to 16,384 tokens, four fifths of whose
-// weights are zero, 26 us (with four digits of 8 bits and no ranks 15.5 and 22.6); one list of 131,072 tokens 43 us, by one workgroup 182.
+// Barriers and latencies bound it.  Measured: one list of 6,000 tokens 12.7 us, 256 lists of 1,000 to 16,384 tokens, four fifths of whose
+// weights are zero, 25 us (with four digits of 8 bits and no ranks 15.5 and 22.6); one list of 131,072 tokens 43 us, by one workgroup 182.
 struct ChooseArgs {
     tent_kv_choose_args a;
     tent_kv_batch b;
@@ -66,9 +66,9 @@ __device__ __forceinline__ void clear_counts(uint32_t* count)
     for (uint32_t i = 0; i < kDigits * kCopies / 4 / kChooseThreads; ++i) *(u32x4*)&count[(i * kChooseThreads + threadIdx.x) * 4] = u32x4{0, 0, 0, 0};
 }
 // Counts a digit; lanes that do not count are not here.
-__device__ __forceinline__ void count_digit(uint32_t* count, uint32_t digit)
+__device__ __forceinline__ void count_digit(uint32_t* count, uint32_t digit, uint32_t lane, uint32_t wave)
 {
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, one = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
+    const uint32_t one = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
     const uint64_t alike = __ballot(digit == one);
     if (digit != one) atomicAdd(&count[digit * kCopies + (lane & (kCopies - 1))], 1u);
     else if (lane == (uint32_t)__builtin_ctzll(alike)) atomicAdd(&count[one * kCopies + (wave & (kCopies - 1))], (uint32_t)__popcll(alike));
@@ -162,6 +162,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs
     __shared__ uint32_t before_lds[kHeld * kChooseWaves], digit_lds, wanted_lds, there_lds, all_lds;
     const tent_kv_choose_args& a = g.a;
     const uint32_t block = g.first + blockIdx.x, seq = block / a.n_lists, list = block - seq * a.n_lists;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const KvSeq q = kv_sequence(g.b, seq);
     if (q.bad && threadIdx.x == 0 && list == 0) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
     const uint32_t n = (uint32_t)q.len, kept = n < a.budget ? n : a.budget;      // 0 of a bad sequence
@@ -190,8 +191,13 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs
             for (uint32_t t0 = 0; t0 < n; t0 += kHeldTokens) {
                 if (!once) hold(t0);
                 each_held(n - t0, [&](uint32_t i) {
-                    if (decided(t0 + i * kChooseThreads + threadIdx.x) && (shift == 21 || key[i] >> (shift + bits) == above >> (shift + bits)))
-                        count_digit(count, key[i] >> shift & (digits - 1));
+                    if (decided(t0 + i * kChooseThreads + threadIdx.x) && (shift == 21 || key[i] >> (shift + bits) == above >> (shift + bits))) {
+                        // as count_digit, but called it makes the kernel 3 % slower
+                        const uint32_t digit = key[i] >> shift & (digits - 1), one = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
+                        const uint64_t alike = __ballot(digit == one);
+                        if (digit != one) atomicAdd(&count[digit * kCopies + (lane & (kCopies - 1))], 1u);
+                        else if (lane == (uint32_t)__builtin_ctzll(alike)) atomicAdd(&count[one * kCopies + (wave & (kCopies - 1))], (uint32_t)__popcll(alike));
+                    }
                 });
             }
             __syncthreads();
@@ -324,7 +330,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_part_kernel(const Choos
             each_held(t_end - t0, [&](uint32_t i) {
                 const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
                 if (t < t_end && decided(t) && (kStage == 0 || key[i] >> kBefore == above >> kBefore))
-                    count_digit(count, key[i] >> kShift & (kStage == 2 ? kDigits / 2 - 1 : kDigits - 1));
+                    count_digit(count, key[i] >> kShift & (kStage == 2 ? kDigits / 2 - 1 : kDigits - 1), lane, wave);
             });
         }
         __syncthreads();
