@@ -492,6 +492,8 @@ __global__ void __launch_bounds__(256) weigh_join_kernel(const WeighArgs g)
     g.out[at] = (g.weights ? g.weights[at] : 0.f) + total;
 }
 
+// Lines that few_kernel holds.  32 rows over 5,120 tokens, 8 heads of 128 dimensions, few_kernel and many_kernel: 4 lines in 4 bits 27 and 244 us, in
+// 16 bits 70 and 312; 32 lines 37 and 245, 74 and 312.
 bool few_lines(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_weigh_args& a)
 {
     return (uint64_t)b.max_rows * (a.q_heads / c.kv_heads) <= 32;
@@ -507,7 +509,8 @@ int launch(bool few, WeighArgs g, hipStream_t s)
     const uint64_t max_kv = g.b.max_kv;
     if (few) {
         const bool one = g.n_lists == 1 && g.c.heads > 1;
-        // a wave's run of tiles: as long as there are workgroups for all compute units eight times over
+        // A wave's run of tiles: as long as there are workgroups for all compute units eight times over.  8 heads of 128 dimensions, 1, 2 and 4 tiles: 4
+        // sequences of 5,120 tokens in 4 bits 7.8, 8.5 and 8.5 us; 16 of them 19.2, 17.0 and 17.7; 64 of them 67.8, 53.1 and 50.2, in 16 bits 152, 138 and 138.
         const uint64_t units = (uint64_t)g.b.n_seqs * g.n_lists * ((max_kv + 127) / 128);
         g.run = one || units < 4096 ? 1 : units < 16384 ? 2 : 4;
         g.tiles = (uint32_t)((max_kv + (one ? 32 : 128 * g.run) - 1) / (one ? 32 : 128 * g.run));
