@@ -33,6 +33,20 @@ constexpr uint32_t kHeld = 16, kHeldTokens = kHeld * kChooseThreads;     // toke
 constexpr uint32_t kDigits = 2048, kCopies = 4;
 constexpr uint32_t kRanked = 128;      // each is compared with each
 
+// The digits of a key, from the highest one down: every bit is in one of them.
+struct Digit {
+    int shift, bits;
+    __device__ __forceinline__ uint32_t of(uint32_t key) const { return key >> shift & ((1u << bits) - 1); }
+};
+constexpr int kDigitsOfKey = 3;
+__host__ __device__ constexpr Digit digit_of_key(int i) { return i == 0 ? Digit{21, 11} : i == 1 ? Digit{10, 11} : Digit{0, 10}; }
+constexpr bool digits_cover_keys(int i)
+{
+    return i == kDigitsOfKey ? digit_of_key(i - 1).shift == 0
+                             : 1u << digit_of_key(i).bits <= kDigits && digit_of_key(i).shift + digit_of_key(i).bits == (i ? digit_of_key(i - 1).shift : 32) && digits_cover_keys(i + 1);
+}
+static_assert(digits_cover_keys(0), "a bit in two digits counts weights twice, one in none leaves them apart");
+
 // Larger weights as larger whole numbers; zeros are alike, NaN is minus infinity.
 __device__ __forceinline__ uint32_t weight_key(float w)
 {
@@ -184,18 +198,19 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs
     uint32_t wanted = a.budget - a.first - a.recent, border = 0xFFFFFFFFu, equal = 0;
     if (wanted) {
         uint32_t above = 0;                                              // the digits found, at their places
-        for (int shift = 21, bits = 11; ; bits = shift >= 10 ? 11 : 10, shift = shift >= 21 ? 10 : 0) {
-            const uint32_t digits = 1u << bits;
+        for (int i_digit = 0; ; ++i_digit) {
+            const Digit digit = digit_of_key(i_digit);
+            const int found_shift = digit.shift + digit.bits;            // the bits from here on are found: 32 at first
             clear_counts(count);
             __syncthreads();
             for (uint32_t t0 = 0; t0 < n; t0 += kHeldTokens) {
                 if (!once) hold(t0);
                 each_held(n - t0, [&](uint32_t i) {
-                    if (decided(t0 + i * kChooseThreads + threadIdx.x) && (shift == 21 || key[i] >> (shift + bits) == above >> (shift + bits))) {
+                    if (decided(t0 + i * kChooseThreads + threadIdx.x) && (i_digit == 0 || key[i] >> found_shift == above >> found_shift)) {
                         // as count_digit, but called it makes the kernel 3 % slower
-                        const uint32_t digit = key[i] >> shift & (digits - 1), one = (uint32_t)__builtin_amdgcn_readfirstlane((int)digit);
-                        const uint64_t alike = __ballot(digit == one);
-                        if (digit != one) atomicAdd(&count[digit * kCopies + (lane & (kCopies - 1))], 1u);
+                        const uint32_t mine = digit.of(key[i]), one = (uint32_t)__builtin_amdgcn_readfirstlane((int)mine);
+                        const uint64_t alike = __ballot(mine == one);
+                        if (mine != one) atomicAdd(&count[mine * kCopies + (lane & (kCopies - 1))], 1u);
                         else if (lane == (uint32_t)__builtin_ctzll(alike)) atomicAdd(&count[one * kCopies + (wave & (kCopies - 1))], (uint32_t)__popcll(alike));
                     }
                 });
@@ -204,17 +219,17 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const ChooseArgs
             if (threadIdx.x == 0) there_lds = 0;
             const uint32_t mine[2] = {counted(count, first_digit()), counted(count, first_digit() - 1)};
             find_digit(mine, wanted, before_lds, digit_lds, wanted_lds, all_lds);
-            above |= digit_lds << shift;
+            above |= digit_lds << digit.shift;
             wanted = wanted_lds;
             const uint32_t there = all_lds;
-            if (shift == 0) break;
+            if (i_digit == kDigitsOfKey - 1) break;
             if (there > kRanked) continue;
             // Those with the digit, in any order, and the rank of each: the greater ones and, of the same, the earlier ones come before it.
             for (uint32_t t0 = 0; t0 < n; t0 += kHeldTokens) {
                 if (!once) hold(t0);
                 each_held(n - t0, [&](uint32_t i) {
                     const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
-                    if (decided(t) && key[i] >> shift == above >> shift) *(u32x2*)&count[2 * atomicAdd(&there_lds, 1u)] = u32x2{key[i], t};
+                    if (decided(t) && key[i] >> digit.shift == above >> digit.shift) *(u32x2*)&count[2 * atomicAdd(&there_lds, 1u)] = u32x2{key[i], t};
                 });
             }
             __syncthreads();
@@ -260,7 +275,8 @@ __global__ void __launch_bounds__(kChooseThreads) choose_part_kernel(const Choos
 {
     __shared__ __align__(16) uint32_t count[kDigits * kCopies];
     __shared__ uint32_t before_lds[kHeld * kChooseWaves], digit_lds, wanted_lds, all_lds, above_lds[kChooseWaves], same_lds;
-    constexpr int kShift = kStage == 0 ? 21 : kStage == 1 ? 10 : 0, kBefore = kStage == 1 ? 21 : kStage == 2 ? 10 : 0;      // of this stage's digit; of the last one's
+    constexpr Digit kDigit = digit_of_key(kStage);                       // this stage's (not of the last stage); how far down the one before it goes
+    constexpr int kBefore = kStage == 0 ? 0 : digit_of_key(kStage - 1).shift;
     const tent_kv_choose_args& a = g.a;
     const uint32_t block = g.first + blockIdx.x, at = block / g.parts, part = block - at * g.parts, seq = at / a.n_lists, list = at - seq * a.n_lists;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
@@ -330,7 +346,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_part_kernel(const Choos
             each_held(t_end - t0, [&](uint32_t i) {
                 const uint32_t t = t0 + i * kChooseThreads + threadIdx.x;
                 if (t < t_end && decided(t) && (kStage == 0 || key[i] >> kBefore == above >> kBefore))
-                    count_digit(count, key[i] >> kShift & (kStage == 2 ? kDigits / 2 - 1 : kDigits - 1), lane, wave);
+                    count_digit(count, kDigit.of(key[i]), lane, wave);
             });
         }
         __syncthreads();

@@ -225,6 +225,47 @@ def test_choose_takes_a_workspace_of_any_contents(kv):
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool((work[need:] == byte).all())
 
 
+def low_weights(kind, shape, g):
+    """Weights of which more than 128 share their leading 22 bits, so that the last ten decide."""
+    if kind == "near one":
+        return 1 + 1e-3 * torch.randn(shape, generator=g)
+    if kind == "bit 10":                                                 # two values, of four in five places the smaller one
+        bits = (torch.rand(shape, generator=g) < 0.2).int() << 10
+    else:
+        bits = torch.randint(0, 4096, shape, generator=g).int()
+    return (bits + 0x3F800000 + (-0x80000000 if kind == "negative" else 0)).int().view(torch.float32)
+
+
+# one list a workgroup, held whole; more lists than workgroups share, several rounds each; lists that workgroups share
+@pytest.mark.parametrize("tokens,heads", [([1000, 16384, 1025], 2), ([20000, 16385], 65), ([33000, 20000], 1)])
+@pytest.mark.parametrize("kind", ["any", "negative", "bit 10", "near one"])
+def test_choose_weights_that_differ_in_their_last_bits(kv, tokens, heads, kind):
+    g = torch.Generator().manual_seed(heads)
+    n = max(tokens)
+    w = low_weights(kind, (len(tokens), heads, n), g)
+    batch, x = a_batch(kv, tokens), w.cuda()
+    sorted_once = {}
+    for share in (0.05, 0.15, 0.3, 0.5, 0.7, 0.95):                      # borders with bit 10 set and not, in each of the groups
+        budget, first, recent = int(share * min(tokens)), 4, 32
+        lists = torch.full((len(tokens), heads, budget + 3), -77, **I32)  # whatever is not written shows
+        counts = torch.full((len(tokens),), -77, **I32)
+        a = T.tent_kv_choose_args(x.data_ptr(), lists.data_ptr(), counts.data_ptr(), n, budget + 3, None, 0, heads, budget, first, recent)
+        need = T.tent_kv_choose_workspace(batch.c, a)
+        assert (need > 0) == (n > T.TENT_KV_CHOOSE_WHOLE and heads == 1)
+        work = torch.full((max(need, 1),), 0xA5, dtype=torch.uint8, device="cuda")
+        a.workspace, a.workspace_bytes = work.data_ptr() if need else None, need
+        T.tent_kv_choose(batch.c, a)
+        assert counts.tolist() == [budget] * len(tokens) and bool((lists[..., budget:] == -77).all()) and int(batch.errors) == 0
+        got = lists[..., :budget].cpu().numpy()
+        for i, t in enumerate(tokens):
+            for h in range(heads):                                       # as TR.choose, sorted once for all budgets
+                if (i, h) not in sorted_once:
+                    order = np.lexsort((np.arange(t), -w[i, h, :t].numpy()))
+                    sorted_once[i, h] = order[(order >= first) & (order < t - recent)]
+                want = np.sort(np.concatenate([np.arange(first), np.arange(t - recent, t), sorted_once[i, h][:budget - first - recent]]))
+                assert (got[i, h] == want).all(), (budget, i, h, int((got[i, h] == -77).sum()))
+
+
 def test_choose_sequences_that_are_left_out(kv):
     batch = a_batch(kv, [50, 60, 70], most=65)
     w = torch.rand(3, 65, generator=torch.Generator().manual_seed(4))
