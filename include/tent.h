@@ -646,7 +646,8 @@ int tent_kv_attend(const tent_kv_cache *cache, const tent_kv_batch *batch, const
  * tent_kv_verify finds which rows stand, given the target's probabilities and random numbers, and tent_kv_keep makes those the
  * sequence.  A cache that gets too long is cut the same way: tent_kv_weigh adds up the attention that every token has got, tent_kv_choose
  * says which tokens a sequence keeps, tent_kv_keep moves them together.  Everything said above of rows, errors, alignment, streams
- * and graphs holds for them; none takes atomics but the error bits, so results repeat bit for bit.
+ * and graphs holds for them; none takes atomics but the error bits, so results repeat bit for bit.  What a call writes shares
+ * no memory with what it reads, unless it says so below: other workgroups may still be reading.
  */
 enum { TENT_KV_KEEP_ROWS = 1u << 0 };                       /* tent_kv_keep_args.flags: lists name rows, not tokens   */
 enum { TENT_KV_MAX_VOCAB = 1 << 20 };

@@ -385,6 +385,24 @@ def _by_list(tensor, name, dtype, n_seqs, width, device):
     return lists, apart
 
 
+def _meets(out, x):
+    """Whether the bytes of `out`, which is contiguous, have any of `x`, whose rows are contiguous and all as far apart."""
+    size, a = x.element_size(), out.data_ptr() - x.data_ptr()
+    width = x.shape[-1] * size
+    if not x.numel() or not out.numel():
+        return False
+    apart = min([stride for stride, n in zip(x.stride()[:-1], x.shape[:-1]) if n > 1], default=x.shape[-1]) * size
+    first = max(0, (a - width) // apart + 1)                             # the first row that ends behind where `out` begins
+    return first < x.numel() // x.shape[-1] and first * apart < a + out.numel() * out.element_size()
+
+
+def _apart(out, name, used):
+    """Refuses an output that other workgroups would still be reading as one of the tensors `used`."""
+    for x in used:
+        if x is not None and _meets(out, x):
+            raise ValueError(f"{name} must not share memory with what the call reads")
+
+
 def _like(tensor, lists, apart, known):
     """A new tensor laid out as one that _by_list has seen, with its values from place `known` of a list on."""
     shape = (tensor.shape[0], apart) if tensor.dim() == 2 else (tensor.shape[0], lists, apart)
@@ -404,7 +422,8 @@ def verify(batch: Batch, target, tokens, accept, next, parents=None, draft=None,
     tokens, of which the first of a sequence stands for the one that is decided already.  parents: int32 [rows], the row of its
     sequence that a row is behind; the one before unless given.  draft: as target, the probabilities that the rows behind a row
     were drawn from, each by itself; None: they were chosen without drawing.  accept: float32 [rows] and next: float32 [sequences],
-    random numbers, 0 <= u < 1.  workspace: a contiguous uint8 tensor of at least verify_workspace bytes to use instead of a new one."""
+    random numbers, 0 <= u < 1.  path: int32 [sequences, max_rows] to use instead of a new one, apart from the tensors that are read.
+    workspace: a contiguous uint8 tensor of at least verify_workspace bytes, likewise."""
     if stream is not None or batch.device.index != _current_device():
         used = [x for x in (*batch.tensors, target, tokens, accept, next, parents, draft, path, workspace) if x is not None]
         return _on(batch.device, stream, used, lambda: verify(batch, target, tokens, accept, next, parents, draft, path, workspace))
@@ -430,6 +449,8 @@ def verify(batch: Batch, target, tokens, accept, next, parents=None, draft=None,
         path = torch.empty((n_seqs, most), dtype=torch.int32, device=device)
     elif not _on_gpu(path, "path", torch.int32, (n_seqs, most)).is_contiguous() or path.device != device:
         raise ValueError("path must be contiguous, on the batch's device")
+    else:
+        _apart(path, "path", (*batch.tensors, target, tokens, accept, next, parents, draft))
     counts, token = torch.empty((n_seqs,), dtype=torch.int32, device=device), torch.empty((n_seqs,), dtype=torch.int32, device=device)
     a.path, a.counts, a.token = path.data_ptr(), counts.data_ptr(), token.data_ptr()
     a.vocab, a.path_stride, a.type = vocab, most, _PROBABILITIES[target.dtype]
@@ -540,7 +561,8 @@ def keep(cache: Cache, batch: Batch, lists, counts, rows: bool = False, to_table
     Token j becomes what token lists[sequence, (head,) j] was, for j below counts[sequence]; one list for all heads or one for each.  With
     rows=True lists name rows of the sequence (verify's path) and the context in front of them stays.  In place, unless to_table
     (int32 [sequences, pages]) names other pages to write to.  weights: float32 [sequences, (heads,) max_kv or more], moved to weights_out
-    (in place itself unless given; a new tensor with to_table), behind the last kept token 0."""
+    (in place itself unless given; a new tensor with to_table), behind the last kept token 0.  kv_len_out shares no memory with what is
+    read, nor with the batch's kv_len: heads whose turn comes later still read that."""
     if stream is not None or cache.index != _current_device():
         used = [x for x in (*cache.tensors, *batch.tensors, lists, counts, to_table, weights, weights_out, kv_len_out) if x is not None]
         return _on(cache.device, stream, used, lambda: keep(cache, batch, lists, counts, rows, to_table, weights, weights_out, kv_len_out))
@@ -570,7 +592,10 @@ def keep(cache: Cache, batch: Batch, lists, counts, rows: bool = False, to_table
         raise ValueError("weights_out goes with weights")
     if kv_len_out is None:
         kv_len_out = torch.empty((n_seqs,), dtype=torch.int32, device=device)
-    a.kv_len_out = _vector(kv_len_out, "kv_len_out", torch.int32, n_seqs, device)
+        a.kv_len_out = kv_len_out.data_ptr()
+    else:
+        a.kv_len_out = _vector(kv_len_out, "kv_len_out", torch.int32, n_seqs, device)
+        _apart(kv_len_out, "kv_len_out", (batch.page_table, batch.errors, lists, to_table, weights))
     a.list_stride, a.n_lists, a.most, a.flags = apart, n_lists, lists.shape[-1], T.TENT_KV_KEEP_ROWS if rows else 0
     _check(T.lib().tent_kv_keep(cache.ref, batch.ref, C.byref(a), _stream(cache.index)), "tent_kv_keep")
     return kv_len_out if weights is None else (kv_len_out, weights_out)

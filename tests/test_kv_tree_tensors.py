@@ -238,6 +238,36 @@ def test_strides_are_handed_on(gpus):
     assert gpus.args.weights != gpus.args.weights_out                    # to other pages: not in place
 
 
+def test_outputs_that_share_memory_with_what_is_read_are_refused(gpus):
+    s = Step(gpus)
+    i32 = torch.int32
+    store = torch.zeros(64, dtype=i32)
+    part = lambda at, *shape, dtype=i32: s.on(store[at:at + int(np.prod(shape))].view(shape).view(dtype))  # noqa: E731
+    rows = lambda at, n, width, apart: s.on(store.as_strided((n, width), (apart, 1), at))  # noqa: E731
+    for at in range(12):                                                 # path: four values from 3 on
+        for name, n in (("tokens", 3), ("parents", 3), ("accept", 3), ("next", 2)):
+            x = part(at, n, dtype=torch.float32 if name in ("accept", "next") else i32)
+            refused(gpus, s.verify, {"path": part(3, 2, 2), name: x}, at < 7 and at + n > 3)
+    s.batch = kv.Batch(s.batch.page_table, part(40, 2), part(50, 3), 3, 2, 20)
+    for at in range(36, 56):
+        refused(gpus, s.verify, dict(path=part(at, 2, 2)), any(at <= x < at + 4 for x in (40, 41, 50, 51, 52)))
+        if at not in (39, 40, 41, 49, 50, 51, 52):                       # those the library refuses
+            refused(gpus, s.keep, dict(kv_len_out=part(at, 2)), False)
+    for at in range(0, 30):                                              # lists of two values, nine apart, from 3 on: 3, 4, 12, 13
+        refused(gpus, s.keep, dict(kv_len_out=part(at, 2), lists=rows(3, 2, 2, 9), weights=None), any(at <= x < at + 2 for x in (3, 4, 12, 13)))
+        refused(gpus, s.keep, dict(kv_len_out=part(at, 2), to_table=rows(3, 2, 2, 9), weights=None), any(at <= x < at + 2 for x in (3, 4, 12, 13)))
+
+
+def refused(gpus, call, change, is_refused):
+    n = len(gpus.log)
+    if is_refused:
+        with pytest.raises(ValueError, match="share memory"):
+            call(**change)
+    else:
+        call(**change)
+    assert any(e[0] in NAMES for e in gpus.log[n:]) != is_refused
+
+
 @pytest.mark.parametrize("seed", range(6))
 def test_masks_of_trees(seed):
     rng = random.Random(seed)
