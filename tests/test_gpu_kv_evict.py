@@ -146,6 +146,72 @@ def test_weigh_no_rows(kv):
     assert not kv.weigh(s.cache, s.batch, q, lse).any()
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("n_seqs,dtype,dim", [(64, BF16, 128), (256, FP16, 64), (64, BF16, 256), (256, BF16, 128)])
+def test_weigh_several_tiles_to_a_wave(kv, n_seqs, dtype, dim, bits):
+    """Eight heads over up to 1,000 tokens: 64 sequences have runs of two tiles, 256 of four.  Lengths end in any tile of a run."""
+    rng = random.Random(n_seqs + dim)
+    rows = [rng.choice([0, 1, 1, 2, 8]) for _ in range(n_seqs)]
+    tokens = [r + rng.choice([0, rng.randint(0, 70), rng.randint(0, 300)]) for r in rows]
+    rows[:4], tokens[:4] = [1, 8, 2, 1], [1000, 999, 513, 512]
+    check_many(kv, rows, tokens, dtype, bits, 16, 8, dim, True, left_out=(5, n_seqs - 1))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("heads,dtype,dim", [(5, BF16, 128), (8, FP16, 64), (9, BF16, 256), (8, BF16, 128)])
+def test_weigh_one_list_for_many_heads(kv, heads, dtype, dim, bits):
+    """Four waves share the heads: they take two or three each, or some none."""
+    check_many(kv, [1, 0, 3, 10, 2, 1], [300, 20, 35, 10, 129, 31], dtype, bits, 2 * heads, heads, dim, False, left_out=(4,))
+
+
+class Coded(Setup):
+    """4-bit pages of any codes, and scales of 2^-3 to 2^3: quicker than packing values."""
+
+    def packed(self, values):
+        n, count = values.shape[0], self.page_tokens * self.heads
+        out = torch.randint(0, 256, (n, self.kv.packed_page_bytes(self.page_tokens, self.heads, self.dim)), generator=self.g).to(torch.uint8)
+        scales = torch.randint(124, 131, (n, count * self.dim // 32), generator=self.g).to(torch.uint8)
+        out[:, count * self.dim // 2:count * self.dim // 2 + scales.shape[1]] = scales
+        return out
+
+
+def check_many(kv, rows, tokens, dtype, bits, q_heads, heads, dim, per_head, left_out=()):
+    """As check_weights, with a window and without; the pages' values are looked up once."""
+    s = Coded(kv, rows, tokens, dtype, bits, q_heads, heads, dim, 16, seed=heads + dim)
+    for i in left_out:
+        s.batch.kv_len[i] = -1
+    values, scale, n, most = s.values(s.k_pool), 1 / math.sqrt(dim), len(rows), max(tokens)
+    keys = [values[s.table[i, :-(-t // 16)].long().numpy()].reshape(-1, heads, dim)[:t] for i, t in enumerate(tokens)]
+    held = torch.rand((n, heads, most) if per_head else (n, most), generator=s.g)
+    for window in (0, 40):
+        seen = [TR.spans(r, t, window) for r, t in zip(rows, tokens)]
+        lse = torch.full((s.n_rows, q_heads), -math.inf)
+        for i, r in enumerate(rows):
+            for j in range(r):
+                at = seen[i][j]
+                x = np.einsum("hd,thd->ht", s.q[s.starts[i] + j].double().numpy(), np.repeat(keys[i][at], q_heads // heads, 1)) * scale
+                if x.shape[1]:
+                    lse[s.starts[i] + j] = torch.from_numpy(np.logaddexp.reduce(x, 1))
+        got = kv.weigh(s.cache, s.batch, s.q.cuda(), lse.cuda(), weights=held.cuda(), per_head=per_head, window=window)
+        fresh = kv.weigh(s.cache, s.batch, s.q.cuda(), lse.cuda(), per_head=per_head, window=window)
+        sides = [(x.cpu().double().numpy(), y.double().numpy()) for x, y in ((got, held), (fresh, torch.zeros(held.shape)))]
+        for i, (r, t) in enumerate(zip(rows, tokens)):
+            if i in left_out or r == 0:
+                for result, before in sides:
+                    same(result[i], before[i])
+                continue
+            at = slice(s.starts[i], s.starts[i] + r)
+            want, off = TR.weigh(s.q[at].double().numpy(), keys[i], lse[at].double().numpy(), seen[i], scale)
+            if not per_head:
+                off, want = off.sum(0) + 2.0 ** -24 * heads * want.sum(0), want.sum(0)
+            for result, before in sides:
+                have = before[i, ..., :t]
+                d = np.abs(result[i, ..., :t] - want - have)
+                assert (d <= off + 2.0 ** -24 * (want + 2 * have)).all(), (window, i)
+                same(result[i, ..., t:], before[i, ..., t:])
+        assert int(s.batch.errors) == (T.TENT_KV_BAD_SEQUENCE if left_out else 0)
+
+
 # ---- choose --------------------------------------------------------------------------------------
 def a_batch(kv, tokens, most=None):
     n = len(tokens)
@@ -364,6 +430,33 @@ def test_keep_long_lists_in_place(kv, bits):
             for i, c in enumerate(counts):
                 for pool, old in zip((s.k_pool, s.v_pool), before[i]):
                     assert (raw(s, pool, i, c) == old[lists[i, :c].numpy()]).all(), (kind, i)
+
+
+@pytest.mark.parametrize("bits,dim", [(16, 64), (16, 128), (16, 256), (4, 128)])
+def test_keep_many_lists_in_place(kv, bits, dim):
+    # as many lists as fill the card: a workgroup moves whole rows of its head
+    rng = np.random.RandomState(dim)
+    tokens = [int(t) for t in rng.randint(0, 200, 64)]
+    s = Setup(kv, [0] * 64, tokens, BF16, bits, 8, 8, dim, 16, seed=dim)
+    counts = [int(rng.randint(0, t + 1)) for t in tokens]
+    entries = np.full((64, 8, max(counts) + 1), -1, np.int32)
+    for i, (t, c) in enumerate(zip(tokens, counts)):
+        for h in range(8):
+            entries[i, h, :c] = np.sort(rng.permutation(t)[:c]) if h % 2 else np.arange(c) + (rng.rand(c) * (t - np.arange(c))).astype(int)
+    before = [[raw(s, p, i) for p in (s.k_pool, s.v_pool)] for i in range(64)]
+    weights = torch.rand(64, 8, s.batch.max_kv, generator=s.g)
+    w = weights.cuda()
+    length, _ = kv.keep(s.cache, s.batch, torch.from_numpy(entries).cuda(), torch.tensor(counts, **I32), weights=w)
+    assert length.tolist() == counts and int(s.batch.errors) == 0
+    w = w.cpu()
+    for i, (t, c) in enumerate(zip(tokens, counts)):
+        for pool, old in zip((s.k_pool, s.v_pool), before[i]):
+            got = raw(s, pool, i)
+            assert (got[c:] == old[c:]).all()
+            for h in range(8):
+                assert (got[:c, h] == old[entries[i, h, :c], h]).all(), (i, h)
+        for h in range(8):
+            assert torch.equal(w[i, h, :c], weights[i, h][torch.from_numpy(entries[i, h, :c]).long()]) and not w[i, h, c:].any()
 
 
 @pytest.mark.parametrize("elsewhere", [True, False])

@@ -189,6 +189,107 @@ def test_wrong_pages_and_sequences(kv):
     check_tree(s, seen, out, lse, skip=(0, 1))
 
 
+# ---- 33 to 64 lines: two waves to 32 of them, each with half of a tile's tokens -------------------
+HALVES = [(BF16, 64), (BF16, 128), (BF16, 256), (FP16, 128)]
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("dtype,dim", HALVES)
+def test_trees_of_33_to_64_lines(kv, dtype, dim, bits):
+    # tokens in the first wave's half of a tile only, in both, and (of a window) in the second's only; lines of the second 32 or none
+    rows, before = [17, 32, 1, 0, 16, 20, 31], [0, 14, 700, 5, 16, 44, 129]
+    s = Setup(kv, rows, [r + b for r, b in zip(rows, before)], dtype, bits, 4, 2, dim, 16, seed=dim, spare_bytes=32)
+    rng = random.Random(dim)
+    trees = [TR.ancestors(some_tree(rng, n)) for n in rows]
+    masks = [np.random.RandomState(dim + i).rand(n, n) < 0.3 for i, n in enumerate(rows)]
+    for x in masks:
+        if len(x):
+            x[0] = False
+    for seen in (trees, masks):
+        for window in (0, 32, 45):
+            out, lse = kv.attend(s.cache, s.batch, s.q.cuda(), tree=masks_of(seen, 3, rng), window=window, want_lse=True)
+            check_tree(s, seen, out, lse, window)
+    assert int(s.batch.errors) == 0
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("dtype,dim", HALVES)
+def test_33_to_64_lines_over_a_split_context(kv, dtype, dim, bits):
+    rows = [20, 32]
+    s = Setup(kv, rows, [2600, 1031], dtype, bits, 4, 2, dim, 16, seed=2 * dim)
+    seen = [TR.ancestors(some_tree(random.Random(dim), n)) for n in rows]
+    for window in (0, 900):
+        assert kv.attend_workspace(s.cache, s.batch, 4, window, tree=True) > 0
+        got = [kv.attend(s.cache, s.batch, s.q.cuda(), tree=masks_of(seen), window=window, want_lse=True) for _ in range(2)]
+        check_tree(s, seen, *got[0], window)
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+def test_33_to_64_lines_in_front_of_the_sequence(kv):
+    rows, tokens = [20, 32, 17], [4, 31, 0]
+    s = Setup(kv, rows, tokens, BF16, 16, 4, 2, 64, 16, seed=9)
+    seen = [np.random.RandomState(i).rand(n, n) < 0.4 for i, n in enumerate(rows)]
+    out, lse = kv.attend(s.cache, s.batch, s.q.cuda(), tree=masks_of(seen), want_lse=True)
+    check_tree(s, seen, out, lse)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_33_to_64_lines_without_influence_of_what_is_not_seen(kv, bits):
+    test_rows_that_are_not_seen_have_no_influence(kv, [20, 30], bits)
+    test_rows_that_are_not_seen_have_no_influence(kv, [32, 17], bits)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("place", [2, 37, 63, 64, 90])
+def test_33_to_64_lines_and_infinite_values(kv, dim, place):
+    # a token of either wave's half, of a tile that every line sees whole or of one that is masked
+    rows, before = [20, 32], [100, 3]
+    s = Setup(kv, rows, [r + b for r, b in zip(rows, before)], BF16, 16, 4, 2, dim, 16, seed=12)
+    seen = [TR.ancestors(some_tree(random.Random(8), n)) for n in rows]
+    q, masks = s.q.cuda(), masks_of(seen)
+    base, base_lse = kv.attend(s.cache, s.batch, q, tree=masks, want_lse=True)
+    at = [place, 3 + place % 32]
+    for i in range(2):
+        s.v_pool[int(s.table[i, at[i] // 16]), at[i] % 16, :, 5] = -math.inf
+    out, lse = kv.attend(s.cache, s.batch, q, tree=masks, want_lse=True)
+    sees = torch.from_numpy(np.concatenate([TR.visible(x, t)[:, a] for x, t, a in zip(seen, s.tokens, at)]))
+    assert torch.equal(lse, base_lse)
+    out, want = out.cpu(), base.cpu()
+    assert bool(sees.any()) and bool((out[sees][:, :, 5] == -math.inf).all())
+    out[sees, :, 5] = want[sees, :, 5] = 0
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("before", [(20, 100), (6000, 100), (0, 44)])
+def test_33_to_64_lines_and_values_near_the_largest(kv, dim, before):
+    rows = [20, 32]
+    s = Setup(kv, rows, [r + b for r, b in zip(rows, before)], BF16, 16, 4, 2, dim, 16, seed=13)
+    s.v_pool.mul_(2.0 ** 125)
+    seen = [TR.ancestors(some_tree(random.Random(9), n)) for n in rows]
+    out, lse = kv.attend(s.cache, s.batch, s.q.cuda(), tree=masks_of(seen), want_lse=True)
+    check_tree(s, seen, out, lse)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_33_to_64_lines_wrong_pages_and_sequences(kv, bits):
+    from paper_2604_00368_amd import binding as T
+    s = Setup(kv, [20, 32, 17], [90, 40, 130], BF16, bits, 4, 2, 64, 16, seed=15)
+    seen = [TR.ancestors(some_tree(random.Random(2), n)) for n in s.rows]
+    s.batch.page_table[0, 2] = 1 << 30                                   # tokens 32 .. 47 of the first: the second wave's
+    s.batch.kv_len[1] = 10_000                                           # and the second is left out
+    held = torch.zeros(69, 4, 64, dtype=BF16, device="cuda").fill_(7)
+    out, lse = kv.attend(s.cache, s.batch, s.q.cuda(), tree=masks_of(seen), want_lse=True, out=held)
+    assert int(s.batch.errors) == T.TENT_KV_BAD_SEQUENCE | T.TENT_KV_BAD_PAGE
+    assert bool((out[20:52] == 7).all())
+    see = TR.visible(seen[0], 90)
+    see[:, 32:48] = False
+    want, _, mass, size = TR.attend(s.q[:20].double().numpy(), s.held(s.k_pool, 0), s.held(s.v_pool, 0), see, 1 / 8)
+    bound, _ = R.attend_bounds(want, mass, size, 90, 64, BF16)
+    assert (np.abs(out[:20].double().cpu().numpy() - want) <= bound).all()
+    check_tree(s, seen, out, lse, skip=(0, 1))
+
+
 # ---- verify --------------------------------------------------------------------------------------
 def probabilities(rng, rows, vocab, dtype, sharp=3.0):
     x = rng.randn(rows, vocab) * sharp
