@@ -760,7 +760,7 @@ int tent_kv_choose_workspace(const tent_kv_batch *batch, const tent_kv_choose_ar
  * In place an entry must not be below its own number j, so that lists may name a token twice and nothing is read that was written;
  * with to_table, whose pages must not be ones that are read, entries may be anything below kv_len (below the rows).  An entry that is not
  * is left out and noted (TENT_KV_BAD_POSITION); wrong pages likewise.  Pages that are written are to be of one sequence.  A sequence with a count that is negative, more than
- * `most`, or more than it has (in place), with
+ * `most`, more than it has (in place), or makes it 2^31 tokens, with
  * rows of which some are at negative positions, and one that is left out, stay as they are, with their kv_len, noted as
  * TENT_KV_BAD_SEQUENCE. */
 int tent_kv_keep(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_keep_args *args, void *stream);

@@ -377,22 +377,17 @@ struct KeepArgs {
 };
 constexpr uint64_t kNowhere = ~0ull;
 
-// What a sequence's lists are about: tokens from `base` on, `have` of them, of which `count` entries are kept.
-struct Kept { int32_t base, have, count; bool bad; };
-__device__ __forceinline__ Kept kept_of(const tent_kv_keep_args& a, const KvSeq& q, uint32_t seq)
+__device__ __forceinline__ KvKept kept_of(const tent_kv_keep_args& a, const KvSeq& q, uint32_t seq)
 {
-    const bool rows = a.flags & TENT_KV_KEEP_ROWS;
-    Kept k{rows ? q.len - q.rows : 0, rows ? q.rows : q.len, a.counts[seq], false};
-    k.bad = q.bad || k.base < 0 || k.count < 0 || (uint32_t)k.count > a.most || (!a.to_table && k.count > k.have);
-    return k;
+    return kv_kept(q, a.flags & TENT_KV_KEEP_ROWS, a.to_table != nullptr, a.counts[seq], a.most);
 }
 // By one thread of the sequence's workgroups.
-__device__ __forceinline__ void tell_length(const KeepArgs& g, const Kept& k, uint32_t seq)
+__device__ __forceinline__ void tell_length(const KeepArgs& g, const KvKept& k, uint32_t seq)
 {
     if (k.bad) kv_note(g.b.errors, TENT_KV_BAD_SEQUENCE);
-    if (g.a.kv_len_out) g.a.kv_len_out[seq] = k.bad ? g.b.kv_len[seq] : k.base + k.count;
+    if (g.a.kv_len_out) g.a.kv_len_out[seq] = k.bad ? g.b.kv_len[seq] : k.length();
 }
-__device__ __forceinline__ bool entry_ok(const tent_kv_keep_args& a, const Kept& k, int32_t entry, int32_t j)
+__device__ __forceinline__ bool entry_ok(const tent_kv_keep_args& a, const KvKept& k, int32_t entry, int32_t j)
 {
     return entry < k.have && entry >= (a.to_table ? 0 : j);
 }
@@ -431,7 +426,7 @@ __global__ void __launch_bounds__(256) keep_kernel(const KeepArgs g)
     const int32_t* const list = a.lists + ((uint64_t)seq * a.n_lists + (a.n_lists == 1 ? 0u : head)) * a.list_stride;
     int32_t entry_ahead = threadIdx.x < kEntries && threadIdx.x < a.most ? list[threadIdx.x] : -1;       // on its way beside the lengths
     const KvSeq q = kv_sequence(g.b, seq);
-    const Kept k = kept_of(a, q, seq);
+    const KvKept k = kept_of(a, q, seq);
     if (column == 0 && head == 0 && threadIdx.x == 0) tell_length(g, k, seq);
     if (k.bad) return;
     const int32_t* const table = g.b.page_table + (uint64_t)seq * g.b.table_stride;
@@ -514,7 +509,7 @@ __global__ void __launch_bounds__(256) keep_copy_kernel(const KeepArgs g)
     if (unit >= g.b.n_seqs * g.parts) return;
     const uint32_t seq = unit % g.b.n_seqs, j0 = unit / g.b.n_seqs * kCopyEntries;
     const KvSeq q = kv_sequence(g.b, seq);
-    const Kept k = kept_of(a, q, seq);
+    const KvKept k = kept_of(a, q, seq);
     if (head == 0 && j0 == 0 && threadIdx.x == 0) tell_length(g, k, seq);
     if (k.bad || j0 >= (uint32_t)k.count) return;
     const uint32_t n = (uint32_t)k.count - j0 < kCopyEntries ? (uint32_t)k.count - j0 : kCopyEntries;
@@ -573,7 +568,7 @@ __global__ void __launch_bounds__(256) keep_weights_kernel(const KeepArgs g)
     const tent_kv_keep_args& a = g.a;
     const uint32_t block = g.first + blockIdx.x, seq = block / a.n_weights, l = block - seq * a.n_weights;
     const KvSeq q = kv_sequence(g.b, seq);
-    const Kept k = kept_of(a, q, seq);
+    const KvKept k = kept_of(a, q, seq);
     const int32_t* const list = a.lists + ((uint64_t)seq * a.n_lists + (a.n_lists == 1 ? 0u : l)) * a.list_stride;
     const float* const from = a.weights + (uint64_t)block * a.weights_stride;
     float* const to = a.weights_out + (uint64_t)block * a.weights_stride;
@@ -598,7 +593,7 @@ __global__ void __launch_bounds__(256) keep_weights_kernel(const KeepArgs g)
             if (j < count && base + j < most) to[base + j] = w[i];
         }
     }
-    for (int32_t t = base + count + (int32_t)threadIdx.x; t < most; t += 256) to[t] = 0.f;
+    for (int32_t t = (k.bad ? most : k.length_up_to(most)) + (int32_t)threadIdx.x; t < most; t += 256) to[t] = 0.f;
 }
 
 // Whether several workgroups share a list, and how many: each finds the digits from the counts of all of them, so there are not many.

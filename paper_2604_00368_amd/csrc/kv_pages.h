@@ -120,6 +120,20 @@ TENT_KV_BOTH KvSeq kv_sequence(const tent_kv_batch& b, int32_t lo, int32_t hi, i
 }
 TENT_KV_BOTH KvSeq kv_sequence(const tent_kv_batch& b, uint32_t s) { return kv_sequence(b, b.row_start[s], b.row_start[s + 1], b.kv_len[s]); }
 
+// What a sequence's lists of kept tokens are about: tokens from `base` on, `have` of them, of which `count` entries are kept.  Bad: it stays as it is.
+struct KvKept {
+    int32_t base, have, count;
+    bool bad;
+    TENT_KV_BOTH int32_t length() const { return base + count; }         // afterwards; of one that is not bad
+    TENT_KV_BOTH int32_t length_up_to(int32_t most) const { return length() < most ? length() : most; }
+};
+TENT_KV_BOTH KvKept kv_kept(const KvSeq& q, bool by_rows, bool elsewhere, int32_t count, uint32_t most)
+{
+    KvKept k{by_rows ? q.len - q.rows : 0, by_rows ? q.rows : q.len, count, false};
+    k.bad = q.bad || k.base < 0 || count < 0 || (uint32_t)count > most || (!elsewhere && count > k.have) || count > 0x7FFFFFFF - k.base;
+    return k;
+}
+
 // Byte offset of the page that holds token t (0 <= t < max_kv) of sequence s; negative where the table names none of the pool.
 TENT_KV_BOTH int64_t kv_page_of(const KvCache& c, const tent_kv_batch& b, uint32_t s, uint32_t t)
 {

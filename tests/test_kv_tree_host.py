@@ -236,6 +236,45 @@ def test_memory_that_two_arguments_share_is_found_on_the_host(tmp_path):
     assert subprocess.check_output([str(exe)]).decode() == "ok\n"
 
 
+KEPT = r'''
+#include <assert.h>
+#include <stdio.h>
+#include "kv_pages.h"
+using namespace tent;
+int main()
+{
+    const int32_t most = 1 << 30;                               // the longest list, and the longest sequence
+    const int32_t sizes[] = {0, 1, 255, 4096, most - 4096, most - 1, most};
+    for (int32_t len : sizes) for (int32_t rows : sizes) for (int32_t count : sizes) for (int flags = 0; flags < 4; ++flags) {
+        const bool by_rows = flags & 1, elsewhere = flags & 2;
+        const KvKept k = kv_kept(KvSeq{0, rows, len, false}, by_rows, elsewhere, count, most);
+        const int64_t base = by_rows ? (int64_t)len - rows : 0, have = by_rows ? rows : len;
+        assert(k.bad == (base < 0 || (!elsewhere && count > have) || base + count > 0x7FFFFFFF));
+        if (k.bad) continue;
+        assert(k.length() == base + count && k.length() >= 0);
+        for (int32_t room : sizes) {                             // places of weights behind the last: from here on, 256 threads
+            const int64_t from = k.length_up_to(room);
+            assert(from == (base + count < room ? base + count : room) && from + 255 <= 0x7FFFFFFF);
+        }
+    }
+    assert(kv_kept(KvSeq{0, 0, most, false}, true, true, most, most).bad);
+    assert(kv_kept(KvSeq{0, 0, 5, false}, false, true, -1, most).bad && kv_kept(KvSeq{0, 0, 5, false}, false, true, 8, 7).bad);
+    assert(kv_kept(KvSeq{0, 0, 0, true}, false, true, 0, most).bad);
+    printf("ok\n");
+    return 0;
+}
+'''
+
+
+def test_lengths_of_what_is_kept_fit_on_the_host(tmp_path):
+    src = tmp_path / "kept.cpp"
+    src.write_text(KEPT)
+    exe = tmp_path / "kept"
+    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover", "-I",
+                           os.path.join(ROOT, "paper_2604_00368_amd", "csrc"), "-o", str(exe), str(src)])
+    assert subprocess.check_output([str(exe)]).decode() == "ok\n"
+
+
 # ---- what a call enqueues ------------------------------------------------------------------------
 def scenario_enqueued():
     from paper_2604_00368_amd import binding as T
