@@ -744,7 +744,8 @@ int tent_kv_verify_workspace(const tent_kv_batch *batch, const tent_kv_verify_ar
 
 /* Attention weights onto the tokens: weights_out[s][l][t] = weights[s][l][t] + the sum over the rows that see token t, and the query heads
  * that read head l (with one list all of them), of exp(scale q . k_t - lse); rows see what tent_kv_attend lets them see, not a tree.  Written for all t below max_kv: where nothing sees a
- * token its weight stays.  Rows whose lse is not finite add nothing.  A sequence that is left out, or has no rows, keeps its weights. */
+ * token its weight stays.  Rows whose lse is not finite add nothing.  A sequence that is left out, or has no rows, keeps its weights.  max_rows times the query heads
+ * that read a head is below 2^31 - 1024 (TENT_ERR_RANGE). */
 int tent_kv_weigh(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_weigh_args *args, void *stream);
 int tent_kv_weigh_workspace(const tent_kv_cache *cache, const tent_kv_batch *batch, const tent_kv_weigh_args *args, uint64_t *bytes);
 

@@ -532,6 +532,9 @@ int launch(bool few, WeighArgs g, hipStream_t s)
     });
 }
 
+// Lines of a sequence and head are numbered in 32 bits, those of a last step behind them as well.
+constexpr uint64_t kMostLines = 0x7FFFFFFFull - 1024;
+
 int check(const tent_kv_cache* cache, const tent_kv_batch* batch, const tent_kv_weigh_args* args)
 {
     int rc = kv_check_cache(cache);
@@ -540,6 +543,7 @@ int check(const tent_kv_cache* cache, const tent_kv_batch* batch, const tent_kv_
     if (!args || args->reserved || (args->flags & ~(uint32_t)TENT_KV_ATTEND_ALL)) return TENT_ERR_INVALID;
     if (args->q_heads < 1 || args->q_heads > TENT_KV_MAX_HEADS || args->q_heads % cache->kv_heads) return TENT_ERR_RANGE;
     if (!(args->scale > 0.f) || args->scale > 3.4e38f || args->window > (1u << 30)) return TENT_ERR_RANGE;
+    if (batch->n_seqs && batch->n_rows && (uint64_t)batch->max_rows * (args->q_heads / cache->kv_heads) > kMostLines) return TENT_ERR_RANGE;
     return args->n_lists != 1 && args->n_lists != cache->kv_heads ? TENT_ERR_RANGE : TENT_OK;
 }
 

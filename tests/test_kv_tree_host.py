@@ -105,6 +105,18 @@ def test_weigh_arguments_that_are_refused(T, change, status):  # noqa: F811
     assert T.lib().tent_kv_weigh(make_cache(T), make_batch(T), make_weigh(T, **change), None) == status
 
 
+def test_weigh_refuses_more_lines_than_it_can_number(T):  # noqa: F811
+    # 2^21 rows of 1024 query heads on one: 256 GiB of queries
+    c = make_cache(T, kv_heads=1, head_dim=64, page_stride=2048)
+    for rows, status in ((1 << 21, RANGE), ((1 << 21) - 1, RANGE), ((1 << 21) - 2, 0)):
+        b, n = make_batch(T, n_rows=1 << 21, max_rows=rows, n_seqs=1), C.c_uint64()
+        a = make_weigh(T, q_heads=1024, q_stride=65536, n_lists=1)
+        assert T.lib().tent_kv_weigh_workspace(c, b, a, n) == status
+        if status:
+            assert T.lib().tent_kv_weigh(c, b, a, None) == status
+    assert T.lib().tent_kv_weigh_workspace(c, make_batch(T, n_rows=0, max_rows=0xFFFFFFFF), a, n) == 0
+
+
 @pytest.mark.parametrize("change,status", [
     (dict(weights=None), INVALID), (dict(lists=None), INVALID), (dict(counts=None), INVALID), (dict(lists=0x2002), INVALID), (dict(n_lists=0), RANGE), (dict(n_lists=1025), RANGE),
     (dict(budget=0, first=0, recent=0), RANGE), (dict(budget=(1 << 30) + 1, list_stride=1 << 31), RANGE), (dict(recent=97), RANGE), (dict(first=0xFFFFFFFF, recent=1), RANGE),
