@@ -646,8 +646,8 @@ int tent_kv_attend(const tent_kv_cache *cache, const tent_kv_batch *batch, const
  * tent_kv_verify finds which rows stand, given the target's probabilities and random numbers, and tent_kv_keep makes those the
  * sequence.  A cache that gets too long is cut the same way: tent_kv_weigh adds up the attention that every token has got, tent_kv_choose
  * says which tokens a sequence keeps, tent_kv_keep moves them together.  Everything said above of rows, errors, alignment, streams
- * and graphs holds for them; none takes atomics but the error bits, so results repeat bit for bit.  What a call writes shares
- * no memory with what it reads, unless it says so below: other workgroups may still be reading.
+ * and graphs holds for them; none takes atomics on results but the error bits, so results repeat bit for bit.  What a call writes
+ * shares no memory with what it reads, unless it says so below: other workgroups may still be reading.
  */
 enum { TENT_KV_KEEP_ROWS = 1u << 0 };                       /* tent_kv_keep_args.flags: lists name rows, not tokens   */
 enum { TENT_KV_MAX_VOCAB = 1 << 20 };
@@ -760,7 +760,9 @@ int tent_kv_choose_workspace(const tent_kv_batch *batch, const tent_kv_choose_ar
  * with base = kv_len - its rows, token base + j becomes what token base + lists[s][l][j] was, and kv_len_out is base + counts[s].
  * In place an entry must not be below its own number j, so that lists may name a token twice and nothing is read that was written;
  * with to_table, whose pages must not be ones that are read, entries may be anything below kv_len (below the rows).  An entry that is not
- * is left out and noted (TENT_KV_BAD_POSITION); wrong pages likewise.  Pages that are written are to be of one sequence.  A sequence with a count that is negative, more than
+ * is left out and noted (TENT_KV_BAD_POSITION); wrong pages likewise, whose weights are moved all the same.  Keys move as they are, with the
+ * rotations of the positions that they had: rows that are appended behind them later need `positions` that go on from those, not
+ * from the shorter length.  Pages that are written are to be of one sequence.  A sequence with a count that is negative, more than
  * `most`, more than it has (in place), or makes it 2^31 tokens, with
  * rows of which some are at negative positions, and one that is left out, stay as they are, with their kv_len, noted as
  * TENT_KV_BAD_SEQUENCE. */

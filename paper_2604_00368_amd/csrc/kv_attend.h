@@ -1408,7 +1408,7 @@ struct Shape {
 //
 // Trees of 33 to 64 lines take the wide kernel with two waves to 32 lines; the narrow one has one wave to a SIMD then.  16 rows of 32 heads on
 // 8 of 128 dimensions, narrow, wide and so: 32 of them over 5k tokens in 4 bits 160, 131 and 96 us, in 16 bits 222, 153 and 145; 4 over 32k
-// 138, 86 and 83, 189, 125 and 122; 500 tokens 18.5, and 18.5 so, 20.7 and 16.8; of 64 dimensions 13 and 15.  Of these workgroups 512 are
+// 138, 86 and 83, 189, 125 and 122; 500 tokens 18.5, and 18.5 so, 20.7 and 16.8; of 64 dimensions 13 and 15, which the rule does not follow.  Of these workgroups 512 are
 // enough: 32 trees over 2k to 8k tokens take 149 us with 512, with 256, 1024 and 1536 229, 152 and 168.
 inline Shape shape_of(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_attend_args& a, bool tree)
 {

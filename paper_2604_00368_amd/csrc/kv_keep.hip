@@ -13,8 +13,10 @@ namespace {
 // are held in registers for all of it; more are read again for each digit, or, where lists are few, shared by several workgroups
 // (choose_part_kernel).
 //
-// Barriers and latencies bound it.  Measured: one list of 6,000 tokens 12.7 us, 256 lists of 1,000 to 16,384 tokens, four fifths of whose
-// weights are zero, 25 us (with four digits of 8 bits and no ranks 15.5 and 22.6); one list of 131,072 tokens 43 us, by one workgroup 182.
+// Barriers and latencies bound it.  Measured: one list of 6,000 tokens 12.6 us, 256 lists of 1,000 to 16,384 tokens, four fifths of whose
+// weights are zero, 25.3 us (with four digits of 8 bits and no ranks 15.5 and 22.6: the digits are those of few lists, at a loss of an eighth
+// for many); weights that differ in their last bits only, which take all three digits, 15.4 and, of 256 lists of 16,384, 26.3; one list of
+// 131,072 tokens 43 us, by one workgroup 182.
 struct ChooseArgs {
     tent_kv_choose_args a;
     tent_kv_batch b;
@@ -24,7 +26,7 @@ struct ChoosePartArgs : ChooseArgs {
     uint32_t* counts;                  // [2][lists][parts][kDigits]: of the digits of two launches, in turn
     uint32_t* before;                  // [lists][parts]: weights above the digits found that lie in the parts before
     u32x2* found;                      // [2][lists]: the digits found, and how many weights are wanted of those that have them; in turn, too
-    uint32_t parts, part_tokens;       // workgroups to a list, and their tokens: a multiple of kHeldTokens
+    uint32_t parts, part_tokens;       // workgroups to a list, and their tokens: whole rounds of kChooseThreads, of kHeldTokens in lists that take several
 };
 constexpr uint32_t kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
 constexpr uint32_t kHeld = 16, kHeldTokens = kHeld * kChooseThreads;     // tokens of a thread, and of the workgroup

@@ -470,7 +470,9 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs g)
 // Whether a launch makes the first sums ahead: where a sequence's workgroup would take longer than a launch does, and the sequences are
 // not enough to fill the card by themselves.  Four drafted tokens each, fp32, by itself and with a launch ahead: 64,000 tokens, 1 and 64
 // sequences 16 and 20 us, 18 and 21; 128,000, 8, 64 and 128 sequences 23 and 21, 26 and 23, 30 and 29; 256,000, 1 and 64 sequences 32
-// and 21, 38 and 30.  Two and three launches ahead gain no more for trees than they cost others.
+// and 21, 38 and 30.  In bfloat16, half the bytes, the same way: 64,000 tokens, 1 and 128 sequences 15 and 19, 18 and 20; 128,000, 1, 64 and
+// 128 sequences 21 and 19, 24 and 21, 25 and 25; 256,000, 8 and 128 sequences 29 and 19, 36 and 33.  Two and three launches ahead gain no
+// more for trees than they cost others.
 struct VerifyShape { uint32_t pieces; bool ahead; uint64_t workspace; };
 VerifyShape shape_of(const tent_kv_batch& b, const tent_kv_verify_args& a)
 {

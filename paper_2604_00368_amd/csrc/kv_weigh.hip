@@ -492,8 +492,9 @@ __global__ void __launch_bounds__(256) weigh_join_kernel(const WeighArgs g)
     g.out[at] = (g.weights ? g.weights[at] : 0.f) + total;
 }
 
-// Lines that few_kernel holds.  32 rows over 5,120 tokens, 8 heads of 128 dimensions, few_kernel and many_kernel: 4 lines in 4 bits 27 and 244 us, in
-// 16 bits 70 and 312; 32 lines 37 and 245, 74 and 312.
+// Lines that few_kernel holds; it has no form for more.  32 sequences of 5,120 tokens, 8 heads of 128 dimensions, few_kernel and many_kernel: 4 lines in
+// 4 bits 27 and 244 us, in 16 bits 70 and 312; 32 lines 37 and 245, 74 and 312.  So a step over a cache is slow from 33 lines on: 33 to 64 lines 245
+// and 310 us, 128 lines 257 and 325, the latencies of a tile with one step of products.
 bool few_lines(const tent_kv_cache& c, const tent_kv_batch& b, const tent_kv_weigh_args& a)
 {
     return (uint64_t)b.max_rows * (a.q_heads / c.kv_heads) <= 32;

@@ -561,7 +561,8 @@ def keep(cache: Cache, batch: Batch, lists, counts, rows: bool = False, to_table
     Token j becomes what token lists[sequence, (head,) j] was, for j below counts[sequence]; one list for all heads or one for each.  With
     rows=True lists name rows of the sequence (verify's path) and the context in front of them stays.  In place, unless to_table
     (int32 [sequences, pages]) names other pages to write to.  weights: float32 [sequences, (heads,) max_kv or more], moved to weights_out
-    (in place itself unless given; a new tensor with to_table), behind the last kept token 0.  kv_len_out shares no memory with what is
+    (in place itself unless given; a new tensor with to_table), behind the last kept token 0.  Keys keep the rotations that they have:
+    after an eviction append takes `positions` that go on from the tokens' own, not from the shorter length.  kv_len_out shares no memory with what is
     read, nor with the batch's kv_len: heads whose turn comes later still read that."""
     if stream is not None or cache.index != _current_device():
         used = [x for x in (*cache.tensors, *batch.tensors, lists, counts, to_table, weights, weights_out, kv_len_out) if x is not None]
