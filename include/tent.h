@@ -720,6 +720,7 @@ typedef struct {
     uint32_t most;             /* most entries of a list, at most list_stride                      */
     uint32_t flags;            /* TENT_KV_KEEP_ROWS                                                */
     uint32_t reserved;         /* 0                                                                */
+    uint32_t to_entries;       /* pages of a sequence in to_table, at most to_stride; 0: to_stride  */
 } tent_kv_keep_args;
 
 /* tent_kv_attend for rows that are a tree (or anything else that masks say): with base = kv_len - its sequence's rows, a row sees the

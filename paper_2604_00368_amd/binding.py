@@ -120,7 +120,7 @@ class tent_kv_choose_args(C.Structure):
 class tent_kv_keep_args(C.Structure):
     _fields_ = [("lists", C.c_void_p), ("counts", C.c_void_p), ("to_table", C.c_void_p), ("kv_len_out", C.c_void_p), ("weights", C.c_void_p),
                 ("weights_out", C.c_void_p), ("list_stride", C.c_uint64), ("weights_stride", C.c_uint64), ("n_lists", C.c_uint32),
-                ("n_weights", C.c_uint32), ("to_stride", C.c_uint32), ("most", C.c_uint32), ("flags", C.c_uint32), ("reserved", C.c_uint32)]
+                ("n_weights", C.c_uint32), ("to_stride", C.c_uint32), ("most", C.c_uint32), ("flags", C.c_uint32), ("reserved", C.c_uint32), ("to_entries", C.c_uint32)]
 
 
 class TentError(RuntimeError):

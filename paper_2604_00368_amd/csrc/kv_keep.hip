@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(256) keep_copy_kernel(const KeepArgs g)
             kv_note(g.b.errors, TENT_KV_BAD_POSITION);
         } else {
             read = place_of(g.c, g.b.page_table + (uint64_t)seq * g.b.table_stride, g.b.table_stride, (uint32_t)(k.base + entry), head);
-            write = place_of(g.c, a.to_table + (uint64_t)seq * a.to_stride, a.to_stride, (uint32_t)(k.base + j), head);
+            write = place_of(g.c, a.to_table + (uint64_t)seq * a.to_stride, a.to_entries, (uint32_t)(k.base + j), head);
             if (read.page == kNowhere || write.page == kNowhere) {
                 kv_note(g.b.errors, TENT_KV_BAD_PAGE);
                 read.page = kNowhere;
@@ -714,13 +714,14 @@ extern "C" int tent_kv_keep(const tent_kv_cache* cache, const tent_kv_batch* bat
     if ((!args->weights) != (!args->weights_out) || (args->to_table && args->weights && args->weights == args->weights_out)) return TENT_ERR_INVALID;
     const uint64_t most = ((uint64_t)1 << 60) / ((uint64_t)batch->n_seqs * cache->kv_heads);
     if ((args->n_lists != 1 && args->n_lists != cache->kv_heads) || args->most > (1u << 30)) return TENT_ERR_RANGE;
-    if (args->list_stride < args->most || args->list_stride > most) return TENT_ERR_RANGE;
+    if (args->list_stride < args->most || args->list_stride > most || args->to_entries > args->to_stride) return TENT_ERR_RANGE;
     if (args->weights) {
         if ((args->n_weights != 1 && args->n_weights != cache->kv_heads) || args->n_weights < args->n_lists) return TENT_ERR_RANGE;
         if (args->weights_stride < batch->max_kv || args->weights_stride > most) return TENT_ERR_RANGE;
         if (kv_lists_meet(args->weights, args->weights_out, (uint64_t)batch->n_seqs * args->n_weights, batch->max_kv, args->weights_stride)) return TENT_ERR_INVALID;
     }
     KeepArgs g{kv_cache_dev(*cache), *batch, *args, 1, 1, 0};
+    if (!g.a.to_entries) g.a.to_entries = g.a.to_stride;
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define TENT_KEEP(dim) (cache->bits == 16 ? launch_keep<dim, 16>(g, s) : launch_keep<dim, 4>(g, s))
     rc = cache->head_dim == 64 ? TENT_KEEP(64) : cache->head_dim == 128 ? TENT_KEEP(128) : TENT_KEEP(256);

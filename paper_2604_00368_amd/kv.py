@@ -577,9 +577,13 @@ def keep(cache: Cache, batch: Batch, lists, counts, rows: bool = False, to_table
         _on_gpu(to_table, "to_table", torch.int32)
         if to_table.dim() != 2 or to_table.shape[0] != n_seqs or to_table.device != device or (to_table.shape[1] > 1 and to_table.stride(1) != 1):
             raise ValueError("to_table must be [sequences, pages] with contiguous rows, on the cache's device")
-        a.to_table, a.to_stride = to_table.data_ptr(), to_table.stride(0) if n_seqs > 1 else to_table.shape[1]
-        if n_seqs > 1 and a.to_stride < to_table.shape[1]:
-            raise ValueError("rows of to_table overlap")
+        entries = to_table.shape[1]
+        to_stride = to_table.stride(0) if n_seqs > 1 else entries
+        if n_seqs and not entries:                                       # no address either: it would be taken for none
+            raise ValueError("to_table names no pages")
+        if not entries <= to_stride < 1 << 32:
+            raise ValueError("rows of to_table overlap, or are too far apart")
+        a.to_table, a.to_stride, a.to_entries = to_table.data_ptr(), to_stride, entries
     if weights is not None:
         a.n_weights, a.weights_stride = _by_list(weights, "weights", torch.float32, n_seqs, batch.max_kv, device)
         if weights_out is None:

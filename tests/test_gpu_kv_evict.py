@@ -521,6 +521,22 @@ def test_keep_refuses_a_table_that_is_too_short_entry_by_entry(kv):
         assert (raw(s, pool, i, 32, to) == old[i][63:31:-1]).all()
 
 
+def test_keep_writes_to_no_page_between_the_rows_of_a_table(kv):
+    # the table's rows lie behind the sequences' own in one tensor: behind the first row's end are the second sequence's pages
+    s = Setup(kv, [0, 0], [64, 64], BF16, 16, 2, 2, 64, 16, seed=34)
+    pool = torch.cat([s.k_pool, torch.zeros(4, 16, 2, 64, dtype=BF16, device="cuda")])
+    cache = kv.Cache(pool, pool.clone())
+    both = torch.cat([s.table, torch.arange(4).reshape(2, 2).int() + pool.shape[0] - 4], 1).cuda()
+    batch = kv.Batch(both[:, :4], s.batch.kv_len, s.batch.row_start, 0, 0, 64)
+    old = pool.clone()
+    lists = torch.arange(63, 13, -1, dtype=torch.int32).repeat(2, 1)
+    length = kv.keep(cache, batch, lists.cuda(), torch.tensor([50, 33], **I32), to_table=both[:, 4:])
+    assert length.tolist() == [50, 33] and int(batch.errors) == T.TENT_KV_BAD_PAGE
+    assert torch.equal(pool[:-4], old[:-4])
+    for i in range(2):
+        assert (raw(s, pool, i, 32, both[:, 4:].cpu()) == raw(s, old, i)[63:31:-1]).all()
+
+
 def test_empty_lists_and_empty_sequences(kv):
     s = Setup(kv, [0, 0], [20, 30], BF16, 16, 2, 2, 64, 16, seed=33)
     old = s.k_pool.clone()

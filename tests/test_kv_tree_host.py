@@ -138,6 +138,11 @@ def test_keep_arguments_that_are_refused(T, change, status):  # noqa: F811
     assert T.lib().tent_kv_keep(make_cache(T), make_batch(T), make_keep(T, **change), None) == status
 
 
+def test_keep_refuses_more_pages_than_lie_between_rows(T):  # noqa: F811
+    for entries in (65, 0xFFFFFFFF):
+        assert T.lib().tent_kv_keep(make_cache(T), make_batch(T), make_keep(T, to_table=0x9000, to_stride=64, to_entries=entries), None) == RANGE
+
+
 def test_nothing_to_do_needs_no_device(T):  # noqa: F811
     assert set(calls(T, make_cache(T), make_batch(T, n_seqs=0, page_table=None)).values()) == {0}
     assert calls(T, make_cache(T), make_batch(T, n_rows=0, page_table=None))["tree"] == 0

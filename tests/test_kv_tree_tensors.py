@@ -238,6 +238,26 @@ def test_strides_are_handed_on(gpus):
     assert gpus.args.weights != gpus.args.weights_out                    # to other pages: not in place
 
 
+def test_tables_to_move_to_end_with_their_rows(gpus):
+    """What lies between the rows of a table is not its own, and a table of no pages is not taken for none."""
+    s = Step(gpus)
+    on, i32 = s.on, torch.int32
+    for table, stride, entries in ((torch.zeros(2, 8, dtype=i32)[:, 5:], 8, 3), (torch.zeros(2, 3, dtype=i32), 3, 3), (torch.zeros(2, 8, dtype=i32)[:, :1], 8, 1)):
+        s.keep(to_table=on(table))
+        assert (gpus.args.to_stride, gpus.args.to_entries) == (stride, entries) and gpus.args.to_table == table.data_ptr()
+    s.keep()
+    assert gpus.args.to_table is None and gpus.args.to_entries == 0
+    n = len(gpus.log)
+    far = torch.zeros(5, dtype=i32)
+    for table in (torch.zeros(2, 0, dtype=i32), torch.zeros(2, 8, dtype=i32)[:, 3:3], far.as_strided((2, 3), (2, 1))):
+        with pytest.raises(ValueError, match="to_table"):
+            s.keep(to_table=on(table))
+    assert not any(e[0] in NAMES for e in gpus.log[n:])
+    nobody = kv.Batch(on(torch.zeros(0, 3, dtype=i32)), on(torch.zeros(0, dtype=i32)), on(torch.zeros(1, dtype=i32)), 0, 0, 20)
+    kv.keep(s.cache, nobody, on(torch.zeros(0, 7, dtype=i32)), on(torch.zeros(0, dtype=i32)), to_table=on(torch.zeros(0, 3, dtype=i32)))
+    assert gpus.log[-1][0] == "keep"
+
+
 def test_outputs_that_share_memory_with_what_is_read_are_refused(gpus):
     s = Step(gpus)
     i32 = torch.int32
